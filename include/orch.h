@@ -363,6 +363,105 @@ int orch_op_attention_noalloc(const void* q, const void* kv_stale, size_t stale_
                               int n_fresh, int B, int heads, int n_q, int n_kv, int head_dim,
                               void* out, int dtype, void* hip_stream);
 
+/* ---- rotary positions and the 8-bit K/V cache ------------------------------
+ * Between the QKV projection and the attention: rotary positions of a band's
+ * Q and K, the stale K/V of the image held in 8 bits (half of bf16's bytes, a
+ * quarter of fp32's, to hold and to exchange with a peer), and the attention
+ * that reads it.  head_dim as in orch_dit_config.  Device pointers of K/V
+ * buffers, Q, cache values and outputs are 16-byte aligned. */
+
+/* Rotary positions on a grid of frames x rows x columns (extent[0..2]): token n
+ * lies at frame f, row r, column c with n = (f * rows + r) * columns + c.  Axis
+ * a (0 time, 1 height, 2 width) rotates channels[a] channels of every head
+ * (even, may be 0), the axes' channels one after the other from channel 0;
+ * channels past them pass through.  Pair i of axis a turns by the angle
+ * (index + origin[a]) * step[a] * theta^(-2 i / channels[a]):
+ *   x' = x cos - y sin,  y' = x sin + y cos.
+ * interleaved != 0: the pairs are neighbours (2 i, 2 i + 1); 0: half an axis
+ * apart (i, i + channels[a] / 2).  Negated steps give the inverse, which is
+ * also the gradient with respect to the input. */
+typedef struct {
+  int channels[3], extent[3];
+  double origin[3], step[3];
+  double theta;               /* > 0 */
+  int interleaved;
+} orch_rotary_axes;
+
+/* One tensor to rotate: element (b, h, i, c) of branch b, head h, token i of the
+ * call at x[b * x_stride[0] + h * x_stride[1] + i * x_stride[2] + c], strides in
+ * elements; out likewise.  out may be x with the same strides (in place). */
+typedef struct {
+  const void* x;
+  void* out;
+  int heads;
+  size_t x_stride[3], out_stride[3];
+} orch_rotary_tensor;
+
+/* Rotary positions of tokens [token_begin, token_begin + n_tok) of the grid, in
+ * one launch for n_tensors (1 or 2, e.g. Q and K) tensors T of head_dim
+ * channels.  Angles are reduced in fp64, so that far positions keep their
+ * places; sines, cosines and products are fp32, rounded once to T.  Every
+ * alignment and stride is taken; 16-byte aligned rows are fastest.  An out that
+ * overlaps an x in any other way than in place is undefined.  Errors: ORCH_EINVAL
+ * (axes, tokens outside the grid, strides shorter than head_dim, NULL). */
+int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tensors, int n_tensors,
+                   int B, int n_tok, int token_begin, int head_dim, int dtype, void* hip_stream);
+
+/* The 8-bit K/V cache of `tokens` tokens.  Branch b holds, from values +
+ * b * values_stride (bytes), e4m3 bytes (OCP: largest 448, no infinity) K
+ * [heads][tokens][head_dim], then V [heads][tokens][head_dim]; from exponents +
+ * b * exponents_stride (bytes) one E8M0 byte e for each of K [heads][tokens], then
+ * V [heads][tokens]: an element stands for value * 2^(e - 127).  V is token-major
+ * here, unlike in the buffer of the operand type: a token's values share one
+ * scale, so a band of tokens is a set of contiguous runs (one per head for each of
+ * K and V) whatever its offset, and a token's bytes depend on that token alone.
+ * values_stride % 16 == 0. */
+typedef struct {
+  void* values;
+  void* exponents;
+  size_t values_stride, exponents_stride;
+  int tokens;
+} orch_quantized_kv;
+
+/* Quantise as written: tokens [kv_offset, kv_offset + n_tok) of the K/V buffer
+ * kv (T, branch stride kv_branch_stride elements, K [heads][kv_tokens][head_dim], then V^T
+ * [heads][head_dim][kv_tokens], as orch_op_qkv_projection writes it) into the
+ * cache's tokens [tok_offset, tok_offset + n_tok); other tokens of the cache are
+ * not touched.  Per token, head and K or V the scale is the smallest power of
+ * two s >= 2^-126 with |x| <= 448 s for every finite x, and a value is x / s
+ * rounded to nearest, ties to even (magnitudes past 1.875 2^127 as 1.875 2^127).  An
+ * infinity or NaN is held as NaN.  Errors: ORCH_EINVAL (shape, ranges, alignment, NULL). */
+int orch_op_kv_quantize(const void* kv, size_t kv_branch_stride, int kv_tokens, int kv_offset,
+                        const orch_quantized_kv* cache, int tok_offset, int B, int heads,
+                        int n_tok, int head_dim, int dtype, void* hip_stream);
+
+/* Read back: the cache's tokens [tok_offset, tok_offset + n_tok) into tokens
+ * [kv_offset, kv_offset + n_tok) of the K/V buffer kv (layout as above), e.g. the
+ * stale buffer of orch_patch_denoise_step; other tokens are not touched.  Exact: every value of the cache
+ * whose scale orch_op_kv_quantize wrote is a bf16 number (below 2^-126 to the
+ * nearest subnormal one).  Errors as above. */
+int orch_op_kv_dequantize(const orch_quantized_kv* cache, int tok_offset, void* kv,
+                          size_t kv_branch_stride, int kv_tokens, int kv_offset, int B, int heads,
+                          int n_tok, int head_dim, int dtype, void* hip_stream);
+
+/* orch_op_attention with the stale K/V in the 8-bit cache: O = softmax(Q K^T /
+ * sqrt(d)) V over cache->tokens keys, those of [fresh_begin, fresh_begin +
+ * n_fresh) from kv_fresh (T, as there), the others from the cache.  q, out and the
+ * branch layout as there.  Every key and query count and every band is taken at full width.  workspace: device
+ * memory (16-byte aligned) of at least orch_attention_quantized_workspace_bytes() bytes lets few queries
+ * split the keys over more workgroups; NULL (or fewer bytes) runs unsplit.  The
+ * result does not depend on the split beyond rounding.  Errors: ORCH_EINVAL (as
+ * orch_op_attention; alignment; tokens * head_dim of 2^31 or more), ORCH_EHIP. */
+int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache,
+                                const void* kv_fresh, size_t fresh_branch_stride, int fresh_begin,
+                                int n_fresh, int B, int heads, int n_q, int head_dim, void* out,
+                                void* workspace, size_t workspace_bytes, int dtype,
+                                void* hip_stream);
+
+/* Workspace bytes orch_op_attention_quantized can use for this shape (0: never splits). */
+size_t orch_attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int head_dim,
+                                                int dtype);
+
 /* Conditioning of the loaded model: out fp32 [cfg_batch][6*H*n_blocks + 2*H],
  * the adaLN vectors of every block followed by the final layer's
  * (shift, scale), for timestep t and host labels[cfg_batch]. */

@@ -24,6 +24,8 @@ Modules:
               devices).
   unet     -- a U-Net block (GroupNorm -> SiLU -> conv3x3) on a band of rows
               with stale halo rows and stale group statistics (§II-B).
+  kvcache  -- rotary positions on a grid, the 8-bit K/V cache (e4m3 values,
+              power-of-two scales) and attention over it.
 
 Parity status: the scheduler, attention, LayerNorm, GELU, sinusoid, patch
 embedding and unpatchify are pinned by the CPU tests; the DiT block as a

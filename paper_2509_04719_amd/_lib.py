@@ -27,7 +27,9 @@ SYMBOLS = (
     "orch_linear_workspace_bytes",
     "orch_plan_devices", "orch_sample_patch_parallel", "orch_set_work_split",
     "orch_op_attention_noalloc", "orch_speeds_from_profiles", "orch_unet_conv_band",
-    "orch_unet_conv_workspace_bytes",
+    "orch_unet_conv_workspace_bytes", "orch_op_rotary", "orch_op_kv_quantize",
+    "orch_op_kv_dequantize", "orch_op_attention_quantized",
+    "orch_attention_quantized_workspace_bytes",
 )
 KCLASSES = ("conditioning", "patch_embed", "layernorm", "qkv_gemm", "attention", "proj_gemm",
             "fc1_gemm", "fc2_gemm", "final_layer", "update")
@@ -42,6 +44,21 @@ class OrchError(RuntimeError):
 class UNetConvShape(C.Structure):
     _fields_ = [("height", C.c_int), ("width", C.c_int), ("channels", C.c_int),
                 ("groups", C.c_int), ("out_channels", C.c_int), ("eps", C.c_float)]
+
+
+class RotaryAxes(C.Structure):
+    _fields_ = [("channels", C.c_int * 3), ("extent", C.c_int * 3), ("origin", C.c_double * 3),
+                ("step", C.c_double * 3), ("theta", C.c_double), ("interleaved", C.c_int)]
+
+
+class RotaryTensor(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("heads", C.c_int),
+                ("x_stride", C.c_size_t * 3), ("out_stride", C.c_size_t * 3)]
+
+
+class QuantizedKV(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("exponents", C.c_void_p), ("values_stride", C.c_size_t),
+                ("exponents_stride", C.c_size_t), ("tokens", C.c_int)]
 
 
 class OrchConfig(C.Structure):
@@ -94,6 +111,12 @@ def _load():
         "orch_unet_conv_workspace_bytes": (sz, [C.POINTER(UNetConvShape), i]),
         "orch_unet_conv_band": (i, [C.POINTER(UNetConvShape), i, i, vp, vp, vp, vp, vp, vp, vp, i,
                                     vp, vp, sz, vp]),
+        "orch_op_rotary": (i, [C.POINTER(RotaryAxes), C.POINTER(RotaryTensor), i, i, i, i, i, i, vp]),
+        "orch_op_kv_quantize": (i, [vp, sz, i, i, C.POINTER(QuantizedKV), i, i, i, i, i, i, vp]),
+        "orch_op_kv_dequantize": (i, [C.POINTER(QuantizedKV), i, vp, sz, i, i, i, i, i, i, i, vp]),
+        "orch_op_attention_quantized": (i, [vp, C.POINTER(QuantizedKV), vp, sz, i, i, i, i, i, i, vp,
+                                            vp, sz, i, vp]),
+        "orch_attention_quantized_workspace_bytes": (sz, [i, i, i, i, i, i]),
         "orch_sample_patch_parallel": (i, [vp, vp, i, C.POINTER(i), C.POINTER(i), C.POINTER(i), i, i,
                                            C.POINTER(i), f, vp, vp, vp]),
     }
@@ -125,6 +148,14 @@ def _stream(stream=None):
     import torch
     s = torch.cuda.current_stream() if stream is None else stream
     return s.cuda_stream
+
+
+def _code(t):
+    """The library's code of a tensor's type."""
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise OrchError(ORCH_EINVAL, f"type {t.dtype} not supported")
+    return ORCH_F32 if t.dtype == torch.float32 else ORCH_BF16
 
 
 def schedule_coefficients(cfg, t: int, t_prev: int, eta: float = 0.0):
@@ -272,6 +303,69 @@ def attention(q, kv_stale, stale_bs, kv_fresh, fresh_bs, fresh_begin, n_fresh, B
     check(lib.orch_op_attention(_ptr(q), _ptr(kv_stale), stale_bs, _ptr(kv_fresh), fresh_bs,
                                 fresh_begin, n_fresh, B, heads, n_q, n_kv, head_dim, _ptr(out),
                                 _ptr(workspace), ws_bytes, dtype, _stream(stream)))
+
+
+def rotary_axes(channels, extent, theta=1e4, origin=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0),
+                interleaved=True) -> RotaryAxes:
+    """Rotary positions of a (frames, rows, columns) grid, see orch_rotary_axes."""
+    return RotaryAxes((C.c_int * 3)(*channels), (C.c_int * 3)(*extent), (C.c_double * 3)(*origin),
+                      (C.c_double * 3)(*step), float(theta), int(interleaved))
+
+
+def rotary(axes: RotaryAxes, token_begin, x, out, stream=None):
+    """Rotate x into out: tensors (or pairs of tensors, e.g. Q and K) [B, heads, n_tok, d] of any
+    strides, their channels next to each other.  out may be x."""
+    xs, outs = (x, out) if isinstance(x, (tuple, list)) else ((x,), (out,))
+    B, _, n_tok, d = xs[0].shape
+    if len(xs) != len(outs):
+        raise OrchError(ORCH_EINVAL, "as many outputs as inputs are needed")
+    ts = (RotaryTensor * len(xs))()
+    for t, a, b in zip(ts, xs, outs):
+        if a.shape != b.shape or a.dtype != xs[0].dtype or b.dtype != a.dtype:
+            raise OrchError(ORCH_EINVAL, "inputs and outputs must agree in shape and type")
+        if (a.shape[0], a.shape[2], a.shape[3]) != (B, n_tok, d) or a.stride(3) != 1 or b.stride(3) != 1:
+            raise OrchError(ORCH_EINVAL, "tensors must be [B, heads, n_tok, d] with channels next to each other")
+        t.x, t.out, t.heads = a.data_ptr(), b.data_ptr(), a.shape[1]
+        t.x_stride[:], t.out_stride[:] = a.stride()[:3], b.stride()[:3]
+    check(lib.orch_op_rotary(C.byref(axes), ts, len(xs), B, n_tok, token_begin, d, _code(xs[0]),
+                             _stream(stream)))
+
+
+def quantized_kv(values, exponents) -> QuantizedKV:
+    """The 8-bit K/V cache held by two tensors: e4m3 (or uint8) values [B, 2, heads, tokens, d]
+    and uint8 exponents [B, 2, heads, tokens], contiguous within a branch.  The caller keeps them."""
+    B, two, heads, tokens, d = values.shape
+    if two != 2 or tuple(exponents.shape) != (B, 2, heads, tokens):
+        raise OrchError(ORCH_EINVAL, "values [B, 2, heads, tokens, d] and exponents [B, 2, heads, tokens] are needed")
+    if values.element_size() != 1 or exponents.element_size() != 1:
+        raise OrchError(ORCH_EINVAL, "values and exponents must be of one byte")
+    if not (values[0].is_contiguous() and exponents[0].is_contiguous()):
+        raise OrchError(ORCH_EINVAL, "a branch's values and exponents must be contiguous")
+    return QuantizedKV(values.data_ptr(), exponents.data_ptr(), values.stride(0), exponents.stride(0), tokens)
+
+
+def kv_quantize(kv, kv_branch_stride, kv_tokens, kv_offset, cache: QuantizedKV, tok_offset, B, heads,
+                n_tok, head_dim, dtype, stream=None):
+    check(lib.orch_op_kv_quantize(_ptr(kv), kv_branch_stride, kv_tokens, kv_offset, C.byref(cache),
+                                  tok_offset, B, heads, n_tok, head_dim, dtype, _stream(stream)))
+
+
+def kv_dequantize(cache: QuantizedKV, tok_offset, kv, kv_branch_stride, kv_tokens, kv_offset, B, heads,
+                  n_tok, head_dim, dtype, stream=None):
+    check(lib.orch_op_kv_dequantize(C.byref(cache), tok_offset, _ptr(kv), kv_branch_stride, kv_tokens,
+                                    kv_offset, B, heads, n_tok, head_dim, dtype, _stream(stream)))
+
+
+def attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype) -> int:
+    return lib.orch_attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype)
+
+
+def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, n_fresh, B, heads, n_q,
+                        head_dim, out, dtype, workspace=None, stream=None):
+    ws_bytes = 0 if workspace is None else workspace.nbytes
+    check(lib.orch_op_attention_quantized(_ptr(q), C.byref(cache), _ptr(kv_fresh), fresh_bs, fresh_begin,
+                                          n_fresh, B, heads, n_q, head_dim, _ptr(out), _ptr(workspace),
+                                          ws_bytes, dtype, _stream(stream)))
 
 
 def unet_shape(cfg, eps: float = 1e-5) -> UNetConvShape:

@@ -20,7 +20,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liborch.so")
 SOURCES = ["k_gemm.hip", "k_attention.hip", "k_attention_general.hip", "k_misc.hip", "k_unet.hip", "orch_abi.hip",
-           "orch_plan.hip", "orch_noalloc.hip"]
+           "orch_plan.hip", "orch_noalloc.hip", "k_rotary.hip", "k_kvcache.hip", "k_attention_quantized.hip",
+           "orch_cache.hip"]
 # per-source extra flags: attention is built without IEEE NaN quieting, so the
 # row max of the online softmax is plain v_max3_f32
 EXTRA = {"k_attention.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"]}

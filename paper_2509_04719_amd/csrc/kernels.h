@@ -168,4 +168,58 @@ size_t unet_conv_workspace_bytes(int W, int C, int G, int C_out, int rows);
 constexpr size_t kUNetMaxTileBytes = (size_t)1 << 31;
 hipError_t launch_unet_conv(const UNetConvParams& p, void* workspace, hipStream_t stream);
 
+// Rotary positions (k_rotary.hip).
+struct RotaryTensor {
+  const void* x;              // T, element (b, h, n, c) at b * xs[0] + h * xs[1] + n * xs[2] + c
+  void* out;                  // T, strides os; may be x with equal strides
+  int heads;
+  size_t xs[3], os[3];
+};
+constexpr int kRotaryMaxPairs = 128;
+struct RotaryParams {
+  RotaryTensor t[2];
+  int n_t, B, n_tok, d, token_begin;
+  int rows, cols;             // token n = (frame * rows + row) * cols + column
+  int pairs[3];               // rotated pairs of each axis, in this order
+  int interleaved;
+  double origin[3];           // position of index i: (i + origin)
+  // turns (angle / 2 pi) per unit of position, the axis' step included
+  double turns[kRotaryMaxPairs];
+};
+hipError_t launch_rotary(const RotaryParams& p, int dtype, hipStream_t stream);
+
+// The 8-bit K/V cache (k_kvcache.hip): e4m3 values K [heads][tokens][d], then V
+// [heads][tokens][d], and E8M0 exponents K [heads][tokens], then V, per branch.
+struct KvCache {
+  unsigned char* values;
+  unsigned char* exps;
+  size_t values_bs, exps_bs;  // bytes between branches
+  int tokens;
+};
+struct KvCacheParams {
+  KvCache c;
+  int c_off;                  // cache token of the first one
+  void* kv;                   // T buffer: K [heads][kv_tokens][d], V^T [heads][d][kv_tokens]
+  size_t kv_bs;               // elements between branches
+  int kv_tokens, kv_off;
+  int B, heads, d, n;
+};
+hipError_t launch_kv_quantize(const KvCacheParams& p, int dtype, hipStream_t stream);
+hipError_t launch_kv_dequantize(const KvCacheParams& p, int dtype, hipStream_t stream);
+
+// Attention over fresh K/V and the 8-bit cache (k_attention_quantized.hip).
+struct AttnQParams {
+  const void* q;              // T [B][heads][n_q][d]
+  KvCache c;                  // every token, c.tokens keys
+  const void* kv_fresh;       // T, K [heads][n_fresh][d], V^T [heads][d][n_fresh]
+  size_t fresh_bs;
+  int fresh_begin, n_fresh;
+  int B, heads, n_q, d;
+  void* out;                  // T [B][n_q][heads * d]
+  void* ws;                   // parts of queries whose keys are split, see the .hip
+  size_t ws_bytes;
+};
+size_t attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int d, int dtype);
+hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream_t stream);
+
 }  // namespace orch

@@ -1,0 +1,203 @@
+// C ABI of the rotary positions, the 8-bit K/V cache and the attention that
+// reads it: argument checks and launches.  Nothing here allocates or throws.
+#include <cmath>
+#include <cstdarg>
+#include <cstdint>
+#include <cstdio>
+
+#include "../../include/orch.h"
+#include "common.h"
+#include "kernels.h"
+
+using namespace orch;
+
+namespace orch_detail {
+int set_error(int code, const char* msg);
+}
+
+namespace {
+
+int fail(const char* fmt, ...) __attribute__((format(printf, 1, 2)));
+int fail(const char* fmt, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return orch_detail::set_error(ORCH_EINVAL, buf);
+}
+
+int launched(hipError_t e, const char* what) {
+  if (e == hipSuccess) return ORCH_OK;
+  char buf[256];
+  snprintf(buf, sizeof buf, "%s: %s", what, hipGetErrorString(e));
+  return orch_detail::set_error(ORCH_EHIP, buf);
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  if (!a || !b || na == 0 || nb == 0) return false;
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+// heads, branches, head size and type that every entry point takes
+int check_common(int B, int heads, int head_dim, int dtype) {
+  if (B < 1 || heads < 1 || (long long)B * heads > 32767) return fail("bad shape: B and heads must be >= 1, B * heads <= 32767");
+  if (!(head_dim == 32 || head_dim == 64 || head_dim == 72 || head_dim == 80 || head_dim == 96 || head_dim == 128))
+    return fail("head_dim %d not supported", head_dim);
+  if (dtype != ORCH_F32 && dtype != ORCH_BF16) return fail("bad dtype");
+  return ORCH_OK;
+}
+
+// a cache of B branches; its extents in bytes
+int check_cache(const orch_quantized_kv* c, int B, int heads, int d, size_t* values, size_t* exps) {
+  if (!c || !c->values || !c->exponents) return fail("NULL cache");
+  if (c->tokens < 1) return fail("the cache's tokens must be >= 1");
+  if ((long long)c->tokens * d >= 1ll << 31) return fail("cache tokens * head_dim must be below 2^31");
+  const size_t e = (size_t)2 * heads * c->tokens, v = e * d;
+  if (B > 1 && (c->values_stride < v || c->exponents_stride < e)) return fail("the cache's branch stride is too small");
+  if (!aligned16(c->values) || (B > 1 && c->values_stride % 16)) return fail("cache values must be 16-byte aligned");
+  *values = (B > 1 ? (B - 1) * c->values_stride : 0) + v;
+  *exps = (B > 1 ? (B - 1) * c->exponents_stride : 0) + e;
+  if (overlap(c->values, *values, c->exponents, *exps)) return fail("the cache's values and exponents overlap");
+  return ORCH_OK;
+}
+
+// checks and parameters of writing and reading back
+int kv_params(KvCacheParams* p, const void* kv, size_t kv_bs, int kv_tokens, int kv_off, const orch_quantized_kv* c,
+              int c_off, int B, int heads, int n, int d, int dtype) {
+  if (!kv) return fail("NULL pointer");
+  int rc = check_common(B, heads, d, dtype);
+  if (rc) return rc;
+  size_t values, exps;
+  rc = check_cache(c, B, heads, d, &values, &exps);
+  if (rc) return rc;
+  if (n < 0 || kv_off < 0 || c_off < 0 || kv_tokens < 1 || n > kv_tokens - kv_off || n > c->tokens - c_off)
+    return fail("tokens [%d, %d + %d) of %d, [%d, %d + %d) of the cache's %d", kv_off, kv_off, n, kv_tokens, c_off,
+                c_off, n, c->tokens);
+  if ((long long)kv_tokens * d >= 1ll << 31) return fail("kv_tokens * head_dim must be below 2^31");
+  const size_t es = dtype == ORCH_BF16 ? 2 : 4, H = (size_t)heads * d, elems = 2 * (size_t)kv_tokens * H;
+  if (B > 1 && kv_bs < elems) return fail("branch stride too small");
+  if (!aligned16(kv) || (B > 1 && kv_bs * es % 16)) return fail("the K/V buffer must be 16-byte aligned");
+  const size_t bytes = ((B > 1 ? (B - 1) * kv_bs : 0) + elems) * es;
+  if (overlap(kv, bytes, c->values, values) || overlap(kv, bytes, c->exponents, exps))
+    return fail("the K/V buffer and the cache overlap");
+  p->c.values = (unsigned char*)c->values; p->c.exps = (unsigned char*)c->exponents;
+  p->c.values_bs = c->values_stride; p->c.exps_bs = c->exponents_stride; p->c.tokens = c->tokens;
+  p->c_off = c_off; p->kv = const_cast<void*>(kv); p->kv_bs = kv_bs; p->kv_tokens = kv_tokens; p->kv_off = kv_off;
+  p->B = B; p->heads = heads; p->d = d; p->n = n;
+  return ORCH_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tensors, int n_tensors, int B, int n_tok,
+                   int token_begin, int head_dim, int dtype, void* hip_stream) {
+  if (!axes || !tensors) return fail("NULL pointer");
+  if (n_tensors < 1 || n_tensors > 2) return fail("n_tensors must be 1 or 2");
+  int rc = check_common(B, 1, head_dim, dtype);
+  if (rc) return rc;
+  RotaryParams p{};
+  long long tokens = 1;
+  int channels = 0, pair = 0;
+  if (!(axes->theta > 0.0) || !std::isfinite(axes->theta)) return fail("theta must be finite and > 0");
+  for (int a = 0; a < 3; ++a) {
+    const int ch = axes->channels[a], ext = axes->extent[a];
+    if (ch < 0 || ch % 2 || ch > head_dim - channels) return fail("axis channels must be even, >= 0 and at most head_dim in all");
+    if (ext < 1 || ext > 0x7fffffffll / tokens) return fail("grid extents must be >= 1 and their product below 2^31");
+    if (!std::isfinite(axes->origin[a]) || !std::isfinite(axes->step[a])) return fail("origin and step must be finite");
+    channels += ch;
+    tokens *= ext;
+    p.pairs[a] = ch / 2;
+    p.origin[a] = axes->origin[a];
+    // theta^(-2 i / channels), one multiplication a pair
+    const double ratio = ch ? std::pow(axes->theta, -2.0 / ch) : 1.0;
+    double f = axes->step[a] / 6.283185307179586476925286766559;
+    for (int i = 0; i < ch / 2; ++i, f *= ratio) p.turns[pair++] = f;
+  }
+  if (n_tok < 0 || token_begin < 0 || n_tok > tokens - token_begin)
+    return fail("tokens [%d, %d + %d) not within the grid's %lld", token_begin, token_begin, n_tok, tokens);
+  if ((long long)n_tok * head_dim >= 1ll << 31) return fail("n_tok * head_dim must be below 2^31");
+  const size_t es = dtype == ORCH_BF16 ? 2 : 4;
+  for (int k = 0; k < n_tensors; ++k) {
+    const orch_rotary_tensor& t = tensors[k];
+    if (!t.x || !t.out) return fail("NULL pointer");
+    if (t.heads < 1 || (long long)t.heads * B > 32767) return fail("bad shape: heads must be >= 1, B * heads <= 32767");
+    if ((uintptr_t)t.x % es || (uintptr_t)t.out % es) return fail("tensors must be aligned to their elements");
+    const int extent[3] = {B, t.heads, n_tok};
+    for (int a = 0; a < 3; ++a)
+      if (n_tok > 0 && extent[a] > 1 && (t.x_stride[a] < (size_t)head_dim || t.out_stride[a] < (size_t)head_dim))
+        return fail("strides must be at least head_dim");
+    p.t[k].x = t.x; p.t[k].out = t.out; p.t[k].heads = t.heads;
+    for (int a = 0; a < 3; ++a) {
+      // (the stride of an extent of one is never used)
+      p.t[k].xs[a] = extent[a] > 1 ? t.x_stride[a] : 0;
+      p.t[k].os[a] = extent[a] > 1 ? t.out_stride[a] : 0;
+    }
+  }
+  p.n_t = n_tensors; p.B = B; p.n_tok = n_tok; p.d = head_dim; p.token_begin = token_begin;
+  p.rows = axes->extent[1]; p.cols = axes->extent[2]; p.interleaved = axes->interleaved != 0;
+  return launched(launch_rotary(p, dtype, (hipStream_t)hip_stream), "rotary launch");
+}
+
+int orch_op_kv_quantize(const void* kv, size_t kv_bs, int kv_tokens, int kv_off, const orch_quantized_kv* cache,
+                        int tok_off, int B, int heads, int n_tok, int head_dim, int dtype, void* hip_stream) {
+  KvCacheParams p{};
+  int rc = kv_params(&p, kv, kv_bs, kv_tokens, kv_off, cache, tok_off, B, heads, n_tok, head_dim, dtype);
+  if (rc) return rc;
+  return launched(launch_kv_quantize(p, dtype, (hipStream_t)hip_stream), "K/V quantise launch");
+}
+
+int orch_op_kv_dequantize(const orch_quantized_kv* cache, int tok_off, void* kv, size_t kv_bs, int kv_tokens,
+                          int kv_off, int B, int heads, int n_tok, int head_dim, int dtype, void* hip_stream) {
+  KvCacheParams p{};
+  int rc = kv_params(&p, kv, kv_bs, kv_tokens, kv_off, cache, tok_off, B, heads, n_tok, head_dim, dtype);
+  if (rc) return rc;
+  return launched(launch_kv_dequantize(p, dtype, (hipStream_t)hip_stream), "K/V read-back launch");
+}
+
+size_t orch_attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int head_dim, int dtype) {
+  if (B < 1 || heads < 1 || n_q < 0 || n_kv < 1 || head_dim < 1 || (dtype != ORCH_F32 && dtype != ORCH_BF16)) return 0;
+  return attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype);
+}
+
+int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache, const void* kv_fresh, size_t fresh_bs,
+                                int fresh_begin, int n_fresh, int B, int heads, int n_q, int head_dim, void* out,
+                                void* workspace, size_t workspace_bytes, int dtype, void* hip_stream) {
+  if (!q || !out || (n_fresh > 0 && !kv_fresh)) return fail("NULL pointer");
+  int rc = check_common(B, heads, head_dim, dtype);
+  if (rc) return rc;
+  size_t values, exps;
+  rc = check_cache(cache, B, heads, head_dim, &values, &exps);
+  if (rc) return rc;
+  if (n_q < 0 || n_fresh < 0 || fresh_begin < 0 || n_fresh > cache->tokens - fresh_begin)
+    return fail("bad shape: %d queries, fresh keys [%d, %d + %d) of %d", n_q, fresh_begin, fresh_begin, n_fresh, cache->tokens);
+  if ((long long)n_q * head_dim >= 1ll << 31) return fail("n_q * head_dim must be below 2^31");
+  const size_t es = dtype == ORCH_BF16 ? 2 : 4, H = (size_t)heads * head_dim;
+  const size_t fresh_elems = 2 * (size_t)n_fresh * H, q_bytes = (size_t)B * n_q * H * es;
+  if (n_fresh > 0 && B > 1 && fresh_bs < fresh_elems) return fail("branch stride too small");
+  if (!aligned16(q) || !aligned16(out) || (n_fresh > 0 && (!aligned16(kv_fresh) || (B > 1 && fresh_bs * es % 16))) ||
+      (workspace && !aligned16(workspace)))
+    return fail("device buffers must be 16-byte aligned");
+  const size_t fresh_bytes = n_fresh > 0 ? ((B > 1 ? (B - 1) * fresh_bs : 0) + fresh_elems) * es : 0;
+  const size_t need = attention_quantized_workspace_bytes(B, heads, n_q, cache->tokens, head_dim, dtype);
+  const bool split = workspace && need > 0 && workspace_bytes >= need;
+  const struct { const void* p; size_t n; } in[] = {{q, q_bytes}, {cache->values, values}, {cache->exponents, exps}, {kv_fresh, fresh_bytes}};
+  for (const auto& r : in)
+    if (overlap(out, q_bytes, r.p, r.n) || (split && overlap(workspace, need, r.p, r.n)))
+      return fail("out or workspace overlaps an input");
+  if (split && overlap(workspace, need, out, q_bytes)) return fail("out and workspace overlap");
+  AttnQParams p{};
+  p.q = q; p.out = out; p.kv_fresh = kv_fresh; p.fresh_bs = fresh_bs; p.fresh_begin = fresh_begin; p.n_fresh = n_fresh;
+  p.c.values = (unsigned char*)cache->values; p.c.exps = (unsigned char*)cache->exponents;
+  p.c.values_bs = cache->values_stride; p.c.exps_bs = cache->exponents_stride; p.c.tokens = cache->tokens;
+  p.B = B; p.heads = heads; p.n_q = n_q; p.d = head_dim;
+  p.ws = split ? workspace : nullptr;
+  p.ws_bytes = split ? workspace_bytes : 0;
+  return launched(launch_attention_quantized(p, dtype, (hipStream_t)hip_stream), "attention launch");
+}
+
+}  // extern "C"

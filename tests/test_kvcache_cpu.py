@@ -1,0 +1,180 @@
+"""CPU side of the rotary positions, the 8-bit K/V cache and the attention over
+it: the oracle's pins, and every call that the library refuses (checked before
+anything is launched, so no GPU is needed; the pointers are never read)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kvcache as ok
+
+F32, BF16 = 0, 1
+P = [0x10000000 * (i + 1) for i in range(8)]      # addresses far apart, 16-byte aligned
+
+
+# ---- the oracle ------------------------------------------------------------------
+
+def test_e4m3_table_is_torchs():
+    t = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy()
+    np.testing.assert_array_equal(t, ok.e4m3_table())
+
+
+def test_rounding_is_torchs():
+    x = np.concatenate([np.linspace(-448, 448, 20001), np.linspace(-0.04, 0.04, 4001),
+                        0.5 * (ok.e4m3_table()[:126] + ok.e4m3_table()[1:127])])
+    x = x.astype(np.float32)
+    want = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    np.testing.assert_array_equal(ok.to_e4m3(x.astype(np.float64)), want)
+
+
+def test_scale_is_the_smallest():
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((500, 8)) * 2.0 ** rng.integers(-140, 120, (500, 1))
+    x[0], x[1] = 0.0, [448, 0, 0, 0, 0, 0, 0, -1]
+    x[2] = np.nextafter(448, 500) * np.array([1, 0, 0, 0, 0, 0, 0, 0])
+    v, e = ok.quantize(x)
+    s, amax = 2.0 ** (e.astype(float) - 127), np.abs(x).max(-1)
+    assert e.min() >= 1 and e[0] == 1 and e[1] == 127 and e[2] == 128
+    assert (amax <= 448 * s).all() and ((amax > 224 * s) | (e == 1)).all()
+    # half a step: 2^-4 of a value, 2^-10 s below the smallest normal 2^-6 s
+    err = np.abs(ok.dequantize(v, e) - x)
+    assert (err <= np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10 * s[:, None])).all()
+
+
+def test_not_finite_is_nan_and_the_rest_keeps_its_scale():
+    v, e = ok.quantize(np.array([[1.0, np.inf, -np.inf, np.nan]]))
+    np.testing.assert_array_equal(ok.dequantize(v, e), [[1.0, np.nan, np.nan, np.nan]])
+
+
+@pytest.mark.parametrize("interleaved", [True, False])
+def test_rotation_depends_on_distance_alone(interleaved):
+    """Scores of rotated q and k depend on the tokens' offset on the grid only."""
+    rng = np.random.default_rng(1)
+    q, k = (np.broadcast_to(rng.standard_normal((1, 1, 1, 32)), (1, 1, 64, 32)) for _ in range(2))
+    rot = [ok.rotary(x, 0, (8, 10, 12), (4, 4, 4), (0.5, -3.0, 7.0), (1.0, 2.0, 0.5), 100.0, interleaved)[0, 0] for x in (q, k)]
+    s = rot[0] @ rot[1].T
+    tok = lambda f, r, c: (f * 4 + r) * 4 + c
+    assert s[tok(0, 0, 0), tok(1, 2, 3)] == pytest.approx(s[tok(2, 1, 0), tok(3, 3, 3)], rel=1e-12)
+    np.testing.assert_allclose((rot[0] ** 2).sum(-1), (q[0, 0] ** 2).sum(-1), rtol=1e-12)
+
+
+# ---- refusals --------------------------------------------------------------------
+
+def _refused(lib, rc, word):
+    assert rc == lib.ORCH_EINVAL
+    assert word in lib.last_error(), lib.last_error()
+
+
+def _rotary(lib, tensors=None, n_tensors=1, B=1, n_tok=4, begin=0, d=32, dtype=BF16, **axes):
+    ax = lib.rotary_axes(axes.get("channels", (0, 16, 16)), axes.get("extent", (1, 4, 4)), axes.get("theta", 1e4),
+                         axes.get("origin", (0, 0, 0)), axes.get("step", (1, 1, 1)))
+    if tensors is None:
+        tensors = [dict()]
+    ts = (lib.RotaryTensor * 2)()
+    for t, kw in zip(ts, tensors):
+        t.x, t.out, t.heads = kw.get("x", P[0]), kw.get("out", P[1]), kw.get("heads", 2)
+        t.x_stride[:] = kw.get("xs", (2 * n_tok * d, n_tok * d, d))
+        t.out_stride[:] = kw.get("os", (2 * n_tok * d, n_tok * d, d))
+    return lib.lib.orch_op_rotary(C.byref(ax), ts, n_tensors, B, n_tok, begin, d, dtype, None)
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(n_tensors=0), "n_tensors"), (dict(n_tensors=3), "n_tensors"), (dict(B=0), "B"), (dict(d=40), "head_dim"),
+    (dict(dtype=2), "dtype"), (dict(theta=0.0), "theta"), (dict(theta=float("nan")), "theta"),
+    (dict(channels=(0, 15, 16)), "channels"), (dict(channels=(2, 16, 16)), "channels"),
+    (dict(channels=(-2, 16, 16)), "channels"), (dict(extent=(1, 0, 4)), "extents"),
+    (dict(extent=(1 << 15, 1 << 15, 2)), "extents"), (dict(origin=(0, float("inf"), 0)), "origin"),
+    (dict(step=(0, 0, float("nan"))), "step"), (dict(n_tok=17), "grid"), (dict(begin=13), "grid"),
+    (dict(begin=-1), "grid"), (dict(n_tok=-1), "grid"), (dict(begin=2 ** 31 - 1), "grid"),
+    (dict(extent=(1 << 10, 1 << 10, 1 << 10), n_tok=1 << 27), "2^31"),
+    (dict(tensors=[dict(x=None)]), "NULL"), (dict(tensors=[dict(out=None)]), "NULL"),
+    (dict(tensors=[dict(heads=0)]), "heads"), (dict(tensors=[dict(heads=40000)]), "heads"),
+    (dict(tensors=[dict(x=P[0] + 1)]), "aligned"), (dict(tensors=[dict(xs=(0, 128, 31))]), "strides"),
+    (dict(tensors=[dict(os=(0, 16, 32))]), "strides"), (dict(B=2, tensors=[dict(os=(8, 128, 32))]), "strides"),
+    (dict(n_tensors=2, tensors=[dict(), dict(out=None)]), "NULL"),
+])
+def test_rotary_refuses(orch_lib, kw, word):
+    _refused(orch_lib, _rotary(orch_lib, **kw), word)
+
+
+def test_rotary_binding_refuses(orch_lib):
+    ax = orch_lib.rotary_axes((0, 16, 16), (1, 4, 4))
+    x = torch.zeros((1, 2, 4, 32))
+    for a, b in ((x, x[..., :16]), (x, x.bfloat16()), (x.half(), x.half()), (x.transpose(2, 3), x.transpose(2, 3)),
+                 ((x, x), (x,)), ((x, x[:, :, :2]), (x, x[:, :, :2]))):
+        with pytest.raises(orch_lib.OrchError):
+            orch_lib.rotary(ax, 0, a, b)
+
+
+def _cache(lib, values=P[2], exponents=P[3], tokens=64, heads=2, d=32, vs=None, es=None):
+    return lib.QuantizedKV(values, exponents, 2 * heads * tokens * d if vs is None else vs,
+                           2 * heads * tokens if es is None else es, tokens)
+
+
+COMMON = [
+    (dict(B=0), "B"), (dict(heads=0), "heads"), (dict(B=200, heads=200), "heads"), (dict(d=40), "head_dim"),
+    (dict(dtype=2), "dtype"), (dict(cache=dict(values=None)), "cache"), (dict(cache=dict(exponents=None)), "cache"),
+    (dict(cache=dict(tokens=0)), "tokens"), (dict(cache=dict(tokens=1 << 26)), "2^31"),
+    (dict(B=2, cache=dict(vs=16)), "stride"), (dict(B=2, cache=dict(es=16)), "stride"),
+    (dict(cache=dict(values=P[2] + 8)), "aligned"), (dict(B=2, cache=dict(vs=1 << 20 | 8)), "aligned"),
+    (dict(cache=dict(exponents=P[2] + 64)), "overlap"),
+]
+RANGES = [
+    (dict(kv=None), "NULL"), (dict(n=-1), "tokens"), (dict(kv_off=-1), "tokens"), (dict(off=-1), "tokens"),
+    (dict(n=41), "tokens"), (dict(n=40, off=25), "tokens"), (dict(kv_off=33), "tokens"),
+    (dict(kv_off=2 ** 31 - 1), "tokens"), (dict(kv_tokens=0, n=0), "tokens"), (dict(kv_tokens=1 << 26), "2^31"),
+    (dict(B=2, bs=16), "stride"), (dict(kv=P[0] + 2), "aligned"), (dict(B=2, bs=(1 << 20) + 4), "aligned"),
+    (dict(kv=P[2] - 64), "overlap"), (dict(kv=P[3] - 64), "overlap"),
+]
+
+
+def _move(lib, back, kv=P[0], bs=1 << 20, kv_tokens=40, kv_off=0, off=0, B=1, heads=2, n=8, d=32, dtype=BF16, cache=None):
+    c = _cache(lib, **(cache or {}))
+    if back:
+        return lib.lib.orch_op_kv_dequantize(C.byref(c), off, kv, bs, kv_tokens, kv_off, B, heads, n, d, dtype, None)
+    return lib.lib.orch_op_kv_quantize(kv, bs, kv_tokens, kv_off, C.byref(c), off, B, heads, n, d, dtype, None)
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("kw,word", COMMON + RANGES)
+def test_cache_refuses(orch_lib, back, kw, word):
+    _refused(orch_lib, _move(orch_lib, back, **kw), word)
+
+
+def _attend(lib, q=P[0], fresh=P[1], bs=1 << 20, fb=4, nf=8, B=1, heads=2, n_q=8, d=32, out=P[4], ws=None, wsb=0,
+            dtype=BF16, cache=None):
+    c = _cache(lib, **(cache or {}))
+    return lib.lib.orch_op_attention_quantized(q, C.byref(c), fresh, bs, fb, nf, B, heads, n_q, d, out, ws, wsb, dtype, None)
+
+
+@pytest.mark.parametrize("kw,word", COMMON + [
+    (dict(q=None), "NULL"), (dict(out=None), "NULL"), (dict(fresh=None), "NULL"), (dict(n_q=-1), "shape"),
+    (dict(nf=-1), "shape"), (dict(fb=-1), "shape"), (dict(fb=57), "shape"), (dict(fb=2 ** 31 - 1), "shape"),
+    (dict(B=2, bs=16), "stride"), (dict(q=P[0] + 2), "aligned"), (dict(out=P[4] + 4), "aligned"),
+    (dict(fresh=P[1] + 8), "aligned"), (dict(B=2, bs=(1 << 20) + 4), "aligned"), (dict(ws=P[5] + 8, wsb=64), "aligned"),
+    (dict(n_q=1 << 26), "2^31"), (dict(out=P[0]), "overlap"), (dict(out=P[2]), "overlap"), (dict(out=P[1]), "overlap"),
+])
+def test_attention_refuses(orch_lib, kw, word):
+    _refused(orch_lib, _attend(orch_lib, **kw), word)
+
+
+def test_null_cache_refused(orch_lib):
+    _refused(orch_lib, orch_lib.lib.orch_op_kv_quantize(P[0], 1 << 20, 40, 0, None, 0, 1, 2, 8, 32, BF16, None), "cache")
+    _refused(orch_lib, orch_lib.lib.orch_op_kv_dequantize(None, 0, P[0], 1 << 20, 40, 0, 1, 2, 8, 32, BF16, None), "cache")
+    _refused(orch_lib, orch_lib.lib.orch_op_attention_quantized(P[0], None, None, 0, 0, 0, 1, 2, 8, 32, P[1], None, 0, BF16, None), "cache")
+
+
+def test_binding_of_the_cache_refuses(orch_lib):
+    v, e = torch.zeros((1, 2, 3, 8, 32), dtype=torch.uint8), torch.zeros((1, 2, 3, 8), dtype=torch.uint8)
+    c = orch_lib.quantized_kv(v, e)
+    assert (c.values, c.exponents, c.tokens) == (v.data_ptr(), e.data_ptr(), 8)
+    for bad in ((v, e[..., :4]), (v.float(), e), (v, e.short()), (v[..., :16], e), (v[:, :1], e[:, :1])):
+        with pytest.raises(orch_lib.OrchError):
+            orch_lib.quantized_kv(*bad)
+
+
+@pytest.mark.parametrize("bad", [dict(B=0), dict(heads=0), dict(n_q=-1), dict(n_kv=0), dict(d=0), dict(d=40), dict(dtype=7)])
+def test_no_workspace_for_bad_shapes(orch_lib, bad):
+    a = dict(B=1, heads=2, n_q=1, n_kv=4096, d=64, dtype=BF16) | bad
+    assert orch_lib.attention_quantized_workspace_bytes(*a.values()) == 0
