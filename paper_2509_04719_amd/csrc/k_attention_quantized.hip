@@ -68,6 +68,8 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   using G = Geo<D, NW>;
   constexpr int NC = G::NC, NT = G::NT, SL = G::SL, CPT = G::CPT, TH = G::THREADS;
   constexpr bool M32 = G::M32;
+  // (the body uses device-only types; the host pass only needs the launch stub)
+#if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, h = lane >> 5;
   const int i16 = lane & 15, g16 = lane >> 4;
@@ -82,7 +84,7 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   const int unit = w / sp.ns, part = w - unit * sp.ns;
   const int pair = unit / n_qt, q0 = (unit - pair * n_qt) * 32 * NW + 32 * wave;
   const int b = pair / p.heads, head = pair - b * p.heads;
-  const int N = p.c.tokens, fb = p.fresh_begin, nf = p.n_fresh;
+  const int N = p.c.tokens, nf = p.n_fresh, fb = nf > 0 ? p.fresh_begin : 0;
   const int nkt = (N + BKV - 1) / BKV;
   const int t0 = (int)((long long)nkt * part / sp.ns), NIT = (int)((long long)nkt * (part + 1) / sp.ns) - t0;
   const size_t H = (size_t)p.heads * D;
@@ -96,98 +98,93 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
     vf = reinterpret_cast<const bf16*>(p.kv_fresh) + b * p.fresh_bs + nf * H + (size_t)head * D * nf;
   }
 
-  // K rows' padding channels [D, 16 NC) and V's: zero, never written again
+  // K rows' padding channels [D, 16 NC): zero, never written again (Q's are zero too; V's may
+  // hold anything, they end in rows of O^T that nobody reads)
   if constexpr (D % 16 != 0) {
-    for (int i = tid; i < 2 * BKV; i += TH) {
+    for (int i = tid; i < 2 * BKV; i += TH)
       *reinterpret_cast<u32x4*>(smem + (i / BKV) * G::KT + (i % BKV) * G::KP + 2 * D) = u32x4{0, 0, 0, 0};
-      *reinterpret_cast<u32x4*>(smem + 2 * G::KT + (i / BKV) * G::VT + (i % BKV) * G::VP + 2 * D) = u32x4{0, 0, 0, 0};
-    }
   }
 
   // Staging.  A tile of 64 tokens is contiguous in the cache: chunk id (8 channels) of key
   // id / CPT.  Key k of the tile goes to K row k, and to V row vrow(k): the transposing reads
   // below take keys 8 g + 4 x + r, r = 0 .. 3, of several g at once, which then lie in
-  // consecutive rows.
+  // consecutive rows.  A tile of fresh keys alone keeps V^T as it is, rows of 64 keys with
+  // their 16-byte chunks swizzled by row.
   auto vrow = [](int k) __attribute__((always_inline)) { return (k & 32) | (k & 4) << 2 | (k & 24) >> 1 | (k & 3); };
   constexpr int KS = TH / CPT;                              // EVEN: keys from slot to slot
   static_assert(!G::EVEN || (KS & (KS - 1)) == 0, "a slot's rows are a constant away");
-  int k_dst_[G::EVEN ? 1 : SL], v_dst_[G::EVEN ? 1 : SL], key_[G::EVEN ? 1 : SL];
+  const int vtid = (NW - 1 - wave) * 64 + lane;             // V's chunks from the last wave down
+  int k_dst_[G::EVEN ? 1 : SL], v_dst_[G::EVEN ? 1 : SL], kkey_[G::EVEN ? 1 : SL], vkey_[G::EVEN ? 1 : SL];
 #pragma unroll
   for (int i = 0; i < (G::EVEN ? 1 : SL); ++i) {
-    const int id = i * TH + tid, key = id / CPT, ch = id - key * CPT;
-    key_[i] = key;
-    k_dst_[i] = (key & 63) * G::KP + ch * 16;
-    v_dst_[i] = 2 * G::KT + vrow(key & 63) * G::VP + ch * 16;
+    const int idk = i * TH + tid, keyk = idk / CPT, idv = i * TH + vtid, keyv = idv / CPT;
+    kkey_[i] = keyk;
+    vkey_[i] = keyv;
+    k_dst_[i] = keyk * G::KP + (idk - keyk * CPT) * 16;
+    v_dst_[i] = 2 * G::KT + vrow(keyv) * G::VP + (idv - keyv * CPT) * 16;
   }
-  auto key_of = [&](int i) __attribute__((always_inline)) { return G::EVEN ? key_[0] + i * KS : key_[i]; };
+  auto key_of = [&](auto isk_c, int i) __attribute__((always_inline)) {
+    const int* k = decltype(isk_c)::value ? kkey_ : vkey_;
+    return G::EVEN ? k[0] + i * KS : k[i];
+  };
   auto k_dst = [&](int i) __attribute__((always_inline)) { return G::EVEN ? k_dst_[0] + i * KS * G::KP : k_dst_[i]; };
   auto v_dst = [&](int i) __attribute__((always_inline)) { return G::EVEN ? v_dst_[0] + vrow(i * KS) * G::VP : v_dst_[i]; };
-  const bool last_on = (SL - 1) * TH + tid < BKV * CPT;     // the last slot's chunk exists
-  auto on = [&](int i) __attribute__((always_inline)) { return (BKV * CPT) % TH == 0 || i + 1 < SL || last_on; };
+  // fresh V^T: slot i holds chunk vtid % 8 (8 keys) of channel vtid / 8 + i TH / 8
+  const int vt_src = (vtid >> 3) * nf + (vtid & 7) * 8;
+  const int vt_dst = 2 * G::KT + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
+  static_assert(TH % 128 == 0 || !G::FRESH, "the swizzle repeats from slot to slot");
+  // the last slot is some waves' alone: the first ones take K's chunks, the last ones V's
+  constexpr int LEFT = (BKV * CPT % TH) / 64;
+  static_assert(BKV * CPT % 64 == 0, "whole waves");
+  auto on = [&](auto isk_c, int i) __attribute__((always_inline)) {
+    return LEFT == 0 || i + 1 < SL || (decltype(isk_c)::value ? wave < LEFT : wave >= NW - LEFT);
+  };
 
   enum { kStale = 0, kFresh = 1, kMixed = 2 };
-  auto type_of = [&](int t) {
-    const int n0 = t * BKV;
-    if (n0 + BKV <= N && (n0 + BKV <= fb || n0 >= fb + nf)) return (int)kStale;
-    if (G::FRESH && n0 >= fb && n0 + BKV <= fb + nf) return (int)kFresh;
-    return (int)kMixed;
+  auto type_of = [&](int t) __attribute__((always_inline)) {
+    const int n0 = t * BKV, n1 = n0 + BKV;
+    if (n1 <= N && (n1 <= fb || n0 >= fb + nf)) return (int)kStale;
+    return G::FRESH && n0 >= fb && n1 <= fb + nf ? (int)kFresh : (int)kMixed;
   };
-  typedef unsigned raw __attribute__((ext_vector_type(G::FRESH ? 4 : 2)));
-  raw kraw[SL], vraw[SL];
-  unsigned kexp[SL], vexp[SL];
-  auto set = [](raw& r, const u32x4& x) __attribute__((always_inline)) {
-    if constexpr (G::FRESH) r = x;
+  struct Raw {
+    typedef unsigned vec __attribute__((ext_vector_type(G::FRESH ? 4 : 2)));
+    vec x[SL];
+    unsigned e[SL];
   };
-  auto get = [](const raw& r) __attribute__((always_inline)) {
-    if constexpr (G::FRESH) return r;
-    else return u32x4{r[0], r[1], 0, 0};
-  };
-  auto load_k = [&](int t) {
-    const int type = type_of(t);
+  // buffers of the cache's and the fresh K's head: one 32-bit offset a lane for every load
+  const __amdgpu_buffer_rsrc_t rk8 = buffer_rsrc(k8, (size_t)N * D), rv8 = buffer_rsrc(v8, (size_t)N * D);
+  const __amdgpu_buffer_rsrc_t rke = buffer_rsrc(ke, N), rve = buffer_rsrc(ve, N);
+  const __amdgpu_buffer_rsrc_t rkf = buffer_rsrc(nf > 0 ? (const void*)kf : k8, nf > 0 ? (size_t)nf * D * 2 : 0);
+  // (tiles of both kinds are read when they are stored)
+  auto load = [&](auto isk_c, Raw& r, int t, int type) __attribute__((always_inline)) {
+    constexpr bool isk = decltype(isk_c)::value;
     if (type == kStale) {
-      const unsigned char* src = k8 + (size_t)t * BKV * D;
-      const unsigned char* e = ke + t * BKV;
 #pragma unroll
       for (int i = 0; i < SL; ++i)
-        if (on(i)) {
-          const u32x2 x = *reinterpret_cast<const u32x2*>(src + (i * TH + tid) * 8);
-          kraw[i][0] = x[0];
-          kraw[i][1] = x[1];
-          kexp[i] = e[key_of(i)];
+        if (on(isk_c, i)) {
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(isk ? rk8 : rv8, (isk ? tid : vtid) * 8,
+                                                                                         t * BKV * D + i * TH * 8, 0));
+          r.x[i][0] = x[0];
+          r.x[i][1] = x[1];
+          r.e[i] = __builtin_amdgcn_raw_buffer_load_b8(isk ? rke : rve, key_of(isk_c, i), t * BKV, 0);
         }
-    } else if (G::FRESH && type == kFresh) {
-      const bf16* src = kf + (size_t)(t * BKV - fb) * D;
+    } else if constexpr (G::FRESH) {
+      if (type == kFresh) {
 #pragma unroll
-      for (int i = 0; i < SL; ++i)
-        if (on(i)) set(kraw[i], *reinterpret_cast<const u32x4*>(src + (i * TH + tid) * 8));
+        for (int i = 0; i < SL; ++i)
+          if (on(isk_c, i)) {
+            if constexpr (isk) {
+              r.x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkf, tid * 16, (unsigned)(t * BKV - fb) * (2u * D) + i * TH * 16, 0));
+            } else {
+              const char* base = reinterpret_cast<const char*>(vf + (t * BKV - fb) + (size_t)i * (TH / 8) * nf);
+              const u32x4_u x = *reinterpret_cast<const u32x4_u*>(base + (unsigned)(vt_src * 2));
+              r.x[i] = u32x4{x[0], x[1], x[2], x[3]};
+            }
+          }
+      }
     }
   };
-  auto load_v = [&](int t) {
-    const int type = type_of(t);
-    if (type == kStale) {
-      const unsigned char* src = v8 + (size_t)t * BKV * D;
-      const unsigned char* e = ve + t * BKV;
-#pragma unroll
-      for (int i = 0; i < SL; ++i)
-        if (on(i)) {
-          const u32x2 x = *reinterpret_cast<const u32x2*>(src + (i * TH + tid) * 8);
-          vraw[i][0] = x[0];
-          vraw[i][1] = x[1];
-          vexp[i] = e[key_of(i)];
-        }
-    } else if (G::FRESH && type == kFresh) {
-      // channel id / 8, keys 8 (id % 8) .. +8
-      const bf16* src = vf + (t * BKV - fb);
-#pragma unroll
-      for (int i = 0; i < SL; ++i)
-        if (on(i)) {
-          const int id = i * TH + tid;
-          const u32x4_u x = *reinterpret_cast<const u32x4_u*>(src + (size_t)(id >> 3) * nf + (id & 7) * 8);
-          set(vraw[i], u32x4{x[0], x[1], x[2], x[3]});
-        }
-    }
-  };
-  auto widen = [](unsigned x0, unsigned x1, unsigned e) {
+  auto widen = [](unsigned x0, unsigned x1, unsigned e) __attribute__((always_inline)) {
     const float s = scale_of(e);
     u32x4 r;
     r[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, s, false));
@@ -196,62 +193,48 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
     r[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, s, true));
     return r;
   };
-  // a chunk of a tile that the band's edge or the last key crosses
-  auto mixed = [&](int t, int i, bool isk) {
-    const int n = t * BKV + key_of(i), f = n - fb, ch = i * TH + tid - key_of(i) * CPT;
-    u32x4 r = {0, 0, 0, 0};
-    if ((unsigned)f < (unsigned)nf) {
-      if (isk) {
-        r = *reinterpret_cast<const u32x4*>(kf + (size_t)f * D + ch * 8);
-      } else {
-        const unsigned short* src = reinterpret_cast<const unsigned short*>(vf) + (size_t)ch * 8 * nf + f;
+  auto store = [&](auto isk_c, const Raw& r, int t, int type) __attribute__((always_inline)) {
+    constexpr bool isk = decltype(isk_c)::value;
+    char* dst = smem + (t & 1) * (isk ? G::KT : G::VT);
+    auto at = [&](int i) __attribute__((always_inline)) { return reinterpret_cast<u32x4*>(dst + (isk ? k_dst(i) : v_dst(i))); };
+    if (type == kStale) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = src[(size_t)2 * e * nf] | (unsigned)src[(size_t)(2 * e + 1) * nf] << 16;
-      }
-    } else if (n < N) {
-      const u32x2 x = *reinterpret_cast<const u32x2*>((isk ? k8 : v8) + (size_t)n * D + ch * 8);
-      r = widen(x[0], x[1], (isk ? ke : ve)[n]);
+      for (int i = 0; i < SL; ++i)
+        if (on(isk_c, i)) *at(i) = widen(r.x[i][0], r.x[i][1], r.e[i]);
+      return;
     }
-    return r;
-  };
-  auto store_k = [&](int t) {
-    const int type = type_of(t);
-    char* dst = smem + (t & 1) * G::KT;
+    if constexpr (G::FRESH) {
+      if (type == kFresh) {
 #pragma unroll
+        for (int i = 0; i < SL; ++i)
+          if (on(isk_c, i)) *(isk ? at(i) : reinterpret_cast<u32x4*>(dst + vt_dst + i * TH * 16)) = r.x[i];
+        return;
+      }
+    }
+    // a tile that the band's edge or the last key crosses
+#pragma unroll 1
     for (int i = 0; i < SL; ++i)
-      if (on(i)) {
-        u32x4 x;
-        if (type == kStale) x = widen(kraw[i][0], kraw[i][1], kexp[i]);
-        else if (G::FRESH && type == kFresh) x = get(kraw[i]);
-        else x = mixed(t, i, true);
-        *reinterpret_cast<u32x4*>(dst + k_dst(i)) = x;
+      if (i * TH + tid < BKV * CPT) {
+        const int id = i * TH + tid, key = id / CPT, ch = id - key * CPT;
+        const int n = t * BKV + key, f = n - fb;
+        u32x4 x = {0, 0, 0, 0};
+        if ((unsigned)f < (unsigned)nf) {
+          if (isk) {
+            x = *reinterpret_cast<const u32x4*>(kf + (size_t)f * D + ch * 8);
+          } else {
+            const unsigned short* src = reinterpret_cast<const unsigned short*>(vf) + (size_t)ch * 8 * nf + f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = src[(size_t)2 * e * nf] | (unsigned)src[(size_t)(2 * e + 1) * nf] << 16;
+          }
+        } else if (n < N) {
+          const u32x2 y = *reinterpret_cast<const u32x2*>((isk ? k8 : v8) + (size_t)n * D + ch * 8);
+          x = widen(y[0], y[1], (isk ? ke : ve)[n]);
+        }
+        *reinterpret_cast<u32x4*>(dst + (isk ? key * G::KP : 2 * G::KT + vrow(key) * G::VP) + ch * 16) = x;
       }
   };
-  auto store_v = [&](int t) {
-    const int type = type_of(t);
-    char* dst = smem + (t & 1) * G::VT;
-    if (G::FRESH && type == kFresh) {
-#pragma unroll
-      for (int i = 0; i < SL; ++i)
-        if (on(i)) {
-          const int id = i * TH + tid;
-          const u32x4 x = get(vraw[i]);
-          unsigned short* col = reinterpret_cast<unsigned short*>(dst + 2 * G::KT + vrow((id & 7) * 8) * G::VP) + (id >> 3);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            col[vrow(e) * (G::VP / 2)] = (unsigned short)(x[e >> 1] >> (16 * (e & 1)));
-        }
-    } else {
-#pragma unroll
-      for (int i = 0; i < SL; ++i)
-        if (on(i)) {
-          u32x4 x;
-          if (type == kStale) x = widen(vraw[i][0], vraw[i][1], vexp[i]);
-          else x = mixed(t, i, false);
-          *reinterpret_cast<u32x4*>(dst + v_dst(i)) = x;
-        }
-    }
-  };
+  constexpr std::true_type kK{};
+  constexpr std::false_type kV{};
 
   // this lane's query (B operand): channels 16 c + 8 h .. +8
   const int qrow = min(q0 + lc, p.n_q - 1);
@@ -275,7 +258,17 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   auto k_frag = [&](int t, int sub, int c) __attribute__((always_inline)) {
     return *reinterpret_cast<const bf16x8*>(smem + (t & 1) * G::KT + sub * 32 * G::KP + k_rd + 32 * c);
   };
-  // O^T tile tt; M32: keys 16 ci .. +16 of the half, else all its 32
+  // O^T tile tt; M32: keys 16 ci .. +16 of the half, else all its 32.  vt: the tile holds V^T rows
+  const int vt_row = M32 ? lc : i16;
+  const int vt_rd[2] = {2 * G::KT + vt_row * 128 + ((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) * 16,
+                        2 * G::KT + vt_row * 128 + (((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) ^ (M32 ? 2 : 4)) * 16};
+  auto vt_frag = [&](int t, int sub, int tt, int ci) __attribute__((always_inline)) {
+    // (the chunk's number 4 sub + 2 ci + h, or 4 sub + lane / 16, is swizzled by row; M32's 4 sub is an XOR of
+    // the address by 64)
+    const char* base = smem + (t & 1) * G::VT;
+    if constexpr (M32) return *reinterpret_cast<const bf16x8*>(base + (vt_rd[ci] ^ (64 * sub)) + tt * 4096);
+    else return *reinterpret_cast<const bf16x8*>(base + vt_rd[sub] + tt * 2048);
+  };
   auto v_frag = [&](int t, int sub, int tt, int ci) __attribute__((always_inline)) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     const char* a = smem + (t & 1) * G::VT + v_rd + (sub * 32 + (M32 ? 8 * ci : 0)) * G::VP + tt * (M32 ? 64 : 32);
@@ -362,13 +355,21 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   // One 32-key half: exponentials of its scores sc between the MFMAs of the next half's scores
   // (NEXT: tile nt, half nsub, into sn) and of the previous half's O^T += V^T P^T (pp; V
   // of tile pt, half psub).  Its probabilities go to pc.
-  auto step = [&](auto next_c, bool first, f32x16& sc, int nt, int nsub, f32x16& sn, int pt, int psub,
+  auto step = [&](auto next_c, bool first, f32x16& sc, int nt, int nsub, f32x16& sn, int pt, int psub, bool vt,
                   bf16x8(&pp)[2], bf16x8(&pc)[2]) __attribute__((always_inline)) {
     constexpr bool NEXT = decltype(next_c)::value;
     constexpr int VF = M32 ? 2 : 1;
     bf16x8 vp[VF][NT], kn[NEXT ? NC : 1];
+    auto v_frags = [&](int ci) __attribute__((always_inline)) {
+      if (G::FRESH && vt) {
 #pragma unroll
-    for (int tt = 0; tt < NT; ++tt) vp[0][tt] = v_frag(pt, psub, tt, 0);
+        for (int tt = 0; tt < NT; ++tt) vp[M32 ? ci : 0][tt] = vt_frag(pt, psub, tt, ci);
+      } else {
+#pragma unroll
+        for (int tt = 0; tt < NT; ++tt) vp[M32 ? ci : 0][tt] = v_frag(pt, psub, tt, ci);
+      }
+    };
+    v_frags(0);
     if constexpr (NEXT) {
 #pragma unroll
       for (int c = 0; c < NC / 2; ++c) kn[c] = k_frag(nt, nsub, c);
@@ -379,10 +380,7 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
 #pragma unroll
         for (int c = NC / 2; c < NC; ++c) kn[c] = k_frag(nt, nsub, c);
       }
-      if constexpr (M32) {
-#pragma unroll
-        for (int tt = 0; tt < NT; ++tt) vp[VF - 1][tt] = v_frag(pt, psub, tt, 1);
-      }
+      if constexpr (M32) v_frags(1);
     };
     bool gone = false;
     p_swap(pp);
@@ -395,12 +393,14 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
       const float alpha = up ? __builtin_amdgcn_exp2f(m_run - mn) : 1.0f;
       // the probabilities of the previous half, not yet in O, are of the old max: they go
       // in here, and nothing below (zeros on both sides: 0 V would be a NaN where V is infinite)
-      if (!first)
+      if (!first) {
+        if constexpr (M32) v_frags(1);
         static_for<0, NT>([&](auto tc) {
           constexpr int tt = decltype(tc)::value;
           pv(tc, std::integral_constant<int, 0>{}, vp[0][tt], pp[0]);
-          pv(tc, std::integral_constant<int, 1>{}, M32 ? v_frag(pt, psub, tt, 1) : vp[0][tt], pp[1]);
+          pv(tc, std::integral_constant<int, 1>{}, vp[VF - 1][tt], pp[1]);
         });
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         pp[0][e] = pp[1][e] = (bf16)0.0f;
@@ -505,16 +505,23 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   // K has two stages, V two: after the barrier between the halves of tile t, K of tile
   // t + 2 takes the place of tile t's and V of t + 1 that of t - 1's; their loads were
   // issued a whole tile earlier, into registers.
-  load_k(t0);
-  load_v(t0);
-  store_k(t0);
-  store_v(t0);
-  if (1 < NIT) {
-    load_k(t0 + 1);
-    load_v(t0 + 1);
-    store_k(t0 + 1);
+  // ty1 .. ty4: kinds of tiles t .. t + 3; vt0: tile t - 1 holds V^T
+  const int te = t0 + NIT;
+  int ty1 = type_of(t0), ty2 = type_of(t0 + 1), ty3 = type_of(t0 + 2);
+  Raw kr, vr;
+  {
+    Raw kr1;
+    load(kK, kr, t0, ty1);
+    load(kV, vr, t0, ty1);
+    if (1 < NIT) load(kK, kr1, t0 + 1, ty2);
+    store(kK, kr, t0, ty1);
+    if (2 < NIT) load(kK, kr, t0 + 2, ty3);
+    store(kV, vr, t0, ty1);
+    if (1 < NIT) {
+      load(kV, vr, t0 + 1, ty2);
+      store(kK, kr1, t0 + 1, ty2);
+    }
   }
-  if (2 < NIT) load_k(t0 + 2);
   lds_sync();
   f32x16 s0, s1;
   s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(t0, 0, 0), qf[0], zero16, 0, 0, 0);
@@ -525,26 +532,45 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int e = 0; e < 8; ++e) pa[j][e] = (bf16)0.0f;
+  bool vt0 = ty1 == kFresh;
   int t = t0;
-  for (; t + 1 < t0 + NIT; ++t) {
-    mask(t, 0, s0);
-    step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, pa, pb);
+  for (; t + 1 < te; ++t) {
+    const bool vt1 = ty1 == kFresh;
+    step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
     lds_sync();
-    if (t + 2 < t0 + NIT) store_k(t + 2);
-    store_v(t + 1);
-    if (t + 3 < t0 + NIT) load_k(t + 3);
-    if (t + 2 < t0 + NIT) load_v(t + 2);
-    mask(t, 1, s1);
-    step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, pb, pa);
+    const int ty4 = t + 3 < te ? type_of(t + 3) : (int)kMixed;
+    // tiles t + 1 .. t + 3 of one kind: nothing more is asked
+    if (ty2 == ty3 && ty3 == ty4 && ty4 != kMixed) {
+      auto all = [&](int type) __attribute__((always_inline)) {
+        store(kK, kr, t + 2, type);
+        load(kK, kr, t + 3, type);
+        store(kV, vr, t + 1, type);
+        load(kV, vr, t + 2, type);
+      };
+      if (ty4 == kStale) all(kStale);
+      else all(kFresh);
+    } else {
+      if (t + 2 < te) store(kK, kr, t + 2, ty3);
+      if (t + 3 < te) load(kK, kr, t + 3, ty4);
+      store(kV, vr, t + 1, ty2);
+      if (t + 2 < te) load(kV, vr, t + 2, ty3);
+    }
+    step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa);
+    vt0 = vt1;
+    ty1 = ty2;
+    ty2 = ty3;
+    ty3 = ty4;
   }
+  const bool vt1 = ty1 == kFresh;
   mask(t, 0, s0);
-  step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, pa, pb);
+  step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
   mask(t, 1, s1);
-  step(std::false_type{}, false, s1, 0, 0, s0, t, 0, pb, pa);
+  step(std::false_type{}, false, s1, 0, 0, s0, t, 0, vt1, pb, pa);
   p_swap(pa);
   static_for<0, NT>([&](auto tc) {
-    pv(tc, std::integral_constant<int, 0>{}, v_frag(t, 1, decltype(tc)::value, 0), pa[0]);
-    pv(tc, std::integral_constant<int, 1>{}, v_frag(t, 1, decltype(tc)::value, 1), pa[1]);
+    constexpr int tt = decltype(tc)::value;
+    pv(tc, std::integral_constant<int, 0>{}, vt1 ? vt_frag(t, 1, tt, 0) : v_frag(t, 1, tt, 0), pa[0]);
+    pv(tc, std::integral_constant<int, 1>{}, vt1 ? vt_frag(t, 1, tt, 1) : v_frag(t, 1, tt, 1), pa[1]);
   });
 
   // a lane holds channels 32 t + 8 g + 4 h .. +4 of query lane & 31 (M32), or 16 t + 4 (lane >> 4)
@@ -580,6 +606,7 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   }
   if (!whole && h == 0 && q0 + lc < p.n_q)
     sp.part_ml[((size_t)unit * sp.ns + part) * (32 * NW) + 32 * wave + lc] = make_float2(m_run, l_run);
+#endif
 }
 
 // ---------------------------------------------------------------------------
@@ -754,27 +781,69 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attn_q8_f32_kernel(A
 }
 
 // The parts of a query tile whose keys ns workgroups shared: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s
-// - m) l_s, m = max_s m_s.  A thread per 4 channels of a query, the parts in their order.
-template <typename T>
+// - m) l_s, m = max_s m_s.  A thread per 4 channels of a query and share of the parts (part s of
+// share s % SG, four in flight), the shares met in LDS in their order.
+template <typename T, int SG>
 __global__ __launch_bounds__(256) void attn_q8_merge_kernel(AttnQParams p, Split sp, int rows) {
-  const int quads = p.d / 4, n_qt = (p.n_q + rows - 1) / rows;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long query = i / quads;                 // (branch, head, query)
-  const int c = 4 * (int)(i - query * quads);
-  if (query >= (long long)p.B * p.heads * p.n_q) return;
-  const int pair = (int)(query / p.n_q), q = (int)(query - (long long)pair * p.n_q);
+  __shared__ float ml_s[256][2];
+  __shared__ f32x4 o_s[256];
+  const int quads = p.d / 4, per = quads * SG, qpb = 256 / per;
+  const int n_qt = (p.n_q + rows - 1) / rows;
+  const int qi = threadIdx.x / per, share = (threadIdx.x - qi * per) / quads, c = 4 * (threadIdx.x % quads);
+  const long long query = (long long)blockIdx.x * qpb + qi;          // (branch, head, query)
+  const bool on = qi < qpb && query < (long long)p.B * p.heads * p.n_q;
+  const int pair = on ? (int)(query / p.n_q) : 0, q = on ? (int)(query - (long long)pair * p.n_q) : 0;
   const size_t slot = ((size_t)pair * n_qt + q / rows) * sp.ns * rows + q % rows;
   const float2* ml = sp.part_ml + slot;
   const float* po = sp.part_o + slot * p.d + c;
-  float m = -INFINITY;
-  for (int s = 0; s < sp.ns; ++s) m = fmaxf(m, ml[(size_t)s * rows].x);
-  float l = 0.0f;
+  float m = -INFINITY, l = 0.0f;
   f32x4 o = {0, 0, 0, 0};
-  for (int s = 0; s < sp.ns; ++s) {
-    const float2 x = ml[(size_t)s * rows];
-    const float f = __builtin_amdgcn_exp2f(x.x - m);
-    const f32x4 y = *reinterpret_cast<const f32x4*>(po + (size_t)s * rows * p.d);
-    l = fmaf(f, x.y, l);
+  // weights relative to a max of minus infinity are 0, not the NaN of inf - inf
+  auto weight = [](float a, float b) { return a == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a - b); };
+  if (on)
+    for (int s0 = share; s0 < sp.ns; s0 += 4 * SG) {
+      float2 x[4];
+      f32x4 y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int s = min(s0 + k * SG, sp.ns - 1);
+        x[k] = ml[(size_t)s * rows];
+        y[k] = *reinterpret_cast<const f32x4*>(po + (size_t)s * rows * p.d);
+        if (s0 + k * SG >= sp.ns) x[k].x = -INFINITY;
+      }
+      const float mn = fmaxf(m, fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)));
+      const float f0 = weight(m, mn);
+      l *= f0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= f0;
+      m = mn;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (s0 + k * SG >= sp.ns) continue;
+        const float f = weight(x[k].x, mn);
+        l = fmaf(f, x[k].y, l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(f, y[k][e], o[e]);
+      }
+    }
+  ml_s[threadIdx.x][0] = m;
+  ml_s[threadIdx.x][1] = l;
+  o_s[threadIdx.x] = o;
+  __syncthreads();
+  if (!on || share > 0) return;
+  float mn = m;
+#pragma unroll
+  for (int k = 1; k < SG; ++k) mn = fmaxf(mn, ml_s[threadIdx.x + k * quads][0]);
+  const float f0 = weight(m, mn);
+  l *= f0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] *= f0;
+#pragma unroll
+  for (int k = 1; k < SG; ++k) {
+    const int i = threadIdx.x + k * quads;
+    const float f = weight(ml_s[i][0], mn);
+    const f32x4 y = o_s[i];
+    l = fmaf(f, ml_s[i][1], l);
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = fmaf(f, y[e], o[e]);
   }
@@ -785,6 +854,14 @@ __global__ __launch_bounds__(256) void attn_q8_merge_kernel(AttnQParams p, Split
   for (int e = 0; e < 4; ++e) v[e] = from_f<T>(o[e] * inv);
   const int b = pair / p.heads, head = pair - b * p.heads;
   *reinterpret_cast<quad*>(reinterpret_cast<T*>(p.out) + ((size_t)b * p.n_q + q) * p.heads * p.d + (size_t)head * p.d + c) = v;
+}
+
+template <typename T, int SG>
+hipError_t launch_merge(const AttnQParams& p, const Split& sp, int rows, hipStream_t s) {
+  const int qpb = 256 / (p.d / 4 * SG);
+  const size_t queries = (size_t)p.B * p.heads * p.n_q;
+  hipLaunchKernelGGL((attn_q8_merge_kernel<T, SG>), dim3((unsigned)((queries + qpb - 1) / qpb)), dim3(256), 0, s, p, sp, rows);
+  return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
@@ -896,11 +973,9 @@ hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream
     }
   });
   if (rc != hipSuccess || pl.ns == 1) return rc;
-  const size_t threads = (size_t)p.B * p.heads * p.n_q * (p.d / 4);
-  const dim3 grid((unsigned)((threads + 255) / 256));
-  if (dtype == kBF16) hipLaunchKernelGGL(attn_q8_merge_kernel<bf16>, grid, dim3(256), 0, s, p, sp, 32 * pl.nw);
-  else hipLaunchKernelGGL(attn_q8_merge_kernel<float>, grid, dim3(256), 0, s, p, sp, 32 * pl.nw);
-  return hipGetLastError();
+  const int rows = 32 * pl.nw;
+  if (dtype == kBF16) return pl.ns > 4 ? launch_merge<bf16, 8>(p, sp, rows, s) : launch_merge<bf16, 2>(p, sp, rows, s);
+  return pl.ns > 4 ? launch_merge<float, 8>(p, sp, rows, s) : launch_merge<float, 2>(p, sp, rows, s);
 }
 
 }  // namespace orch
