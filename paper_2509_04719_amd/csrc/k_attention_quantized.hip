@@ -23,7 +23,13 @@ typedef unsigned u32x4_u __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr int BKV = 64;
 
-__device__ __forceinline__ float scale_of(unsigned byte) { return __uint_as_float(byte << 23); }
+// 2^(byte - 127).  (As a shift in C the compiler keeps the bytes of the tile in flight as 16 bits, widens
+// them at the end of the loop that loads them, and waits for the loads there.)
+__device__ __forceinline__ float scale_of(unsigned byte) {
+  float r;
+  asm("v_lshlrev_b32 %0, 23, %1" : "=v"(r) : "v"(byte));
+  return r;
+}
 
 // key of row r of a 32-key half of S^T: bits 2 and 3 swapped, so that the eight scores a lane
 // holds of a 16-key chunk are consecutive keys
@@ -54,7 +60,8 @@ struct Geo {
   static constexpr int WPC = cmin(8 / NW, 160 * 1024 / LDS);       // workgroups of a CU
   static constexpr int WPE = (WPC * NW + 3) / 4;                   // waves of a SIMD
   static constexpr bool EVEN = THREADS % CPT == 0;                 // a thread's chunks are THREADS / CPT keys apart
-  static constexpr bool FRESH = NW == 4;         // fresh tiles are fetched ahead too
+  static constexpr bool FRESH = NW == 4;         // tiles of fresh keys alone have a path of their own,
+  static constexpr bool AHEAD = FRESH && D <= 96;   // and are fetched ahead (where registers allow)
 };
 
 struct Split {
@@ -146,43 +153,43 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
     if (n1 <= N && (n1 <= fb || n0 >= fb + nf)) return (int)kStale;
     return G::FRESH && n0 >= fb && n1 <= fb + nf ? (int)kFresh : (int)kMixed;
   };
+  // What a thread holds of a tile on its way: the cache's chunks and exponents, read of every tile
+  // (unused where the keys are fresh: a load under a branch costs register moves, and those a
+  // wait for the load), and the fresh keys' chunks of a tile of these alone.
   struct Raw {
-    typedef unsigned vec __attribute__((ext_vector_type(G::FRESH ? 4 : 2)));
-    vec x[SL];
+    u32x2 x[SL];
     unsigned e[SL];
+    u32x4 f[G::AHEAD ? SL : 1];
   };
-  // buffers of the cache's and the fresh K's head: one 32-bit offset a lane for every load
+  // buffers of the cache's and the fresh K's head: one 32-bit offset a lane for every load, zero past the last key
   const __amdgpu_buffer_rsrc_t rk8 = buffer_rsrc(k8, (size_t)N * D), rv8 = buffer_rsrc(v8, (size_t)N * D);
   const __amdgpu_buffer_rsrc_t rke = buffer_rsrc(ke, N), rve = buffer_rsrc(ve, N);
   const __amdgpu_buffer_rsrc_t rkf = buffer_rsrc(nf > 0 ? (const void*)kf : k8, nf > 0 ? (size_t)nf * D * 2 : 0);
-  // (tiles of both kinds are read when they are stored)
+  auto load_fresh = [&](auto isk_c, int t, int i) __attribute__((always_inline)) {
+    if constexpr (decltype(isk_c)::value) {
+      return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkf, tid * 16, (unsigned)(t * BKV - fb) * (2u * D) + i * TH * 16, 0));
+    } else {
+      // (rows of V^T start at any element)
+      const char* base = reinterpret_cast<const char*>(vf + (t * BKV - fb) + (size_t)i * (TH / 8) * nf);
+      const u32x4_u x = *reinterpret_cast<const u32x4_u*>(base + (unsigned)(vt_src * 2));
+      return u32x4{x[0], x[1], x[2], x[3]};
+    }
+  };
   auto load = [&](auto isk_c, Raw& r, int t, int type) __attribute__((always_inline)) {
     constexpr bool isk = decltype(isk_c)::value;
-    if (type == kStale) {
 #pragma unroll
-      for (int i = 0; i < SL; ++i)
-        if (on(isk_c, i)) {
-          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(isk ? rk8 : rv8, (isk ? tid : vtid) * 8,
-                                                                                         t * BKV * D + i * TH * 8, 0));
-          r.x[i][0] = x[0];
-          r.x[i][1] = x[1];
-          r.e[i] = __builtin_amdgcn_raw_buffer_load_b8(isk ? rke : rve, key_of(isk_c, i), t * BKV, 0);
-        }
-    } else if constexpr (G::FRESH) {
+    for (int i = 0; i < SL; ++i) {
+      // (a last slot that is not this wave's reads nothing)
+      const int off = on(isk_c, i) ? 0 : 0x7fffffff - BKV * D;
+      r.x[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(isk ? rk8 : rv8, (isk ? tid : vtid) * 8 + off, t * BKV * D + i * TH * 8, 0));
+      r.e[i] = __builtin_amdgcn_raw_buffer_load_b8(isk ? rke : rve, key_of(isk_c, i), t * BKV, 0);
+    }
+    if constexpr (G::AHEAD)
       if (type == kFresh) {
 #pragma unroll
         for (int i = 0; i < SL; ++i)
-          if (on(isk_c, i)) {
-            if constexpr (isk) {
-              r.x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkf, tid * 16, (unsigned)(t * BKV - fb) * (2u * D) + i * TH * 16, 0));
-            } else {
-              const char* base = reinterpret_cast<const char*>(vf + (t * BKV - fb) + (size_t)i * (TH / 8) * nf);
-              const u32x4_u x = *reinterpret_cast<const u32x4_u*>(base + (unsigned)(vt_src * 2));
-              r.x[i] = u32x4{x[0], x[1], x[2], x[3]};
-            }
-          }
+          if (on(isk_c, i)) r.f[i] = load_fresh(isk_c, t, i);
       }
-    }
   };
   auto widen = [](unsigned x0, unsigned x1, unsigned e) __attribute__((always_inline)) {
     const float s = scale_of(e);
@@ -203,21 +210,24 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
         if (on(isk_c, i)) *at(i) = widen(r.x[i][0], r.x[i][1], r.e[i]);
       return;
     }
-    if constexpr (G::FRESH) {
+    if constexpr (G::FRESH)
       if (type == kFresh) {
 #pragma unroll
         for (int i = 0; i < SL; ++i)
-          if (on(isk_c, i)) *(isk ? at(i) : reinterpret_cast<u32x4*>(dst + vt_dst + i * TH * 16)) = r.x[i];
+          if (on(isk_c, i)) {
+            u32x4 x;
+            if constexpr (G::AHEAD) x = r.f[i];
+            else x = load_fresh(isk_c, t, i);
+            *(isk ? at(i) : reinterpret_cast<u32x4*>(dst + vt_dst + i * TH * 16)) = x;
+          }
         return;
       }
-    }
-    // a tile that the band's edge or the last key crosses
-#pragma unroll 1
+    // a tile that the band's edge or the last key crosses (past it the loads gave zeros)
+#pragma unroll
     for (int i = 0; i < SL; ++i)
-      if (i * TH + tid < BKV * CPT) {
-        const int id = i * TH + tid, key = id / CPT, ch = id - key * CPT;
-        const int n = t * BKV + key, f = n - fb;
-        u32x4 x = {0, 0, 0, 0};
+      if (on(isk_c, i)) {
+        const int key = key_of(isk_c, i), ch = i * TH + (isk ? tid : vtid) - key * CPT, f = t * BKV + key - fb;
+        u32x4 x = widen(r.x[i][0], r.x[i][1], r.e[i]);
         if ((unsigned)f < (unsigned)nf) {
           if (isk) {
             x = *reinterpret_cast<const u32x4*>(kf + (size_t)f * D + ch * 8);
@@ -226,11 +236,8 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = src[(size_t)2 * e * nf] | (unsigned)src[(size_t)(2 * e + 1) * nf] << 16;
           }
-        } else if (n < N) {
-          const u32x2 y = *reinterpret_cast<const u32x2*>((isk ? k8 : v8) + (size_t)n * D + ch * 8);
-          x = widen(y[0], y[1], (isk ? ke : ve)[n]);
         }
-        *reinterpret_cast<u32x4*>(dst + (isk ? key * G::KP : 2 * G::KT + vrow(key) * G::VP) + ch * 16) = x;
+        *at(i) = x;
       }
   };
   constexpr std::true_type kK{};
@@ -507,20 +514,18 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   // issued a whole tile earlier, into registers.
   // ty1 .. ty4: kinds of tiles t .. t + 3; vt0: tile t - 1 holds V^T
   const int te = t0 + NIT;
-  int ty1 = type_of(t0), ty2 = type_of(t0 + 1), ty3 = type_of(t0 + 2);
+  int ty1 = type_of(t0), ty2 = type_of(min(t0 + 1, te - 1)), ty3 = type_of(min(t0 + 2, te - 1));
   Raw kr, vr;
   {
     Raw kr1;
     load(kK, kr, t0, ty1);
     load(kV, vr, t0, ty1);
-    if (1 < NIT) load(kK, kr1, t0 + 1, ty2);
+    load(kK, kr1, min(t0 + 1, te - 1), ty2);
     store(kK, kr, t0, ty1);
-    if (2 < NIT) load(kK, kr, t0 + 2, ty3);
+    load(kK, kr, min(t0 + 2, te - 1), ty3);
     store(kV, vr, t0, ty1);
-    if (1 < NIT) {
-      load(kV, vr, t0 + 1, ty2);
-      store(kK, kr1, t0 + 1, ty2);
-    }
+    load(kV, vr, min(t0 + 1, te - 1), ty2);
+    if (1 < NIT) store(kK, kr1, t0 + 1, ty2);
   }
   lds_sync();
   f32x16 s0, s1;
@@ -538,23 +543,11 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
     const bool vt1 = ty1 == kFresh;
     step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
     lds_sync();
-    const int ty4 = t + 3 < te ? type_of(t + 3) : (int)kMixed;
-    // tiles t + 1 .. t + 3 of one kind: nothing more is asked
-    if (ty2 == ty3 && ty3 == ty4 && ty4 != kMixed) {
-      auto all = [&](int type) __attribute__((always_inline)) {
-        store(kK, kr, t + 2, type);
-        load(kK, kr, t + 3, type);
-        store(kV, vr, t + 1, type);
-        load(kV, vr, t + 2, type);
-      };
-      if (ty4 == kStale) all(kStale);
-      else all(kFresh);
-    } else {
-      if (t + 2 < te) store(kK, kr, t + 2, ty3);
-      if (t + 3 < te) load(kK, kr, t + 3, ty4);
-      store(kV, vr, t + 1, ty2);
-      if (t + 2 < te) load(kV, vr, t + 2, ty3);
-    }
+    const int t2 = min(t + 2, te - 1), t3 = min(t + 3, te - 1), ty4 = type_of(t3);
+    if (t + 2 < te) store(kK, kr, t + 2, ty3);
+    load(kK, kr, t3, ty4);
+    store(kV, vr, t + 1, ty2);
+    load(kV, vr, t2, ty3);
     step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa);
     vt0 = vt1;
     ty1 = ty2;
