@@ -44,24 +44,31 @@ __device__ __forceinline__ void lds_sync() {
 }
 
 // ---------------------------------------------------------------------------
-// bf16
+// bf16.  A workgroup is four waves.  NW = 4: each has 32 queries, and they share every tile of
+// keys.  NW = 1: all have the same 32 queries, and each takes every key tile of a quarter of the
+// keys alone, without a barrier; their parts meet in LDS at the end.  (Few queries leave
+// most SIMDs without a wave otherwise, and a wave's own chain is what bounds it.)
 template <int D, int NW>
 struct Geo {
+  static constexpr int KG = 4 / NW;              // key groups
   static constexpr int NC = (D + 15) / 16;       // 16-channel chunks of a score
   static constexpr bool M32 = D % 32 == 0;       // PV on 32x32x16, else on 16x16x32
   static constexpr int NT = M32 ? D / 32 : NC;   // row tiles of O^T
   static constexpr int KP = NC * 32 + 16;        // bytes of a K row: an odd number of 16-byte chunks
   static constexpr int VP = M32 ? (D * 2 % 128 == 64 ? D * 2 : D * 2 + 64) : NC * 32;   // of a V row
   static constexpr int KT = BKV * KP, VT = BKV * VP;
-  static constexpr int LDS = 2 * (KT + VT);
-  static constexpr int THREADS = 64 * NW;
+  static constexpr int ST = NW == 4 ? 2 : 1;     // stages: a wave alone needs no second one
+  static constexpr int GROUP = ST * (KT + VT);
+  static constexpr int LDS = KG * GROUP;
+  static constexpr int THREADS = 64 * NW;        // that share a tile
   static constexpr int CPT = D / 8;              // 8-channel chunks of a token
   static constexpr int SL = (BKV * CPT + THREADS - 1) / THREADS;   // chunks of a thread, K and V each
-  static constexpr int WPC = cmin(8 / NW, 160 * 1024 / LDS);       // workgroups of a CU
-  static constexpr int WPE = (WPC * NW + 3) / 4;                   // waves of a SIMD
+  static constexpr int WPC = cmin(2, 160 * 1024 / LDS);            // workgroups of a CU, waves of a SIMD
   static constexpr bool EVEN = THREADS % CPT == 0;                 // a thread's chunks are THREADS / CPT keys apart
   static constexpr bool FRESH = NW == 4;         // tiles of fresh keys alone have a path of their own,
   static constexpr bool AHEAD = FRESH && D <= 96;   // and are fetched ahead (where registers allow)
+  static constexpr int NO = M32 ? NT : (2 * NT + 3) / 4;           // 16-register blocks of O^T
+  static_assert(KG == 1 || (NO * 16 + 2) * 256 <= GROUP, "a group's part fits its tile's place");
 };
 
 struct Split {
@@ -71,16 +78,19 @@ struct Split {
 };
 
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQParams p, Split sp) {
+__global__ __launch_bounds__(256, (Geo<D, NW>::WPC)) void attn_q8_kernel(AttnQParams p, Split sp) {
   using G = Geo<D, NW>;
-  constexpr int NC = G::NC, NT = G::NT, SL = G::SL, CPT = G::CPT, TH = G::THREADS;
+  constexpr int NC = G::NC, NT = G::NT, SL = G::SL, CPT = G::CPT, TH = G::THREADS, KG = G::KG;
   constexpr bool M32 = G::M32;
   // (the body uses device-only types; the host pass only needs the launch stub)
 #if defined(__HIP_DEVICE_COMPILE__)
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, h = lane >> 5;
+  extern __shared__ __attribute__((aligned(1024))) char smem_all[];
+  const int lane = threadIdx.x & 63, lc = lane & 31, h = lane >> 5;
   const int i16 = lane & 15, g16 = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = KG == 1 ? 0 : wave_all, wave = KG == 1 ? wave_all : 0;
+  const int tid = KG == 1 ? threadIdx.x : lane;          // of the threads that share a tile
+  char* smem = smem_all + kg * G::GROUP;
 
   // workgroups in the order (branch, head, query tile, split); an eighth of them in a row on
   // each XCD, so that those that read the same K/V share an L2
@@ -93,7 +103,8 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   const int b = pair / p.heads, head = pair - b * p.heads;
   const int N = p.c.tokens, nf = p.n_fresh, fb = nf > 0 ? p.fresh_begin : 0;
   const int nkt = (N + BKV - 1) / BKV;
-  const int t0 = (int)((long long)nkt * part / sp.ns), NIT = (int)((long long)nkt * (part + 1) / sp.ns) - t0;
+  const int shares = sp.ns * KG, share = part * KG + kg;
+  const int t0 = (int)((long long)nkt * share / shares), te = (int)((long long)nkt * (share + 1) / shares);
   const size_t H = (size_t)p.heads * D;
   const unsigned char* k8 = p.c.values + b * p.c.values_bs + (size_t)head * N * D;
   const unsigned char* v8 = p.c.values + b * p.c.values_bs + (size_t)(p.heads + head) * N * D;
@@ -108,7 +119,7 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   // K rows' padding channels [D, 16 NC): zero, never written again (Q's are zero too; V's may
   // hold anything, they end in rows of O^T that nobody reads)
   if constexpr (D % 16 != 0) {
-    for (int i = tid; i < 2 * BKV; i += TH)
+    for (int i = tid; i < G::ST * BKV; i += TH)
       *reinterpret_cast<u32x4*>(smem + (i / BKV) * G::KT + (i % BKV) * G::KP + 2 * D) = u32x4{0, 0, 0, 0};
   }
 
@@ -128,7 +139,7 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
     kkey_[i] = keyk;
     vkey_[i] = keyv;
     k_dst_[i] = keyk * G::KP + (idk - keyk * CPT) * 16;
-    v_dst_[i] = 2 * G::KT + vrow(keyv) * G::VP + (idv - keyv * CPT) * 16;
+    v_dst_[i] = G::ST * G::KT + vrow(keyv) * G::VP + (idv - keyv * CPT) * 16;
   }
   auto key_of = [&](auto isk_c, int i) __attribute__((always_inline)) {
     const int* k = decltype(isk_c)::value ? kkey_ : vkey_;
@@ -138,7 +149,7 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   auto v_dst = [&](int i) __attribute__((always_inline)) { return G::EVEN ? v_dst_[0] + vrow(i * KS) * G::VP : v_dst_[i]; };
   // fresh V^T: slot i holds chunk vtid % 8 (8 keys) of channel vtid / 8 + i TH / 8
   const int vt_src = (vtid >> 3) * nf + (vtid & 7) * 8;
-  const int vt_dst = 2 * G::KT + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
+  const int vt_dst = G::ST * G::KT + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
   static_assert(TH % 128 == 0 || !G::FRESH, "the swizzle repeats from slot to slot");
   // the last slot is some waves' alone: the first ones take K's chunks, the last ones V's
   constexpr int LEFT = (BKV * CPT % TH) / 64;
@@ -202,12 +213,15 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   };
   auto store = [&](auto isk_c, const Raw& r, int t, int type) __attribute__((always_inline)) {
     constexpr bool isk = decltype(isk_c)::value;
-    char* dst = smem + (t & 1) * (isk ? G::KT : G::VT);
+    char* dst = smem + (G::ST == 2 ? t & 1 : 0) * (isk ? G::KT : G::VT);
+    auto chunk = [&](int i) __attribute__((always_inline)) {
+      return widen(r.x[i][0], r.x[i][1], r.e[i]);
+    };
     auto at = [&](int i) __attribute__((always_inline)) { return reinterpret_cast<u32x4*>(dst + (isk ? k_dst(i) : v_dst(i))); };
     if (type == kStale) {
 #pragma unroll
       for (int i = 0; i < SL; ++i)
-        if (on(isk_c, i)) *at(i) = widen(r.x[i][0], r.x[i][1], r.e[i]);
+        if (on(isk_c, i)) *at(i) = chunk(i);
       return;
     }
     if constexpr (G::FRESH)
@@ -227,7 +241,7 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
     for (int i = 0; i < SL; ++i)
       if (on(isk_c, i)) {
         const int key = key_of(isk_c, i), ch = i * TH + (isk ? tid : vtid) - key * CPT, f = t * BKV + key - fb;
-        u32x4 x = widen(r.x[i][0], r.x[i][1], r.e[i]);
+        u32x4 x = chunk(i);
         if ((unsigned)f < (unsigned)nf) {
           if (isk) {
             x = *reinterpret_cast<const u32x4*>(kf + (size_t)f * D + ch * 8);
@@ -261,24 +275,24 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   // fragment reads: K row of key 32 sub + kperm(lc), chunk 2 c + h; V rows by the transposing
   // read (lane i of 16 points at four channels of row i / 4 and gets channel i of the four rows)
   const int k_rd = kperm(lc) * G::KP + 16 * h;
-  const int v_rd = 2 * G::KT + (M32 ? (4 * h + (i16 >> 2)) * G::VP + (g16 & 1) * 32 : (4 * g16 + (i16 >> 2)) * G::VP) + (i16 & 3) * 8;
+  const int v_rd = G::ST * G::KT + (M32 ? (4 * h + (i16 >> 2)) * G::VP + (g16 & 1) * 32 : (4 * g16 + (i16 >> 2)) * G::VP) + (i16 & 3) * 8;
   auto k_frag = [&](int t, int sub, int c) __attribute__((always_inline)) {
-    return *reinterpret_cast<const bf16x8*>(smem + (t & 1) * G::KT + sub * 32 * G::KP + k_rd + 32 * c);
+    return *reinterpret_cast<const bf16x8*>(smem + (G::ST == 2 ? t & 1 : 0) * G::KT + sub * 32 * G::KP + k_rd + 32 * c);
   };
   // O^T tile tt; M32: keys 16 ci .. +16 of the half, else all its 32.  vt: the tile holds V^T rows
   const int vt_row = M32 ? lc : i16;
-  const int vt_rd[2] = {2 * G::KT + vt_row * 128 + ((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) * 16,
-                        2 * G::KT + vt_row * 128 + (((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) ^ (M32 ? 2 : 4)) * 16};
+  const int vt_rd[2] = {G::ST * G::KT + vt_row * 128 + ((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) * 16,
+                        G::ST * G::KT + vt_row * 128 + (((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) ^ (M32 ? 2 : 4)) * 16};
   auto vt_frag = [&](int t, int sub, int tt, int ci) __attribute__((always_inline)) {
     // (the chunk's number 4 sub + 2 ci + h, or 4 sub + lane / 16, is swizzled by row; M32's 4 sub is an XOR of
     // the address by 64)
-    const char* base = smem + (t & 1) * G::VT;
+    const char* base = smem + (G::ST == 2 ? t & 1 : 0) * G::VT;
     if constexpr (M32) return *reinterpret_cast<const bf16x8*>(base + (vt_rd[ci] ^ (64 * sub)) + tt * 4096);
     else return *reinterpret_cast<const bf16x8*>(base + vt_rd[sub] + tt * 2048);
   };
   auto v_frag = [&](int t, int sub, int tt, int ci) __attribute__((always_inline)) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
-    const char* a = smem + (t & 1) * G::VT + v_rd + (sub * 32 + (M32 ? 8 * ci : 0)) * G::VP + tt * (M32 ? 64 : 32);
+    const char* a = smem + (G::ST == 2 ? t & 1 : 0) * G::VT + v_rd + (sub * 32 + (M32 ? 8 * ci : 0)) * G::VP + tt * (M32 ? 64 : 32);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ORCH_LDS s16x4*)(a));
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ORCH_LDS s16x4*)(a + 16 * G::VP));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -286,7 +300,7 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
 
   // O^T.  M32: tile t (channels 32 t ..) of the lane's query, 16 registers.  Else tile t (channels 16
   // t ..) of queries 16 j + (lane & 15): four registers at 4 (f % 4) of oo[f / 4], f = 2 t + j.
-  constexpr int NO = M32 ? NT : (2 * NT + 3) / 4;
+  constexpr int NO = G::NO;
   f32x16 oo[NO];
   const f32x16 zero16 = {};
 #pragma unroll
@@ -359,6 +373,10 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
   auto raised = [&](float mx) __attribute__((always_inline)) { return mx > m_run && !(mx < m_run + 1.0f); };
   auto needs_care = [&]() __attribute__((always_inline)) { return __any(!(fabsf(m_run) <= 2 * kHuge)); };
 
+  auto tiles_sync = [&]() __attribute__((always_inline)) {
+    if constexpr (KG == 1) lds_sync();
+    else asm volatile("" ::: "memory");    // one wave's LDS operations are in order
+  };
   // One 32-key half: exponentials of its scores sc between the MFMAs of the next half's scores
   // (NEXT: tile nt, half nsub, into sn) and of the previous half's O^T += V^T P^T (pp; V
   // of tile pt, half psub).  Its probabilities go to pc.
@@ -509,66 +527,111 @@ __global__ __launch_bounds__(64 * NW, (Geo<D, NW>::WPE)) void attn_q8_kernel(Att
     }
   };
 
-  // K has two stages, V two: after the barrier between the halves of tile t, K of tile
-  // t + 2 takes the place of tile t's and V of t + 1 that of t - 1's; their loads were
-  // issued a whole tile earlier, into registers.
+  // Between the halves of tile t (behind a barrier where waves share tiles) K of tile t + KA
+  // takes the place of tile t's, and V of t + VA that of t - 1's; their loads were issued a whole
+  // tile earlier, into registers.  Two stages: KA = 2, VA = 1; one: KA = 1, VA = 0.
+  constexpr int KA = G::ST, VA = G::ST - 1;
   // ty1 .. ty4: kinds of tiles t .. t + 3; vt0: tile t - 1 holds V^T
-  const int te = t0 + NIT;
-  int ty1 = type_of(t0), ty2 = type_of(min(t0 + 1, te - 1)), ty3 = type_of(min(t0 + 2, te - 1));
-  Raw kr, vr;
-  {
-    Raw kr1;
-    load(kK, kr, t0, ty1);
-    load(kV, vr, t0, ty1);
-    load(kK, kr1, min(t0 + 1, te - 1), ty2);
-    store(kK, kr, t0, ty1);
-    load(kK, kr, min(t0 + 2, te - 1), ty3);
-    store(kV, vr, t0, ty1);
-    load(kV, vr, min(t0 + 1, te - 1), ty2);
-    if (1 < NIT) store(kK, kr1, t0 + 1, ty2);
-  }
-  lds_sync();
-  f32x16 s0, s1;
-  s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(t0, 0, 0), qf[0], zero16, 0, 0, 0);
+  auto tile = [&](int t) __attribute__((always_inline)) { return min(t, te - 1); };
+  if (KG == 1 || t0 < te) {
+    int ty1 = type_of(t0), ty2 = type_of(tile(t0 + 1)), ty3 = type_of(tile(t0 + 2));
+    Raw kr, vr;
+    if constexpr (G::ST == 2) {
+      Raw kr1;
+      load(kK, kr, t0, ty1);
+      load(kV, vr, t0, ty1);
+      load(kK, kr1, tile(t0 + 1), ty2);
+      store(kK, kr, t0, ty1);
+      load(kK, kr, tile(t0 + 2), ty3);
+      store(kV, vr, t0, ty1);
+      load(kV, vr, tile(t0 + 1), ty2);
+      if (t0 + 1 < te) store(kK, kr1, t0 + 1, ty2);
+    } else {
+      load(kK, kr, t0, ty1);
+      load(kV, vr, t0, ty1);
+      store(kK, kr, t0, ty1);
+      load(kK, kr, tile(t0 + 1), ty2);
+    }
+    tiles_sync();
+    f32x16 s0, s1;
+    s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(t0, 0, 0), qf[0], zero16, 0, 0, 0);
 #pragma unroll
-  for (int c = 1; c < NC; ++c) s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(t0, 0, c), qf[c], s0, 0, 0, 0);
-  bf16x8 pa[2], pb[2];
+    for (int c = 1; c < NC; ++c) s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(t0, 0, c), qf[c], s0, 0, 0, 0);
+    bf16x8 pa[2], pb[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) pa[j][e] = (bf16)0.0f;
-  bool vt0 = ty1 == kFresh;
-  int t = t0;
-  for (; t + 1 < te; ++t) {
+      for (int e = 0; e < 8; ++e) pa[j][e] = (bf16)0.0f;
+    bool vt0 = ty1 == kFresh;
+    int t = t0;
+    for (; t + 1 < te; ++t) {
+      const bool vt1 = ty1 == kFresh;
+      step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
+      tiles_sync();
+      const int t3 = tile(t + 3), ty4 = type_of(t3);
+      if (t + KA < te) store(kK, kr, t + KA, G::ST == 2 ? ty3 : ty2);
+      load(kK, kr, G::ST == 2 ? t3 : tile(t + 2), G::ST == 2 ? ty4 : ty3);
+      store(kV, vr, t + VA, G::ST == 2 ? ty2 : ty1);
+      load(kV, vr, tile(t + VA + 1), G::ST == 2 ? ty3 : ty2);
+      step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa);
+      vt0 = vt1;
+      ty1 = ty2;
+      ty2 = ty3;
+      ty3 = ty4;
+    }
     const bool vt1 = ty1 == kFresh;
+    mask(t, 0, s0);
     step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
-    lds_sync();
-    const int t2 = min(t + 2, te - 1), t3 = min(t + 3, te - 1), ty4 = type_of(t3);
-    if (t + 2 < te) store(kK, kr, t + 2, ty3);
-    load(kK, kr, t3, ty4);
-    store(kV, vr, t + 1, ty2);
-    load(kV, vr, t2, ty3);
-    step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa);
-    vt0 = vt1;
-    ty1 = ty2;
-    ty2 = ty3;
-    ty3 = ty4;
+    if constexpr (G::ST == 1) store(kV, vr, t, ty1);
+    mask(t, 1, s1);
+    step(std::false_type{}, false, s1, 0, 0, s0, t, 0, vt1, pb, pa);
+    p_swap(pa);
+    static_for<0, NT>([&](auto tc) {
+      constexpr int tt = decltype(tc)::value;
+      pv(tc, std::integral_constant<int, 0>{}, vt1 ? vt_frag(t, 1, tt, 0) : v_frag(t, 1, tt, 0), pa[0]);
+      pv(tc, std::integral_constant<int, 1>{}, vt1 ? vt_frag(t, 1, tt, 1) : v_frag(t, 1, tt, 1), pa[1]);
+    });
   }
-  const bool vt1 = ty1 == kFresh;
-  mask(t, 0, s0);
-  step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
-  mask(t, 1, s1);
-  step(std::false_type{}, false, s1, 0, 0, s0, t, 0, vt1, pb, pa);
-  p_swap(pa);
-  static_for<0, NT>([&](auto tc) {
-    constexpr int tt = decltype(tc)::value;
-    pv(tc, std::integral_constant<int, 0>{}, vt1 ? vt_frag(t, 1, tt, 0) : v_frag(t, 1, tt, 0), pa[0]);
-    pv(tc, std::integral_constant<int, 1>{}, vt1 ? vt_frag(t, 1, tt, 1) : v_frag(t, 1, tt, 1), pa[1]);
-  });
+  l_run += __shfl_xor(l_run, 32, kWave);
+
+  // key groups: group 0 takes the others' parts, [register][lane] in their tiles' places, in their order
+  if constexpr (KG > 1) {
+    __syncthreads();
+    if (kg > 0) {
+      float* o = reinterpret_cast<float*>(smem) + lane;
+#pragma unroll
+      for (int k = 0; k < NO; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[(16 * k + r) * 64] = oo[k][r];
+      o[NO * 1024] = m_run;
+      o[NO * 1024 + 64] = l_run;
+    }
+    __syncthreads();
+    if (kg > 0) return;
+    // (relative to a max of minus infinity: 0, not the NaN of inf - inf)
+    auto weight = [](float a, float b) { return a == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a - b); };
+#pragma unroll 1
+    for (int g = 1; g < KG; ++g) {
+      const float* o = reinterpret_cast<const float*>(smem_all + g * G::GROUP) + lane;
+      const float m2 = o[NO * 1024], mn = fmaxf(m_run, m2), f1 = weight(m_run, mn), f2 = weight(m2, mn);
+      rescale(f1);
+      l_run = l_run * f1 + o[NO * 1024 + 64] * f2;
+      m_run = mn;
+      float fj[2] = {f2, f2};
+      if constexpr (!M32) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) fj[j] = __shfl(f2, 16 * j + i16, kWave);
+      }
+#pragma unroll
+      for (int k = 0; k < NO; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (M32 || 4 * k + r / 4 < 2 * NT) oo[k][r] = fmaf(o[(16 * k + r) * 64], fj[(r >> 2) & 1], oo[k][r]);
+    }
+  }
 
   // a lane holds channels 32 t + 8 g + 4 h .. +4 of query lane & 31 (M32), or 16 t + 4 (lane >> 4)
   // .. +4 of queries 16 j + (lane & 15)
-  l_run += __shfl_xor(l_run, 32, kWave);
   const bool whole = sp.ns == 1;
   auto put = [&](int ql, int c, float l, float x0, float x1, float x2, float x3) __attribute__((always_inline)) {
     const int q = q0 + ql;
@@ -858,32 +921,12 @@ hipError_t launch_merge(const AttnQParams& p, const Split& sp, int rows, hipStre
 }
 
 // ---------------------------------------------------------------------------
-// Waves of a workgroup by the number of queries, and workgroups that share a query tile's keys: the ns
-// that minimises the rounds of resident workgroups times a workgroup's key tiles (and two more for
-// its start), with the merge's cost where ns > 1.
+// The plan of a call: query groups of a workgroup (4, or 1 with the keys shared by its waves) and
+// workgroups that share a query tile's keys.
 struct Plan {
   int nw, ns;
   size_t tiles;
 };
-
-constexpr int few_waves(int d, bool f32) { return !f32 && d <= 80 ? 1 : 2; }
-
-template <typename G>
-Plan plan_geo(int nw, int bk, int B, int heads, int n_q, int n_kv) {
-  const long long tiles = (long long)ceil_div(n_q, 32 * nw) * heads * B, slots = 256 * G::WPC;
-  const int nkt = ceil_div(n_kv, bk);
-  int best = 1;
-  double cost = 1e300;
-  for (int ns = 1; ns <= nkt && ns <= 64; ++ns) {
-    const double rounds = (double)((tiles * ns + slots - 1) / slots);
-    const double c = rounds * (ceil_div(nkt, ns) + 2.0) + (ns > 1 ? 6.0 : 0.0);
-    if (c < cost) {
-      cost = c;
-      best = ns;
-    }
-  }
-  return {nw, best, (size_t)tiles};
-}
 
 template <typename F>
 void with_d(int d, F&& f) {
@@ -897,26 +940,38 @@ void with_d(int d, F&& f) {
   }
 }
 
-// f(dimension, waves) with both as constants
-template <typename F>
-void with_shape(int d, int n_q, int dtype, F&& f) {
-  with_d(d, [&](auto dc) {
-    constexpr int D = decltype(dc)::value;
-    if (n_q > 64) f(dc, std::integral_constant<int, 4>{});
-    else if (dtype == kBF16) f(dc, std::integral_constant<int, few_waves(D, false)>{});
-    else f(dc, std::integral_constant<int, few_waves(D, true)>{});
-  });
+// The ns that minimises the rounds of resident workgroups times a wave's key tiles (and two more
+// for its start), with the merge's launch where ns > 1.
+void best_split(long long tiles, int wpc, int groups, int nkt, int* ns, double* cost) {
+  const long long slots = 256 * wpc;
+  for (int n = 1; n * groups <= nkt + groups - 1 && n <= 64; ++n) {
+    const long long rounds = (tiles * n + slots - 1) / slots;
+    const double c = (double)rounds * (ceil_div(nkt, n * groups) + 2) + (n > 1 ? 3.0 : 0.0);
+    if (c < *cost) {
+      *cost = c;
+      *ns = n;
+    }
+  }
 }
 
 Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype) {
   Plan r{0, 1, 0};
-  with_shape(d, n_q, dtype, [&](auto dc, auto nc) {
-    constexpr int D = decltype(dc)::value, NW = decltype(nc)::value;
+  const long long pairs = (long long)B * heads;
+  with_d(d, [&](auto dc) {
+    constexpr int D = decltype(dc)::value;
+    double c4 = 1e300, c1 = 1e300;
+    int n4 = 1, n1 = 1;
     if (dtype == kBF16) {
-      if constexpr (NW == 4 || NW == few_waves(D, false)) r = plan_geo<Geo<D, NW>>(NW, BKV, B, heads, n_q, n_kv);
-    } else if constexpr (NW == 4 || NW == few_waves(D, true)) {
-      r = plan_geo<Geo32<D, NW>>(NW, Geo32<D, NW>::BK, B, heads, n_q, n_kv);
+      const int nkt = ceil_div(n_kv, BKV);
+      best_split(ceil_div(n_q, 128) * pairs, Geo<D, 4>::WPC, 1, nkt, &n4, &c4);
+      best_split(ceil_div(n_q, 32) * pairs, Geo<D, 1>::WPC, 4, nkt, &n1, &c1);
+    } else {
+      const int nkt = ceil_div(n_kv, Geo32<D, 4>::BK);
+      best_split(ceil_div(n_q, 128) * pairs, Geo32<D, 4>::WPC, 1, nkt, &n4, &c4);
+      if (n_q <= 64) best_split(ceil_div(n_q, 64) * pairs, Geo32<D, 2>::WPC, 1, nkt, &n1, &c1);
     }
+    if (c1 <= c4) r = {dtype == kBF16 ? 1 : 2, n1, (size_t)(ceil_div(n_q, dtype == kBF16 ? 32 : 64) * pairs)};
+    else r = {4, n4, (size_t)(ceil_div(n_q, 128) * pairs)};
   });
   return r;
 }
@@ -927,6 +982,14 @@ template <typename K>
 hipError_t launch(K kern, int lds, int threads, size_t groups, const AttnQParams& p, const Split& sp, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(threads), lds, s, p, sp);
   return hipGetLastError();
+}
+
+template <int D, int NW>
+hipError_t launch_bf16(const Plan& pl, const AttnQParams& p, const Split& sp, hipStream_t s) {
+  constexpr int lds = Geo<D, NW>::LDS;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_q8_kernel<D, NW>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  return attr != hipSuccess ? attr : launch(attn_q8_kernel<D, NW>, lds, 256, pl.tiles * pl.ns, p, sp, s);
 }
 
 }  // namespace q8attn
@@ -952,18 +1015,11 @@ hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream
     sp.part_ml = reinterpret_cast<float2*>(sp.part_o + part_floats(pl, p.d));
   }
   hipError_t rc = hipErrorInvalidValue;
-  with_shape(p.d, p.n_q, dtype, [&](auto dc, auto nc) {
-    constexpr int D = decltype(dc)::value, NW = decltype(nc)::value;
-    if (dtype == kBF16) {
-      if constexpr (NW == 4 || NW == few_waves(D, false)) {
-        constexpr int lds = Geo<D, NW>::LDS;
-        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_q8_kernel<D, NW>),
-                                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        rc = attr != hipSuccess ? attr : launch(attn_q8_kernel<D, NW>, lds, 64 * NW, pl.tiles * pl.ns, p, sp, s);
-      }
-    } else if constexpr (NW == 4 || NW == few_waves(D, true)) {
-      rc = launch(attn_q8_f32_kernel<D, NW>, Geo32<D, NW>::LDS, 64 * NW, pl.tiles * pl.ns, p, sp, s);
-    }
+  with_d(p.d, [&](auto dc) {
+    constexpr int D = decltype(dc)::value;
+    if (dtype == kBF16) rc = pl.nw == 4 ? launch_bf16<D, 4>(pl, p, sp, s) : launch_bf16<D, 1>(pl, p, sp, s);
+    else if (pl.nw == 4) rc = launch(attn_q8_f32_kernel<D, 4>, Geo32<D, 4>::LDS, 256, pl.tiles * pl.ns, p, sp, s);
+    else rc = launch(attn_q8_f32_kernel<D, 2>, Geo32<D, 2>::LDS, 128, pl.tiles * pl.ns, p, sp, s);
   });
   if (rc != hipSuccess || pl.ns == 1) return rc;
   const int rows = 32 * pl.nw;
