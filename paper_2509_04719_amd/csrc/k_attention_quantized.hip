@@ -64,7 +64,12 @@ struct Geo {
   static constexpr int CPT = D / 8;              // 8-channel chunks of a token
   static constexpr int SL = (BKV * CPT + THREADS - 1) / THREADS;   // chunks of a thread, K and V each
   static constexpr int WPC = cmin(2, 160 * 1024 / LDS);            // workgroups of a CU, waves of a SIMD
+  static constexpr int WPE = NW == 1 && D == 128 ? 1 : 2;          // waves of a SIMD that registers allow
   static constexpr bool EVEN = THREADS % CPT == 0;                 // a thread's chunks are THREADS / CPT keys apart
+  // NW = 1: lanes of a key, each with CPL chunks in a row, keys 64 / LPK apart
+  static constexpr int LPK = D == 128 ? 4 : D == 64 || D == 80 || D == 96 ? 2 : 1;
+  static constexpr int CPL = CPT / LPK;
+  static constexpr int NE = NW == 1 ? LPK : SL;  // scales of a thread
   static constexpr bool FRESH = NW == 4;         // tiles of fresh keys alone have a path of their own,
   static constexpr bool AHEAD = FRESH && D <= 96;   // and are fetched ahead (where registers allow)
   static constexpr int NO = M32 ? NT : (2 * NT + 3) / 4;           // 16-register blocks of O^T
@@ -78,7 +83,7 @@ struct Split {
 };
 
 template <int D, int NW>
-__global__ __launch_bounds__(256, (Geo<D, NW>::WPC)) void attn_q8_kernel(AttnQParams p, Split sp) {
+__global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQParams p, Split sp) {
   using G = Geo<D, NW>;
   constexpr int NC = G::NC, NT = G::NT, SL = G::SL, CPT = G::CPT, TH = G::THREADS, KG = G::KG;
   constexpr bool M32 = G::M32;
@@ -130,12 +135,17 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPC)) void attn_q8_kernel(AttnQPa
   // their 16-byte chunks swizzled by row.
   auto vrow = [](int k) __attribute__((always_inline)) { return (k & 32) | (k & 4) << 2 | (k & 24) >> 1 | (k & 3); };
   constexpr int KS = TH / CPT;                              // EVEN: keys from slot to slot
-  static_assert(!G::EVEN || (KS & (KS - 1)) == 0, "a slot's rows are a constant away");
+  static_assert(NW == 1 || !G::EVEN || (KS & (KS - 1)) == 0, "a slot's rows are a constant away");
+  // A wave alone has LPK lanes for each key, with CPL neighbouring chunks: few scales a lane, rows a
+  // constant apart, at the price of loads that touch more lines of the tile than they take from them.
+  constexpr bool ROW = NW == 1;
+  constexpr int LPK = G::LPK, CPL = G::CPL, KR = 64 / LPK;  // ROW: keys between a lane's rows
   const int vtid = (NW - 1 - wave) * 64 + lane;             // V's chunks from the last wave down
-  int k_dst_[G::EVEN ? 1 : SL], v_dst_[G::EVEN ? 1 : SL], kkey_[G::EVEN ? 1 : SL], vkey_[G::EVEN ? 1 : SL];
+  constexpr int NA = ROW || G::EVEN ? 1 : SL;
+  int k_dst_[NA], v_dst_[NA], kkey_[NA], vkey_[NA];
 #pragma unroll
-  for (int i = 0; i < (G::EVEN ? 1 : SL); ++i) {
-    const int idk = i * TH + tid, keyk = idk / CPT, idv = i * TH + vtid, keyv = idv / CPT;
+  for (int i = 0; i < NA; ++i) {
+    const int idk = ROW ? lane * CPL : i * TH + tid, keyk = idk / CPT, idv = ROW ? idk : i * TH + vtid, keyv = idv / CPT;
     kkey_[i] = keyk;
     vkey_[i] = keyv;
     k_dst_[i] = keyk * G::KP + (idk - keyk * CPT) * 16;
@@ -143,10 +153,13 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPC)) void attn_q8_kernel(AttnQPa
   }
   auto key_of = [&](auto isk_c, int i) __attribute__((always_inline)) {
     const int* k = decltype(isk_c)::value ? kkey_ : vkey_;
-    return G::EVEN ? k[0] + i * KS : k[i];
+    return ROW ? k[0] + i / CPL * KR : G::EVEN ? k[0] + i * KS : k[i];
   };
-  auto k_dst = [&](int i) __attribute__((always_inline)) { return G::EVEN ? k_dst_[0] + i * KS * G::KP : k_dst_[i]; };
-  auto v_dst = [&](int i) __attribute__((always_inline)) { return G::EVEN ? v_dst_[0] + vrow(i * KS) * G::VP : v_dst_[i]; };
+  auto chunk_of = [&](auto isk_c, int i) __attribute__((always_inline)) {
+    return ROW ? lane % LPK * CPL + i % CPL : i * TH + (decltype(isk_c)::value ? tid : vtid) - key_of(isk_c, i) * CPT;
+  };
+  auto k_dst = [&](int i) __attribute__((always_inline)) { return ROW ? k_dst_[0] + i / CPL * KR * G::KP + i % CPL * 16 : G::EVEN ? k_dst_[0] + i * KS * G::KP : k_dst_[i]; };
+  auto v_dst = [&](int i) __attribute__((always_inline)) { return ROW ? v_dst_[0] + vrow(i / CPL * KR) * G::VP + i % CPL * 16 : G::EVEN ? v_dst_[0] + vrow(i * KS) * G::VP : v_dst_[i]; };
   // fresh V^T: slot i holds chunk vtid % 8 (8 keys) of channel vtid / 8 + i TH / 8
   const int vt_src = (vtid >> 3) * nf + (vtid & 7) * 8;
   const int vt_dst = G::ST * G::KT + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
@@ -169,7 +182,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPC)) void attn_q8_kernel(AttnQPa
   // wait for the load), and the fresh keys' chunks of a tile of these alone.
   struct Raw {
     u32x2 x[SL];
-    unsigned e[SL];
+    unsigned e[G::NE];
     u32x4 f[G::AHEAD ? SL : 1];
   };
   // buffers of the cache's and the fresh K's head: one 32-bit offset a lane for every load, zero past the last key
@@ -188,12 +201,32 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPC)) void attn_q8_kernel(AttnQPa
   };
   auto load = [&](auto isk_c, Raw& r, int t, int type) __attribute__((always_inline)) {
     constexpr bool isk = decltype(isk_c)::value;
+    const __amdgpu_buffer_rsrc_t rx = isk ? rk8 : rv8, re = isk ? rke : rve;
+    if constexpr (ROW) {
 #pragma unroll
-    for (int i = 0; i < SL; ++i) {
-      // (a last slot that is not this wave's reads nothing)
-      const int off = on(isk_c, i) ? 0 : 0x7fffffff - BKV * D;
-      r.x[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(isk ? rk8 : rv8, (isk ? tid : vtid) * 8 + off, t * BKV * D + i * TH * 8, 0));
-      r.e[i] = __builtin_amdgcn_raw_buffer_load_b8(isk ? rke : rve, key_of(isk_c, i), t * BKV, 0);
+      for (int j = 0; j < LPK; ++j) {
+        const int so = t * BKV * D + j * KR * D;
+#pragma unroll
+        for (int c = 0; c < CPL; c += 2) {
+          const int i = j * CPL + c;
+          if (c + 1 < CPL) {
+            const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, (lane * CPL + c) * 8, so, 0));
+            r.x[i] = u32x2{x[0], x[1]};
+            r.x[cmin(i + 1, SL - 1)] = u32x2{x[2], x[3]};
+          } else {
+            r.x[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, (lane * CPL + c) * 8, so, 0));
+          }
+        }
+        r.e[j] = __builtin_amdgcn_raw_buffer_load_b8(re, lane / LPK, t * BKV + j * KR, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < SL; ++i) {
+        // (a last slot that is not this wave's reads nothing)
+        const int off = on(isk_c, i) ? 0 : 0x7fffffff - BKV * D;
+        r.x[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, (isk ? tid : vtid) * 8 + off, t * BKV * D + i * TH * 8, 0));
+        r.e[i] = __builtin_amdgcn_raw_buffer_load_b8(re, key_of(isk_c, i), t * BKV, 0);
+      }
     }
     if constexpr (G::AHEAD)
       if (type == kFresh) {
@@ -215,7 +248,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPC)) void attn_q8_kernel(AttnQPa
     constexpr bool isk = decltype(isk_c)::value;
     char* dst = smem + (G::ST == 2 ? t & 1 : 0) * (isk ? G::KT : G::VT);
     auto chunk = [&](int i) __attribute__((always_inline)) {
-      return widen(r.x[i][0], r.x[i][1], r.e[i]);
+      return widen(r.x[i][0], r.x[i][1], r.e[ROW ? i / CPL : i]);
     };
     auto at = [&](int i) __attribute__((always_inline)) { return reinterpret_cast<u32x4*>(dst + (isk ? k_dst(i) : v_dst(i))); };
     if (type == kStale) {
@@ -240,7 +273,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPC)) void attn_q8_kernel(AttnQPa
 #pragma unroll
     for (int i = 0; i < SL; ++i)
       if (on(isk_c, i)) {
-        const int key = key_of(isk_c, i), ch = i * TH + (isk ? tid : vtid) - key * CPT, f = t * BKV + key - fb;
+        const int ch = chunk_of(isk_c, i), f = t * BKV + key_of(isk_c, i) - fb;
         u32x4 x = chunk(i);
         if ((unsigned)f < (unsigned)nf) {
           if (isk) {
