@@ -48,20 +48,25 @@ __device__ __forceinline__ void lds_sync() {
 // keys.  NW = 1: all have the same 32 queries, and each takes every key tile of a quarter of the
 // keys alone, without a barrier; their parts meet in LDS at the end.  (Few queries leave
 // most SIMDs without a wave otherwise, and a wave's own chain is what bounds it.)
-template <int D, int NW>
+template <int D, int NW, bool PREP = false>
 struct Geo {
   static constexpr int KG = 4 / NW;              // key groups
   static constexpr int NC = (D + 15) / 16;       // 16-channel chunks of a score
   static constexpr bool M32 = D % 32 == 0;       // PV on 32x32x16, else on 16x16x32
   static constexpr int NT = M32 ? D / 32 : NC;   // row tiles of O^T
-  static constexpr int KP = NC * 32 + 16;        // bytes of a K row: an odd number of 16-byte chunks
+  static constexpr int CPT = D / 8;              // 8-channel chunks of a token
+  // bytes of a K row, an odd number of 16-byte chunks (prepared tiles hold no padding channels)
+  static constexpr int KP = PREP ? (CPT | 1) * 16 : NC * 32 + 16;
   static constexpr int VP = M32 ? (D * 2 % 128 == 64 ? D * 2 : D * 2 + 64) : NC * 32;   // of a V row
-  static constexpr int KT = BKV * KP, VT = BKV * VP;
+  // PREP: tiles as they lie in memory, KT bytes of K rows, then VT of V^T rows
+  static constexpr int KT = BKV * KP, VT = PREP ? (M32 ? D : 16 * NT) * 128 : BKV * VP;
+  static constexpr int ZERO = PREP && D % 16 ? 1024 : 0;           // zeros behind a K stage: channels past the last
+  static constexpr bool ONES = PREP && !M32 && 16 * NT > D;        // row D of V^T is ones: O^T's row D is the sum
   static constexpr int ST = NW == 4 ? 2 : 1;     // stages: a wave alone needs no second one
-  static constexpr int GROUP = ST * (KT + VT);
+  static constexpr int KS = KT + ZERO;           // a K stage
+  static constexpr int GROUP = ST * (KS + VT);
   static constexpr int LDS = KG * GROUP;
   static constexpr int THREADS = 64 * NW;        // that share a tile
-  static constexpr int CPT = D / 8;              // 8-channel chunks of a token
   static constexpr int SL = (BKV * CPT + THREADS - 1) / THREADS;   // chunks of a thread, K and V each
   static constexpr int WPC = cmin(2, 160 * 1024 / LDS);            // workgroups of a CU, waves of a SIMD
   static constexpr int WPE = NW == 1 && D == 128 ? 1 : 2;          // waves of a SIMD that registers allow
@@ -70,21 +75,22 @@ struct Geo {
   static constexpr int LPK = D == 128 ? 4 : D == 64 || D == 80 || D == 96 ? 2 : 1;
   static constexpr int CPL = CPT / LPK;
   static constexpr int NE = NW == 1 ? LPK : SL;  // scales of a thread
-  static constexpr bool FRESH = NW == 4;         // tiles of fresh keys alone have a path of their own,
+  static constexpr bool FRESH = NW == 4 && !PREP;         // tiles of fresh keys alone have a path of their own,
   static constexpr bool AHEAD = FRESH && D <= 96;   // and are fetched ahead (where registers allow)
   static constexpr int NO = M32 ? NT : (2 * NT + 3) / 4;           // 16-register blocks of O^T
   static_assert(KG == 1 || (NO * 16 + 2) * 256 <= GROUP, "a group's part fits its tile's place");
 };
 
 struct Split {
+  const char* tiles; // prepared tiles, [branch, head][key tile] of KT + VT bytes
   int ns;            // workgroups that share a query tile's keys
   float* part_o;     // fp32 [tiles * ns][32 NW][D], unnormalised
   float2* part_ml;   // (max, sum)
 };
 
-template <int D, int NW>
-__global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQParams p, Split sp) {
-  using G = Geo<D, NW>;
+template <int D, int NW, bool PREP>
+__global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(AttnQParams p, Split sp) {
+  using G = Geo<D, NW, PREP>;
   constexpr int NC = G::NC, NT = G::NT, SL = G::SL, CPT = G::CPT, TH = G::THREADS, KG = G::KG;
   constexpr bool M32 = G::M32;
   // (the body uses device-only types; the host pass only needs the launch stub)
@@ -123,9 +129,11 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
 
   // K rows' padding channels [D, 16 NC): zero, never written again (Q's are zero too; V's may
   // hold anything, they end in rows of O^T that nobody reads)
-  if constexpr (D % 16 != 0) {
+  if constexpr (PREP && D % 16 != 0) {
+    if (tid < 2) *reinterpret_cast<u32x4*>(smem + tid * G::KS + G::KT) = u32x4{0, 0, 0, 0};
+  } else if constexpr (D % 16 != 0) {
     for (int i = tid; i < G::ST * BKV; i += TH)
-      *reinterpret_cast<u32x4*>(smem + (i / BKV) * G::KT + (i % BKV) * G::KP + 2 * D) = u32x4{0, 0, 0, 0};
+      *reinterpret_cast<u32x4*>(smem + (i / BKV) * G::KS + (i % BKV) * G::KP + 2 * D) = u32x4{0, 0, 0, 0};
   }
 
   // Staging.  A tile of 64 tokens is contiguous in the cache: chunk id (8 channels) of key
@@ -149,7 +157,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
     kkey_[i] = keyk;
     vkey_[i] = keyv;
     k_dst_[i] = keyk * G::KP + (idk - keyk * CPT) * 16;
-    v_dst_[i] = G::ST * G::KT + vrow(keyv) * G::VP + (idv - keyv * CPT) * 16;
+    v_dst_[i] = G::ST * G::KS + vrow(keyv) * G::VP + (idv - keyv * CPT) * 16;
   }
   auto key_of = [&](auto isk_c, int i) __attribute__((always_inline)) {
     const int* k = decltype(isk_c)::value ? kkey_ : vkey_;
@@ -162,7 +170,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
   auto v_dst = [&](int i) __attribute__((always_inline)) { return ROW ? v_dst_[0] + vrow(i / CPL * KR) * G::VP + i % CPL * 16 : G::EVEN ? v_dst_[0] + vrow(i * KS) * G::VP : v_dst_[i]; };
   // fresh V^T: slot i holds chunk vtid % 8 (8 keys) of channel vtid / 8 + i TH / 8
   const int vt_src = (vtid >> 3) * nf + (vtid & 7) * 8;
-  const int vt_dst = G::ST * G::KT + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
+  const int vt_dst = G::ST * G::KS + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
   static_assert(TH % 128 == 0 || !G::FRESH, "the swizzle repeats from slot to slot");
   // the last slot is some waves' alone: the first ones take K's chunks, the last ones V's
   constexpr int LEFT = (BKV * CPT % TH) / 64;
@@ -246,7 +254,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
   };
   auto store = [&](auto isk_c, const Raw& r, int t, int type) __attribute__((always_inline)) {
     constexpr bool isk = decltype(isk_c)::value;
-    char* dst = smem + (G::ST == 2 ? t & 1 : 0) * (isk ? G::KT : G::VT);
+    char* dst = smem + (G::ST == 2 ? t & 1 : 0) * (isk ? G::KS : G::VT);
     auto chunk = [&](int i) __attribute__((always_inline)) {
       return widen(r.x[i][0], r.x[i][1], r.e[ROW ? i / CPL : i]);
     };
@@ -289,6 +297,28 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
   };
   constexpr std::true_type kK{};
   constexpr std::false_type kV{};
+  // prepared tiles: straight to LDS, 1 KB a wave and load, K's from the first wave on, V's from the last
+  const __amdgpu_buffer_rsrc_t rt = buffer_rsrc(PREP ? (const void*)(sp.tiles + (size_t)pair * nkt * (G::KT + G::VT)) : k8,
+                                                PREP ? (size_t)nkt * (G::KT + G::VT) : 0);
+  auto issue = [&](auto isk_c, int t) __attribute__((always_inline)) {
+    constexpr bool isk = decltype(isk_c)::value;
+    constexpr int NL = (isk ? G::KT : G::VT) / 1024;
+    char* dst = smem + (isk ? (t & 1) * G::KS : 2 * G::KS + (t & 1) * G::VT);
+    const int so = t * (G::KT + G::VT) + (isk ? 0 : G::KT);
+#pragma unroll
+    for (int i = 0; i < (NL + 3) / 4; ++i) {
+      const int j = 4 * i + (isk ? wave : 3 - wave);
+      if (NL % 4 == 0 || i + 1 < (NL + 3) / 4 || j < NL)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rt, (ORCH_LDS void*)(dst + j * 1024), 16, lane * 16, so + j * 1024, 0, 0);
+    }
+  };
+  // the wave's loads and LDS operations done, then the workgroup's barrier
+  auto tiles_wait = [&]() __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(7 << 4);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
 
   // this lane's query (B operand): channels 16 c + 8 h .. +8
   const int qrow = min(q0 + lc, p.n_q - 1);
@@ -308,14 +338,18 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
   // fragment reads: K row of key 32 sub + kperm(lc), chunk 2 c + h; V rows by the transposing
   // read (lane i of 16 points at four channels of row i / 4 and gets channel i of the four rows)
   const int k_rd = kperm(lc) * G::KP + 16 * h;
-  const int v_rd = G::ST * G::KT + (M32 ? (4 * h + (i16 >> 2)) * G::VP + (g16 & 1) * 32 : (4 * g16 + (i16 >> 2)) * G::VP) + (i16 & 3) * 8;
+  const int v_rd = G::ST * G::KS + (M32 ? (4 * h + (i16 >> 2)) * G::VP + (g16 & 1) * 32 : (4 * g16 + (i16 >> 2)) * G::VP) + (i16 & 3) * 8;
   auto k_frag = [&](int t, int sub, int c) __attribute__((always_inline)) {
-    return *reinterpret_cast<const bf16x8*>(smem + (G::ST == 2 ? t & 1 : 0) * G::KT + sub * 32 * G::KP + k_rd + 32 * c);
+    // (prepared rows end with channel D: the last chunk's upper half reads zeros)
+    int at = sub * 32 * G::KP + k_rd + 32 * c;
+    if constexpr (PREP && D % 16 != 0)
+      if (c == NC - 1) at = h ? G::KT : at;
+    return *reinterpret_cast<const bf16x8*>(smem + (G::ST == 2 ? t & 1 : 0) * G::KS + at);
   };
   // O^T tile tt; M32: keys 16 ci .. +16 of the half, else all its 32.  vt: the tile holds V^T rows
   const int vt_row = M32 ? lc : i16;
-  const int vt_rd[2] = {G::ST * G::KT + vt_row * 128 + ((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) * 16,
-                        G::ST * G::KT + vt_row * 128 + (((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) ^ (M32 ? 2 : 4)) * 16};
+  const int vt_rd[2] = {G::ST * G::KS + vt_row * 128 + ((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) * 16,
+                        G::ST * G::KS + vt_row * 128 + (((M32 ? h : g16) ^ ((vt_row >> 1) & 7)) ^ (M32 ? 2 : 4)) * 16};
   auto vt_frag = [&](int t, int sub, int tt, int ci) __attribute__((always_inline)) {
     // (the chunk's number 4 sub + 2 ci + h, or 4 sub + lane / 16, is swizzled by row; M32's 4 sub is an XOR of
     // the address by 64)
@@ -407,7 +441,8 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
   auto needs_care = [&]() __attribute__((always_inline)) { return __any(!(fabsf(m_run) <= 2 * kHuge)); };
 
   auto tiles_sync = [&]() __attribute__((always_inline)) {
-    if constexpr (KG == 1) lds_sync();
+    if constexpr (PREP) tiles_wait();
+    else if constexpr (KG == 1) lds_sync();
     else asm volatile("" ::: "memory");    // one wave's LDS operations are in order
   };
   // One 32-key half: exponentials of its scores sc between the MFMAs of the next half's scores
@@ -419,7 +454,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
     constexpr int VF = M32 ? 2 : 1;
     bf16x8 vp[VF][NT], kn[NEXT ? NC : 1];
     auto v_frags = [&](int ci) __attribute__((always_inline)) {
-      if (G::FRESH && vt) {
+      if (PREP || (G::FRESH && vt)) {
 #pragma unroll
         for (int tt = 0; tt < NT; ++tt) vp[M32 ? ci : 0][tt] = vt_frag(pt, psub, tt, ci);
       } else {
@@ -540,6 +575,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
         }
       careful = needs_care();
     }
+    if constexpr (G::ONES) return;
     // the sum of the rounded probabilities, in fp32
     const bf16x2 one2 = {(bf16)1.0f, (bf16)1.0f};
     const u32x4 pa = __builtin_bit_cast(u32x4, pc[0]), pb = __builtin_bit_cast(u32x4, pc[1]);
@@ -567,9 +603,13 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
   // ty1 .. ty4: kinds of tiles t .. t + 3; vt0: tile t - 1 holds V^T
   auto tile = [&](int t) __attribute__((always_inline)) { return min(t, te - 1); };
   if (KG == 1 || t0 < te) {
-    int ty1 = type_of(t0), ty2 = type_of(tile(t0 + 1)), ty3 = type_of(tile(t0 + 2));
+    int ty1 = PREP ? 0 : type_of(t0), ty2 = PREP ? 0 : type_of(tile(t0 + 1)), ty3 = PREP ? 0 : type_of(tile(t0 + 2));
     Raw kr, vr;
-    if constexpr (G::ST == 2) {
+    if constexpr (PREP) {
+      issue(kK, t0);
+      issue(kV, t0);
+      issue(kK, tile(t0 + 1));
+    } else if constexpr (G::ST == 2) {
       Raw kr1;
       load(kK, kr, t0, ty1);
       load(kV, vr, t0, ty1);
@@ -601,6 +641,12 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
       const bool vt1 = ty1 == kFresh;
       step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
       tiles_sync();
+      if constexpr (PREP) {
+        if (t + 2 < te) issue(kK, t + 2);
+        issue(kV, t + 1);
+        step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa);
+        continue;
+      }
       const int t3 = tile(t + 3), ty4 = type_of(t3);
       if (t + KA < te) store(kK, kr, t + KA, G::ST == 2 ? ty3 : ty2);
       load(kK, kr, G::ST == 2 ? t3 : tile(t + 2), G::ST == 2 ? ty4 : ty3);
@@ -621,11 +667,20 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
     p_swap(pa);
     static_for<0, NT>([&](auto tc) {
       constexpr int tt = decltype(tc)::value;
-      pv(tc, std::integral_constant<int, 0>{}, vt1 ? vt_frag(t, 1, tt, 0) : v_frag(t, 1, tt, 0), pa[0]);
-      pv(tc, std::integral_constant<int, 1>{}, vt1 ? vt_frag(t, 1, tt, 1) : v_frag(t, 1, tt, 1), pa[1]);
+      pv(tc, std::integral_constant<int, 0>{}, PREP || vt1 ? vt_frag(t, 1, tt, 0) : v_frag(t, 1, tt, 0), pa[0]);
+      pv(tc, std::integral_constant<int, 1>{}, PREP || vt1 ? vt_frag(t, 1, tt, 1) : v_frag(t, 1, tt, 1), pa[1]);
     });
   }
-  l_run += __shfl_xor(l_run, 32, kWave);
+  if constexpr (G::ONES) {
+    // row D of O^T, of query 16 j + i: register (D % 16) % 4 of lane 16 (D % 16 / 4) + i
+    constexpr int f0 = 2 * (D / 16), r0 = D % 16 % 4;
+    float lj[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) lj[j] = __shfl(oo[(f0 + j) / 4][4 * ((f0 + j) % 4) + r0], 16 * (D % 16 / 4) + i16, kWave);
+    l_run = lc < 16 ? lj[0] : lj[1];
+  } else {
+    l_run += __shfl_xor(l_run, 32, kWave);
+  }
 
   // key groups: group 0 takes the others' parts, [register][lane] in their tiles' places, in their order
   if constexpr (KG > 1) {
@@ -696,6 +751,98 @@ __global__ __launch_bounds__(256, (Geo<D, NW>::WPE)) void attn_q8_kernel(AttnQPa
   if (!whole && h == 0 && q0 + lc < p.n_q)
     sp.part_ml[((size_t)unit * sp.ns + part) * (32 * NW) + 32 * wave + lc] = make_float2(m_run, l_run);
 #endif
+}
+
+// ---------------------------------------------------------------------------
+// Prepared tiles.  Every 128 queries of a (branch, head) read the same keys, and a wave's VALU work is
+// paid in full next to its MFMAs: with many queries the keys are widened once, fresh and cached ones
+// together, into tiles that lie in memory as they will in LDS: K rows of KP bytes, V^T rows of 64 keys
+// with their 16-byte chunks swizzled by row (keys past the last are zeros).
+template <int D>
+__global__ __launch_bounds__(256) void attn_q8_prepare_kernel(AttnQParams p, char* tiles) {
+  using G = Geo<D, 4, true>;
+  constexpr int CPT = G::CPT, PITCH = D + 4, QUADS = D / 4;
+  __shared__ __attribute__((aligned(16))) unsigned char bytes[BKV * PITCH];
+  const int tid = threadIdx.x, t = blockIdx.x, pair = blockIdx.y;
+  const int b = pair / p.heads, head = pair - b * p.heads;
+  const int N = p.c.tokens, nf = p.n_fresh, fb = nf > 0 ? p.fresh_begin : 0, n0 = t * BKV;
+  const size_t H = (size_t)p.heads * D;
+  const unsigned char* vals = p.c.values + b * p.c.values_bs;
+  const unsigned char* exps = p.c.exps + b * p.c.exps_bs;
+  const size_t krow = (size_t)head * N + n0, vrow = (size_t)(p.heads + head) * N + n0;
+  const bf16* kf = reinterpret_cast<const bf16*>(p.kv_fresh) + b * p.fresh_bs + (size_t)head * nf * D;
+  const bf16* vf = reinterpret_cast<const bf16*>(p.kv_fresh) + b * p.fresh_bs + nf * H + (size_t)head * D * nf;
+  char* img = tiles + ((size_t)pair * gridDim.x + t) * (G::KT + G::VT);
+  auto fresh = [&](int key) { return (unsigned)(n0 + key - fb) < (unsigned)nf; };
+
+  u32x2 vb[(BKV * CPT + 255) / 256];
+#pragma unroll
+  for (int i = 0; i < (BKV * CPT + 255) / 256; ++i) {
+    const int id = i * 256 + tid, key = id / CPT;
+    vb[i] = id < BKV * CPT && n0 + key < N && !fresh(key) ? *reinterpret_cast<const u32x2*>(vals + vrow * D + (size_t)id * 8) : u32x2{0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < (BKV * CPT + 255) / 256; ++i) {
+    const int id = i * 256 + tid, key = id / CPT, ch = id - key * CPT;
+    if (id >= BKV * CPT) continue;
+    u32x4 x = {0, 0, 0, 0};
+    if (fresh(key)) {
+      x = *reinterpret_cast<const u32x4*>(kf + (size_t)(n0 + key - fb) * D + ch * 8);
+    } else if (n0 + key < N) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(vals + krow * D + (size_t)id * 8);
+      const float s = scale_of(exps[krow + key]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        x[2 * k] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[k], s, false));
+        x[2 * k + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[k], s, true));
+      }
+    }
+    *reinterpret_cast<u32x4*>(img + key * G::KP + ch * 16) = x;
+    unsigned* to = reinterpret_cast<unsigned*>(bytes + key * PITCH + ch * 8);
+    to[0] = vb[i][0];
+    to[1] = vb[i][1];
+  }
+  __syncthreads();
+  // V^T: 8 keys x 4 channels a thread, eight neighbouring lanes the same keys
+  const int lane = tid & 63, tg = lane >> 3, quad = (tid >> 6) * 8 + (lane & 7);
+  auto put = [&](int c, const u32x4& x) {
+    *reinterpret_cast<u32x4*>(img + G::KT + c * 128 + ((tg ^ ((c >> 1) & 7)) * 16)) = x;
+  };
+  if constexpr (G::ONES)
+    if (quad == QUADS) put(D, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+  if (quad >= QUADS) return;
+  const int f = n0 + 8 * tg - fb;
+  if (f >= 0 && f + 8 <= nf) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const u32x4_u x = *reinterpret_cast<const u32x4_u*>(vf + (size_t)(4 * quad + c) * nf + f);
+      put(4 * quad + c, u32x4{x[0], x[1], x[2], x[3]});
+    }
+    return;
+  }
+  unsigned short o[4][8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int key = 8 * tg + e;
+    const float s = scale_of(n0 + key < N ? exps[vrow + key] : 127u);
+    const unsigned w = *reinterpret_cast<const unsigned*>(bytes + key * PITCH + 4 * quad);
+    const unsigned lo = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false));
+    const unsigned hi = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true));
+    o[0][e] = (unsigned short)lo;
+    o[1][e] = (unsigned short)(lo >> 16);
+    o[2][e] = (unsigned short)hi;
+    o[3][e] = (unsigned short)(hi >> 16);
+    if (fresh(key))
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c][e] = reinterpret_cast<const unsigned short*>(vf)[(size_t)(4 * quad + c) * nf + f + e];
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    u32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = o[c][2 * e] | (unsigned)o[c][2 * e + 1] << 16;
+    put(4 * quad + c, x);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1017,12 +1164,31 @@ hipError_t launch(K kern, int lds, int threads, size_t groups, const AttnQParams
   return hipGetLastError();
 }
 
-template <int D, int NW>
+template <int D, int NW, bool PREP>
 hipError_t launch_bf16(const Plan& pl, const AttnQParams& p, const Split& sp, hipStream_t s) {
-  constexpr int lds = Geo<D, NW>::LDS;
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_q8_kernel<D, NW>),
+  constexpr int lds = Geo<D, NW, PREP>::LDS;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_q8_kernel<D, NW, PREP>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  return attr != hipSuccess ? attr : launch(attn_q8_kernel<D, NW>, lds, 256, pl.tiles * pl.ns, p, sp, s);
+  return attr != hipSuccess ? attr : launch(attn_q8_kernel<D, NW, PREP>, lds, 256, pl.tiles * pl.ns, p, sp, s);
+}
+
+// Tiles are prepared from this many queries on.
+constexpr int kPrepareQueries = 512;
+
+// Bytes of the prepared tiles (0: not prepared).
+size_t tile_bytes(int B, int heads, int n_q, int n_kv, int d, int dtype) {
+  size_t r = 0;
+  if (dtype == kBF16 && n_q >= kPrepareQueries)
+    with_d(d, [&](auto dc) {
+      using G = Geo<decltype(dc)::value, 4, true>;
+      const size_t one = (size_t)ceil_div(n_kv, BKV) * (G::KT + G::VT);
+      if (one < (size_t)1 << 31) r = one * B * heads;
+    });
+  return r;
+}
+
+size_t split_bytes(const Plan& pl, int d) {
+  return pl.ns == 1 ? 0 : part_floats(pl, d) * 4 + pl.tiles * pl.ns * 32 * pl.nw * sizeof(float2);
 }
 
 }  // namespace q8attn
@@ -1031,8 +1197,7 @@ size_t attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, 
   using namespace q8attn;
   if (n_q <= 0) return 0;
   const Plan pl = plan(B, heads, n_q, n_kv, d, dtype);
-  if (pl.nw == 0 || pl.ns == 1) return 0;
-  return part_floats(pl, d) * 4 + pl.tiles * pl.ns * 32 * pl.nw * sizeof(float2);
+  return pl.nw == 0 ? 0 : split_bytes(pl, d) + tile_bytes(B, heads, n_q, n_kv, d, dtype);
 }
 
 hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream_t s) {
@@ -1040,17 +1205,28 @@ hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream
   if (p.n_q <= 0) return hipSuccess;
   Plan pl = plan(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype);
   if (pl.nw == 0) return hipErrorInvalidValue;
-  if (!p.ws) pl.ns = 1;
+  const size_t split = split_bytes(pl, p.d), tiles = tile_bytes(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype);
+  // (a workspace too small for both holds the parts alone, or nothing)
+  const bool prepare = pl.nw == 4 && tiles > 0 && p.ws && p.ws_bytes >= split + tiles;
+  if (!p.ws || p.ws_bytes < split) pl.ns = 1;
   if (pl.tiles * pl.ns > 0x7fffffff) return hipErrorInvalidValue;
-  Split sp{pl.ns, nullptr, nullptr};
+  Split sp{nullptr, pl.ns, nullptr, nullptr};
+  if (prepare) sp.tiles = reinterpret_cast<const char*>(p.ws);
   if (pl.ns > 1) {
-    sp.part_o = reinterpret_cast<float*>(p.ws);
+    sp.part_o = reinterpret_cast<float*>((char*)p.ws + (prepare ? tiles : 0));
     sp.part_ml = reinterpret_cast<float2*>(sp.part_o + part_floats(pl, p.d));
   }
   hipError_t rc = hipErrorInvalidValue;
   with_d(p.d, [&](auto dc) {
     constexpr int D = decltype(dc)::value;
-    if (dtype == kBF16) rc = pl.nw == 4 ? launch_bf16<D, 4>(pl, p, sp, s) : launch_bf16<D, 1>(pl, p, sp, s);
+    if (dtype == kBF16 && prepare) {
+      hipLaunchKernelGGL(attn_q8_prepare_kernel<D>, dim3(ceil_div(p.c.tokens, BKV), p.B * p.heads), dim3(256), 0, s, p,
+                         reinterpret_cast<char*>(p.ws));
+      rc = hipGetLastError();
+      if (rc == hipSuccess) rc = launch_bf16<D, 4, true>(pl, p, sp, s);
+      return;
+    }
+    if (dtype == kBF16) rc = pl.nw == 4 ? launch_bf16<D, 4, false>(pl, p, sp, s) : launch_bf16<D, 1, false>(pl, p, sp, s);
     else if (pl.nw == 4) rc = launch(attn_q8_f32_kernel<D, 4>, Geo32<D, 4>::LDS, 256, pl.tiles * pl.ns, p, sp, s);
     else rc = launch(attn_q8_f32_kernel<D, 2>, Geo32<D, 2>::LDS, 128, pl.tiles * pl.ns, p, sp, s);
   });

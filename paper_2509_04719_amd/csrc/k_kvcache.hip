@@ -48,21 +48,41 @@ __device__ __forceinline__ unsigned to_e4m3(float a, float b, float s) {
   return (unsigned short)r[0];
 }
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* src, bool vec, int count, float (&v)[8]) {
-  typedef T vec8 __attribute__((ext_vector_type(8)));
-  if (vec) {
-    const vec8 x = *reinterpret_cast<const vec8*>(src);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = to_f<T>(x[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < count ? to_f<T>(src[e]) : 0.0f;
-  }
+// max over the 8 lanes of an aligned group, on the VALU
+__device__ __forceinline__ unsigned max8(unsigned v) {
+  v = max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, false));    // quad_perm 1, 0, 3, 2
+  v = max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, false));    // quad_perm 2, 3, 0, 1
+  return max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, false));  // row_half_mirror
 }
 
-// G lanes take a K row of d = 8 x chunks channels, a chunk each.
-__host__ __device__ inline int row_lanes(int d) { return d <= 32 ? 4 : d <= 64 ? 8 : 16; }
+template <typename T>
+__device__ __forceinline__ void load8(const T* src, float (&v)[8]) {
+  typedef T vec8 __attribute__((ext_vector_type(8)));
+  const vec8 x = *reinterpret_cast<const vec8*>(src);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = to_f<T>(x[e]);
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* dst, const float (&v)[8]) {
+  typedef T vec8 __attribute__((ext_vector_type(8)));
+  vec8 x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = from_f<T>(v[e]);
+  *reinterpret_cast<vec8*>(dst) = x;
+}
+
+template <int D>
+struct Geo {
+  static constexpr int CPT = D / 8;              // 8-channel chunks of a token
+  // K, writing: LPR lanes a row, chunks j, j + LPR, ...
+  static constexpr int LPR = D == 72 ? 3 : D == 80 ? 2 : 4, CPR = CPT / LPR, RPW = 64 / LPR;   // rows of a wave
+  // V: a thread holds 8 tokens x 4 channels
+  static constexpr int QUADS = D / 4, THREADS = (QUADS * 8 + 63) / 64 * 64, WAVES = THREADS / 64;
+  static constexpr int PITCH = D + 4;            // bytes of a token's row in LDS
+  static constexpr int KROWS = WAVES * RPW;      // K rows of a workgroup, writing
+  static constexpr int KCH = 4;                  // K chunks of a thread, reading back
+};
 
 struct Launch {
   KvCacheParams p;
@@ -70,171 +90,205 @@ struct Launch {
   int vec;           // V^T rows and offsets in whole 16-byte chunks
 };
 
-template <typename T>
+template <typename T, int D>
 __global__ __launch_bounds__(256) void kv_quantize_kernel(Launch L) {
+  using G = Geo<D>;
   const KvCacheParams& p = L.p;
-  const int b = blockIdx.y / p.heads, h = blockIdx.y - b * p.heads, tid = threadIdx.x;
-  const size_t H = (size_t)p.heads * p.d;
+  const int b = blockIdx.y / p.heads, h = blockIdx.y - b * p.heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const size_t H = (size_t)p.heads * D;
   const T* kv = reinterpret_cast<const T*>(p.kv) + b * p.kv_bs;
   unsigned char* vals = p.c.values + b * p.c.values_bs;
   unsigned char* exps = p.c.exps + b * p.c.exps_bs;
   if ((int)blockIdx.x < L.k_blocks) {
-    const int G = row_lanes(p.d), ch = tid % G;
-    const int n = blockIdx.x * (256 / G) + tid / G;
-    const bool on = n < p.n && ch * 8 < p.d;
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (on) load8(kv + ((size_t)h * p.kv_tokens + p.kv_off + n) * p.d + ch * 8, true, 8, v);
+    const int r = lane / G::LPR, j = lane - r * G::LPR, n = blockIdx.x * G::KROWS + wave * G::RPW + r;
+    const bool on = n < p.n && r < G::RPW;
+    const T* src = kv + ((size_t)h * p.kv_tokens + p.kv_off + (on ? n : 0)) * D + j * 8;
+    float v[G::CPR][8];
     unsigned amax = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) amax = max(amax, finite_bits(v[e]));
-    for (int o = 1; o < G; o <<= 1) amax = max(amax, (unsigned)__shfl_xor((int)amax, o, kWave));
+    for (int i = 0; i < G::CPR; ++i) load8(src + i * G::LPR * 8, v[i]);
+#pragma unroll
+    for (int i = 0; i < G::CPR; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) amax = max(amax, finite_bits(v[i][e]));
+    unsigned all = amax;
+#pragma unroll
+    for (int k = 1; k < G::LPR; ++k) all = max(all, (unsigned)__shfl((int)amax, r * G::LPR + (j + k) % G::LPR, kWave));
     if (!on) return;
-    const unsigned e8 = scale_byte(amax);
+    const unsigned e8 = scale_byte(all);
     const float s = scale_of(e8);
     const size_t row = (size_t)h * p.c.tokens + p.c_off + n;
-    u32x2 w;
-    w[0] = to_e4m3(v[0], v[1], s) | to_e4m3(v[2], v[3], s) << 16;
-    w[1] = to_e4m3(v[4], v[5], s) | to_e4m3(v[6], v[7], s) << 16;
-    *reinterpret_cast<u32x2*>(vals + row * p.d + ch * 8) = w;
-    if (ch == 0) exps[row] = (unsigned char)e8;
+#pragma unroll
+    for (int i = 0; i < G::CPR; ++i) {
+      u32x2 w;
+      w[0] = to_e4m3(v[i][0], v[i][1], s) | to_e4m3(v[i][2], v[i][3], s) << 16;
+      w[1] = to_e4m3(v[i][4], v[i][5], s) | to_e4m3(v[i][6], v[i][7], s) << 16;
+      *reinterpret_cast<u32x2*>(vals + row * D + (j + i * G::LPR) * 8) = w;
+    }
+    if (j == 0) exps[row] = (unsigned char)e8;
     return;
   }
-  // V: thread (cl, tg) holds tokens 8 tg .. +8 of channels cl + 32 i
-  __shared__ unsigned red[4][kTile];
-  __shared__ __attribute__((aligned(16))) unsigned char tile[kTile * 136];
+  // V: eight neighbouring lanes hold the same 8 tokens, 4 channels each
+  __shared__ unsigned red[G::WAVES][kTile];
+  __shared__ __attribute__((aligned(16))) unsigned char tile[kTile * G::PITCH];
   const int n0 = (blockIdx.x - L.k_blocks) * kTile;
-  const int tg = tid & 7, cl = tid >> 3, pitch = p.d + 8;
+  const int tg = lane >> 3, quad = wave * 8 + (lane & 7);
+  const bool on = quad < G::QUADS;
   const int count = min(max(p.n - n0 - 8 * tg, 0), 8);
-  const T* vt = kv + p.kv_tokens * H + (size_t)h * p.d * p.kv_tokens + p.kv_off + n0 + 8 * tg;
+  const T* vt = kv + p.kv_tokens * H + ((size_t)h * D + 4 * (on ? quad : 0)) * p.kv_tokens + p.kv_off + n0 + 8 * tg;
   float v[4][8];
-  unsigned amax[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = cl + 32 * i;
-    if (c < p.d && count > 0) load8(vt + (size_t)c * p.kv_tokens, L.vec && count == 8, count, v[i]);
-    else
+  for (int c = 0; c < 4; ++c) {
+    if (L.vec && count == 8) {
+      load8(vt + (size_t)c * p.kv_tokens, v[c]);
+    } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) amax[e] = max(amax[e], finite_bits(v[i][e]));
+      for (int e = 0; e < 8; ++e) v[c][e] = e < count ? to_f<T>(vt[(size_t)c * p.kv_tokens + e]) : 0.0f;
+    }
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-#pragma unroll
-    for (int o = 8; o < 64; o <<= 1) amax[e] = max(amax[e], (unsigned)__shfl_xor((int)amax[e], o, kWave));
-    if ((tid & 63) < 8) red[tid >> 6][8 * tg + e] = amax[e];
+    const unsigned m = max(max(finite_bits(v[0][e]), finite_bits(v[1][e])), max(finite_bits(v[2][e]), finite_bits(v[3][e])));
+    const unsigned all = max8(on ? m : 0u);
+    if ((lane & 7) == e) red[wave][8 * tg + e] = all;
   }
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int t = 8 * tg + e;
-    const unsigned e8 = scale_byte(max(max(red[0][t], red[1][t]), max(red[2][t], red[3][t])));
-    const float s = scale_of(e8);
+    unsigned amax = red[0][t];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (cl + 32 * i < p.d) tile[t * pitch + cl + 32 * i] = (unsigned char)to_e4m3(v[i][e], 0.0f, s);
-    if (cl == 0 && e < count)
-      exps[(size_t)(p.heads + h) * p.c.tokens + p.c_off + n0 + t] = (unsigned char)e8;
+    for (int w = 1; w < G::WAVES; ++w) amax = max(amax, red[w][t]);
+    const unsigned e8 = scale_byte(amax);
+    const float s = scale_of(e8);
+    if (on) *reinterpret_cast<unsigned*>(tile + t * G::PITCH + 4 * quad) = to_e4m3(v[0][e], v[1][e], s) | to_e4m3(v[2][e], v[3][e], s) << 16;
+    if (quad == 0 && e < count) exps[(size_t)(p.heads + h) * p.c.tokens + p.c_off + n0 + t] = (unsigned char)e8;
   }
   __syncthreads();
-  unsigned char* dst = vals + ((size_t)(p.heads + h) * p.c.tokens + p.c_off + n0) * p.d;
-  const int chunks = p.d / 8, total = min(kTile, p.n - n0) * chunks;
-  for (int i = tid; i < total; i += 256) {
-    const int t = i / chunks, ch = i - t * chunks;
-    *reinterpret_cast<u32x2*>(dst + (size_t)i * 8) = *reinterpret_cast<const u32x2*>(tile + t * pitch + ch * 8);
+  unsigned char* dst = vals + ((size_t)(p.heads + h) * p.c.tokens + p.c_off + n0) * D;
+  const int total = min(kTile, p.n - n0) * G::CPT;
+  for (int i = tid; i < total; i += G::THREADS) {
+    const unsigned* src = reinterpret_cast<const unsigned*>(tile + i / G::CPT * G::PITCH + i % G::CPT * 8);
+    *reinterpret_cast<u32x2*>(dst + (size_t)i * 8) = u32x2{src[0], src[1]};
   }
 }
 
-// the 8 values of two words of e4m3 bytes, times s
-__device__ __forceinline__ void from_e4m3(u32x2 w, float s, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], s, false);
-    const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], s, true);
-    v[4 * i] = lo[0];
-    v[4 * i + 1] = lo[1];
-    v[4 * i + 2] = hi[0];
-    v[4 * i + 3] = hi[1];
-  }
+// four values of a word of e4m3 bytes, times s
+__device__ __forceinline__ void from_e4m3(unsigned w, float s, float (&v)[4]) {
+  const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false);
+  const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true);
+  v[0] = lo[0];
+  v[1] = lo[1];
+  v[2] = hi[0];
+  v[3] = hi[1];
 }
 
-template <typename T>
-__device__ __forceinline__ void store8(T* dst, bool vec, int count, const float (&v)[8]) {
-  typedef T vec8 __attribute__((ext_vector_type(8)));
-  if (vec) {
-    vec8 x;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = from_f<T>(v[e]);
-    *reinterpret_cast<vec8*>(dst) = x;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < count) dst[e] = from_f<T>(v[e]);
-  }
-}
-
-template <typename T>
+template <typename T, int D>
 __global__ __launch_bounds__(256) void kv_dequantize_kernel(Launch L) {
+  using G = Geo<D>;
   const KvCacheParams& p = L.p;
   const int b = blockIdx.y / p.heads, h = blockIdx.y - b * p.heads, tid = threadIdx.x;
-  const size_t H = (size_t)p.heads * p.d;
+  const size_t H = (size_t)p.heads * D;
   T* kv = reinterpret_cast<T*>(p.kv) + b * p.kv_bs;
   const unsigned char* vals = p.c.values + b * p.c.values_bs;
   const unsigned char* exps = p.c.exps + b * p.c.exps_bs;
   if ((int)blockIdx.x < L.k_blocks) {
-    const int G = row_lanes(p.d), ch = tid % G;
-    const int n = blockIdx.x * (256 / G) + tid / G;
-    if (n >= p.n || ch * 8 >= p.d) return;
-    const size_t row = (size_t)h * p.c.tokens + p.c_off + n;
-    float v[8];
-    from_e4m3(*reinterpret_cast<const u32x2*>(vals + row * p.d + ch * 8), scale_of(exps[row]), v);
-    store8(kv + ((size_t)h * p.kv_tokens + p.kv_off + n) * p.d + ch * 8, true, 8, v);
+    // both sides contiguous: chunk after chunk
+    const size_t row0 = (size_t)h * p.c.tokens + p.c_off;
+    T* dst = kv + ((size_t)h * p.kv_tokens + p.kv_off) * D;
+    const int first = blockIdx.x * G::THREADS * G::KCH, total = p.n * G::CPT;
+    u32x2 w[G::KCH];
+    float s[G::KCH];
+#pragma unroll
+    for (int k = 0; k < G::KCH; ++k) {
+      const int i = min(first + k * G::THREADS + tid, total - 1);
+      w[k] = *reinterpret_cast<const u32x2*>(vals + row0 * D + (size_t)i * 8);
+      s[k] = scale_of(exps[row0 + i / G::CPT]);
+    }
+#pragma unroll
+    for (int k = 0; k < G::KCH; ++k) {
+      const int i = first + k * G::THREADS + tid;
+      float lo[4], hi[4];
+      from_e4m3(w[k][0], s[k], lo);
+      from_e4m3(w[k][1], s[k], hi);
+      if (i < total) store8(dst + (size_t)i * 8, {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    }
     return;
   }
-  __shared__ __attribute__((aligned(16))) unsigned char tile[kTile * 136];
+  __shared__ __attribute__((aligned(16))) unsigned char tile[kTile * G::PITCH];
   const int n0 = (blockIdx.x - L.k_blocks) * kTile;
-  const int chunks = p.d / 8, total = min(kTile, p.n - n0) * chunks, pitch = p.d + 8;
+  const int total = min(kTile, p.n - n0) * G::CPT;
   const size_t row0 = (size_t)(p.heads + h) * p.c.tokens + p.c_off + n0;
-  for (int i = tid; i < total; i += 256) {
-    const int t = i / chunks, ch = i - t * chunks;
-    *reinterpret_cast<u32x2*>(tile + t * pitch + ch * 8) = *reinterpret_cast<const u32x2*>(vals + row0 * p.d + (size_t)i * 8);
-  }
-  __syncthreads();
-  const int tg = tid & 7, cl = tid >> 3;
+  const int lane = tid & 63, tg = lane >> 3, quad = (tid >> 6) * 8 + (lane & 7);
   const int count = min(max(p.n - n0 - 8 * tg, 0), 8);
-  if (count == 0) return;
   float s[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s[e] = scale_of(e < count ? exps[row0 + 8 * tg + e] : 127u);
-  T* vt = kv + p.kv_tokens * H + (size_t)h * p.d * p.kv_tokens + p.kv_off + n0 + 8 * tg;
-  for (int c = cl; c < p.d; c += 32) {
-    float v[8];
+  for (int e = 0; e < 8; ++e) s[e] = scale_of(exps[row0 + (e < count ? 8 * tg + e : 0)]);
+  for (int i = tid; i < total; i += G::THREADS) {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(vals + row0 * D + (size_t)i * 8);
+    unsigned* to = reinterpret_cast<unsigned*>(tile + i / G::CPT * G::PITCH + i % G::CPT * 8);
+    to[0] = x[0];
+    to[1] = x[1];
+  }
+  __syncthreads();
+  if (count == 0 || quad >= G::QUADS) return;
+  float v[4][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      v[e] = e < count ? __builtin_amdgcn_cvt_scalef32_f32_fp8((unsigned)tile[(8 * tg + e) * pitch + c], s[e], 0) : 0.0f;
-    store8(vt + (size_t)c * p.kv_tokens, L.vec && count == 8, count, v);
+  for (int e = 0; e < 8; ++e) {
+    // (past the last token: bytes of another workgroup, not stored)
+    float x[4];
+    from_e4m3(*reinterpret_cast<const unsigned*>(tile + (8 * tg + e) * G::PITCH + 4 * quad), s[e], x);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c][e] = x[c];
+  }
+  T* vt = kv + p.kv_tokens * H + ((size_t)h * D + 4 * quad) * p.kv_tokens + p.kv_off + n0 + 8 * tg;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    if (L.vec && count == 8) {
+      store8(vt + (size_t)c * p.kv_tokens, v[c]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < count) vt[(size_t)c * p.kv_tokens + e] = from_f<T>(v[c][e]);
+    }
   }
 }
 
-template <typename K>
-hipError_t launch(K kern, const KvCacheParams& p, int esize, hipStream_t s) {
-  if (p.n <= 0) return hipSuccess;
+template <typename T, int D>
+hipError_t launch_d(const KvCacheParams& p, bool back, hipStream_t s) {
+  using G = Geo<D>;
   Launch L;
   L.p = p;
-  L.k_blocks = ceil_div(p.n, 256 / row_lanes(p.d));
+  L.k_blocks = back ? ceil_div(p.n * G::CPT, G::THREADS * G::KCH) : ceil_div(p.n, G::KROWS);
   L.vec = p.kv_tokens % 8 == 0 && p.kv_off % 8 == 0;
-  hipLaunchKernelGGL(kern, dim3(L.k_blocks + ceil_div(p.n, kTile), p.heads * p.B), dim3(256), 0, s, L);
+  const dim3 grid(L.k_blocks + ceil_div(p.n, kTile), p.heads * p.B), block(G::THREADS);
+  if (back) hipLaunchKernelGGL((kv_dequantize_kernel<T, D>), grid, block, 0, s, L);
+  else hipLaunchKernelGGL((kv_quantize_kernel<T, D>), grid, block, 0, s, L);
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch(const KvCacheParams& p, bool back, hipStream_t s) {
+  if (p.n <= 0) return hipSuccess;
+  switch (p.d) {
+    case 32: return launch_d<T, 32>(p, back, s);
+    case 64: return launch_d<T, 64>(p, back, s);
+    case 72: return launch_d<T, 72>(p, back, s);
+    case 80: return launch_d<T, 80>(p, back, s);
+    case 96: return launch_d<T, 96>(p, back, s);
+    case 128: return launch_d<T, 128>(p, back, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 hipError_t launch_kv_quantize(const KvCacheParams& p, int dtype, hipStream_t s) {
-  return dtype == kBF16 ? launch(kv_quantize_kernel<bf16>, p, 2, s) : launch(kv_quantize_kernel<float>, p, 4, s);
+  return dtype == kBF16 ? launch<bf16>(p, false, s) : launch<float>(p, false, s);
 }
 
 hipError_t launch_kv_dequantize(const KvCacheParams& p, int dtype, hipStream_t s) {
-  return dtype == kBF16 ? launch(kv_dequantize_kernel<bf16>, p, 2, s) : launch(kv_dequantize_kernel<float>, p, 4, s);
+  return dtype == kBF16 ? launch<bf16>(p, true, s) : launch<float>(p, true, s);
 }
 
 }  // namespace orch

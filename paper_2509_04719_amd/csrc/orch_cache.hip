@@ -184,19 +184,19 @@ int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache, c
     return fail("device buffers must be 16-byte aligned");
   const size_t fresh_bytes = n_fresh > 0 ? ((B > 1 ? (B - 1) * fresh_bs : 0) + fresh_elems) * es : 0;
   const size_t need = attention_quantized_workspace_bytes(B, heads, n_q, cache->tokens, head_dim, dtype);
-  const bool split = workspace && need > 0 && workspace_bytes >= need;
+  const size_t ws_used = !workspace ? 0 : workspace_bytes < need ? workspace_bytes : need;
   const struct { const void* p; size_t n; } in[] = {{q, q_bytes}, {cache->values, values}, {cache->exponents, exps}, {kv_fresh, fresh_bytes}};
   for (const auto& r : in)
-    if (overlap(out, q_bytes, r.p, r.n) || (split && overlap(workspace, need, r.p, r.n)))
+    if (overlap(out, q_bytes, r.p, r.n) || overlap(workspace, ws_used, r.p, r.n))
       return fail("out or workspace overlaps an input");
-  if (split && overlap(workspace, need, out, q_bytes)) return fail("out and workspace overlap");
+  if (overlap(workspace, ws_used, out, q_bytes)) return fail("out and workspace overlap");
   AttnQParams p{};
   p.q = q; p.out = out; p.kv_fresh = kv_fresh; p.fresh_bs = fresh_bs; p.fresh_begin = fresh_begin; p.n_fresh = n_fresh;
   p.c.values = (unsigned char*)cache->values; p.c.exps = (unsigned char*)cache->exponents;
   p.c.values_bs = cache->values_stride; p.c.exps_bs = cache->exponents_stride; p.c.tokens = cache->tokens;
   p.B = B; p.heads = heads; p.n_q = n_q; p.d = head_dim;
-  p.ws = split ? workspace : nullptr;
-  p.ws_bytes = split ? workspace_bytes : 0;
+  p.ws = ws_used ? workspace : nullptr;
+  p.ws_bytes = ws_used;
   return launched(launch_attention_quantized(p, dtype, (hipStream_t)hip_stream), "attention launch");
 }
 
