@@ -55,28 +55,32 @@ struct Geo {
   static constexpr bool M32 = D % 32 == 0;       // PV on 32x32x16, else on 16x16x32
   static constexpr int NT = M32 ? D / 32 : NC;   // row tiles of O^T
   static constexpr int CPT = D / 8;              // 8-channel chunks of a token
-  // bytes of a K row, an odd number of 16-byte chunks (prepared tiles hold no padding channels)
-  static constexpr int KP = PREP ? (CPT | 1) * 16 : NC * 32 + 16;
-  static constexpr int VP = M32 ? (D * 2 % 128 == 64 ? D * 2 : D * 2 + 64) : NC * 32;   // of a V row
+  // bytes of a K row, an odd number of 16-byte chunks; TRIM: without padding channels
+  static constexpr bool TRIM = PREP || NW == 1;
+  static constexpr int KP = TRIM ? (CPT | 1) * 16 : NC * 32 + 16;
+  // of a V row: an odd multiple of 32 (16-row reads) or 64 (32-row reads; at D = 64 a wave alone
+  // takes 160, some conflicts, for a second workgroup on the CU)
+  static constexpr int VP = !M32 ? NC * 32 : NW == 1 && D == 64 ? 160 : D * 2 % 128 == 64 ? D * 2 : D * 2 + 64;
   // PREP: tiles as they lie in memory, KT bytes of K rows, then VT of V^T rows
   static constexpr int KT = BKV * KP, VT = PREP ? (M32 ? D : 16 * NT) * 128 : BKV * VP;
-  static constexpr int ZERO = PREP && D % 16 ? 1024 : 0;           // zeros behind a K stage: channels past the last
+  static constexpr int ZERO = TRIM && D % 16 ? (PREP ? 1024 : 128) : 0;   // zeros behind a K stage: channels past the last
   static constexpr bool ONES = PREP && !M32 && 16 * NT > D;        // row D of V^T is ones: O^T's row D is the sum
   static constexpr int ST = NW == 4 ? 2 : 1;     // stages: a wave alone needs no second one
   static constexpr int KS = KT + ZERO;           // a K stage
   static constexpr int GROUP = ST * (KS + VT);
+  static_assert(KS % 128 == 0 && VT % 128 == 0, "the swizzle of V^T rows is an XOR of the address");
   static constexpr int LDS = KG * GROUP;
   static constexpr int THREADS = 64 * NW;        // that share a tile
   static constexpr int SL = (BKV * CPT + THREADS - 1) / THREADS;   // chunks of a thread, K and V each
-  static constexpr int WPC = cmin(2, 160 * 1024 / LDS);            // workgroups of a CU, waves of a SIMD
-  static constexpr int WPE = NW == 1 && D == 128 ? 1 : 2;          // waves of a SIMD that registers allow
+  
+  static constexpr int WPE = NW == 1 && D == 128 ? 1 : PREP && D <= 80 ? 3 : 2;          // waves of a SIMD that registers allow
+  static constexpr int WPC = cmin(WPE, 160 * 1024 / LDS);          // workgroups of a CU
   static constexpr bool EVEN = THREADS % CPT == 0;                 // a thread's chunks are THREADS / CPT keys apart
   // NW = 1: lanes of a key, each with CPL chunks in a row, keys 64 / LPK apart
   static constexpr int LPK = D == 128 ? 4 : D == 64 || D == 80 || D == 96 ? 2 : 1;
   static constexpr int CPL = CPT / LPK;
   static constexpr int NE = NW == 1 ? LPK : SL;  // scales of a thread
-  static constexpr bool FRESH = NW == 4 && !PREP;         // tiles of fresh keys alone have a path of their own,
-  static constexpr bool AHEAD = FRESH && D <= 96;   // and are fetched ahead (where registers allow)
+  static constexpr bool AHEAD = NW == 4 && !PREP && D <= 96;       // tiles of fresh keys alone are fetched ahead too
   static constexpr int NO = M32 ? NT : (2 * NT + 3) / 4;           // 16-register blocks of O^T
   static_assert(KG == 1 || (NO * 16 + 2) * 256 <= GROUP, "a group's part fits its tile's place");
 };
@@ -129,8 +133,8 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
 
   // K rows' padding channels [D, 16 NC): zero, never written again (Q's are zero too; V's may
   // hold anything, they end in rows of O^T that nobody reads)
-  if constexpr (PREP && D % 16 != 0) {
-    if (tid < 2) *reinterpret_cast<u32x4*>(smem + tid * G::KS + G::KT) = u32x4{0, 0, 0, 0};
+  if constexpr (G::ZERO > 0) {
+    if (tid < G::ST) *reinterpret_cast<u32x4*>(smem + tid * G::KS + G::KT) = u32x4{0, 0, 0, 0};
   } else if constexpr (D % 16 != 0) {
     for (int i = tid; i < G::ST * BKV; i += TH)
       *reinterpret_cast<u32x4*>(smem + (i / BKV) * G::KS + (i % BKV) * G::KP + 2 * D) = u32x4{0, 0, 0, 0};
@@ -170,8 +174,10 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   auto v_dst = [&](int i) __attribute__((always_inline)) { return ROW ? v_dst_[0] + vrow(i / CPL * KR) * G::VP + i % CPL * 16 : G::EVEN ? v_dst_[0] + vrow(i * KS) * G::VP : v_dst_[i]; };
   // fresh V^T: slot i holds chunk vtid % 8 (8 keys) of channel vtid / 8 + i TH / 8
   const int vt_src = (vtid >> 3) * nf + (vtid & 7) * 8;
-  const int vt_dst = G::ST * G::KS + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
-  static_assert(TH % 128 == 0 || !G::FRESH, "the swizzle repeats from slot to slot");
+  const int vt_dst_ = G::ST * G::KS + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
+  auto vt_dst = [&](int i) __attribute__((always_inline)) {
+    return (TH % 128 == 0 || i % 2 == 0 ? vt_dst_ : vt_dst_ ^ 64) + i * TH * 16;   // (64 threads: 8 rows on, 4 in the swizzle)
+  };
   // the last slot is some waves' alone: the first ones take K's chunks, the last ones V's
   constexpr int LEFT = (BKV * CPT % TH) / 64;
   static_assert(BKV * CPT % 64 == 0, "whole waves");
@@ -183,7 +189,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   auto type_of = [&](int t) __attribute__((always_inline)) {
     const int n0 = t * BKV, n1 = n0 + BKV;
     if (n1 <= N && (n1 <= fb || n0 >= fb + nf)) return (int)kStale;
-    return G::FRESH && n0 >= fb && n1 <= fb + nf ? (int)kFresh : (int)kMixed;
+    return n0 >= fb && n1 <= fb + nf ? (int)kFresh : (int)kMixed;
   };
   // What a thread holds of a tile on its way: the cache's chunks and exponents, read of every tile
   // (unused where the keys are fresh: a load under a branch costs register moves, and those a
@@ -265,35 +271,95 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
         if (on(isk_c, i)) *at(i) = chunk(i);
       return;
     }
-    if constexpr (G::FRESH)
-      if (type == kFresh) {
+    if (type == kFresh) {
+      constexpr int BATCH = G::AHEAD ? SL : cmin(SL, NW == 4 || D == 80 || D == 96 ? 4 : 6);
 #pragma unroll
-        for (int i = 0; i < SL; ++i)
-          if (on(isk_c, i)) {
-            u32x4 x;
-            if constexpr (G::AHEAD) x = r.f[i];
-            else x = load_fresh(isk_c, t, i);
-            *(isk ? at(i) : reinterpret_cast<u32x4*>(dst + vt_dst + i * TH * 16)) = x;
+      for (int i0 = 0; i0 < SL; i0 += BATCH) {
+        u32x4 x[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+          if (i0 + k < SL && on(isk_c, i0 + k)) {
+            if constexpr (G::AHEAD) x[k] = r.f[i0 + k];
+            else x[k] = load_fresh(isk_c, t, i0 + k);
           }
-        return;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+          if (i0 + k < SL && on(isk_c, i0 + k))
+            *reinterpret_cast<u32x4*>(dst + (isk ? (ROW ? (tid + 64 * (i0 + k)) / CPT * G::KP + (tid + 64 * (i0 + k)) % CPT * 16 : k_dst(i0 + k)) : vt_dst(i0 + k))) = x[k];
       }
-    // a tile that the band's edge or the last key crosses (past it the loads gave zeros)
+      return;
+    }
+    // a tile that the band's edge or the last key crosses (past it the loads gave zeros): the
+    // cache's keys, then the fresh ones, K's in rows, V's along the keys
+    const int n0 = t * BKV;
+    auto fresh = [&](int key) __attribute__((always_inline)) { return (unsigned)(n0 + key - fb) < (unsigned)nf; };
+    constexpr int BATCH = cmin(SL, NW == 4 ? 2 : D <= 72 || D == 128 ? 8 : 4);
 #pragma unroll
-    for (int i = 0; i < SL; ++i)
-      if (on(isk_c, i)) {
-        const int ch = chunk_of(isk_c, i), f = t * BKV + key_of(isk_c, i) - fb;
-        u32x4 x = chunk(i);
-        if ((unsigned)f < (unsigned)nf) {
-          if (isk) {
-            x = *reinterpret_cast<const u32x4*>(kf + (size_t)f * D + ch * 8);
-          } else {
-            const unsigned short* src = reinterpret_cast<const unsigned short*>(vf) + (size_t)ch * 8 * nf + f;
+    for (int i0 = 0; i0 < SL; i0 += BATCH) {
+      u32x4 x[BATCH];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = src[(size_t)2 * e * nf] | (unsigned)src[(size_t)(2 * e + 1) * nf] << 16;
+      for (int k = 0; k < BATCH; ++k) {
+        const int i = cmin(i0 + k, SL - 1);
+        x[k] = chunk(i);
+        if (isk && i0 + k < SL && on(isk_c, i) && fresh(key_of(isk_c, i)))
+          x[k] = *reinterpret_cast<const u32x4*>(kf + (size_t)(n0 + key_of(isk_c, i) - fb) * D + chunk_of(isk_c, i) * 8);
+      }
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const int i = cmin(i0 + k, SL - 1);
+        if (i0 + k < SL && on(isk_c, i) && (isk || !fresh(key_of(isk_c, i)))) *at(i) = x[k];
+      }
+    }
+    if (!isk && n0 + BKV > fb && n0 < fb + nf) {
+      // chunk id: channel id / 8, keys 8 (id % 8) .. +8
+      const int kc = 8 * (vtid & 7), f = n0 + kc - fb;
+      unsigned short* col = reinterpret_cast<unsigned short*>(dst + G::ST * G::KS + vrow(kc) * G::VP) + (vtid >> 3);
+#pragma unroll
+      for (int i0 = 0; i0 < SL; i0 += BATCH) {
+        u32x4 x[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+          const int i = cmin(i0 + k, SL - 1);
+          const unsigned short* src = reinterpret_cast<const unsigned short*>(vf) + (size_t)((vtid >> 3) + i * (TH / 8)) * nf + f;
+          x[k] = u32x4{0, 0, 0, 0};
+          if (i0 + k < SL && on(isk_c, i)) {
+            if (f >= 0 && f + 8 <= nf) {
+              const u32x4_u y = *reinterpret_cast<const u32x4_u*>(src);
+              x[k] = u32x4{y[0], y[1], y[2], y[3]};
+            } else if (f > -8 && f < nf) {
+              // (all eight loads in flight: the ones outside the band read its nearest element)
+              unsigned y[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] = src[min(max(f + e, 0), nf - 1) - f];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[k][e] = y[2 * e] | y[2 * e + 1] << 16;
+            }
           }
         }
-        *at(i) = x;
+        if (f >= 0 && f + 8 <= nf) {
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) {
+            const int i = cmin(i0 + k, SL - 1);
+            if (i0 + k < SL && on(isk_c, i)) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                col[vrow(e) * (G::VP / 2) + i * (TH / 8)] = (unsigned short)(x[k][e >> 1] >> (16 * (e & 1)));
+            }
+          }
+        } else {
+#pragma unroll 1
+          for (int e = 0; e < 8; ++e)
+            if ((unsigned)(f + e) < (unsigned)nf) {
+#pragma unroll
+              for (int k = 0; k < BATCH; ++k) {
+                const int i = cmin(i0 + k, SL - 1);
+                const unsigned w = e & 4 ? (e & 2 ? x[k][3] : x[k][2]) : (e & 2 ? x[k][1] : x[k][0]);
+                if (i0 + k < SL && on(isk_c, i)) col[vrow(e) * (G::VP / 2) + i * (TH / 8)] = (unsigned short)(w >> (16 * (e & 1)));
+              }
+            }
+        }
       }
+    }
   };
   constexpr std::true_type kK{};
   constexpr std::false_type kV{};
@@ -340,9 +406,9 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   const int k_rd = kperm(lc) * G::KP + 16 * h;
   const int v_rd = G::ST * G::KS + (M32 ? (4 * h + (i16 >> 2)) * G::VP + (g16 & 1) * 32 : (4 * g16 + (i16 >> 2)) * G::VP) + (i16 & 3) * 8;
   auto k_frag = [&](int t, int sub, int c) __attribute__((always_inline)) {
-    // (prepared rows end with channel D: the last chunk's upper half reads zeros)
+    // (trimmed rows end with channel D: the last chunk's upper half reads zeros)
     int at = sub * 32 * G::KP + k_rd + 32 * c;
-    if constexpr (PREP && D % 16 != 0)
+    if constexpr (G::ZERO > 0)
       if (c == NC - 1) at = h ? G::KT : at;
     return *reinterpret_cast<const bf16x8*>(smem + (G::ST == 2 ? t & 1 : 0) * G::KS + at);
   };
@@ -454,7 +520,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     constexpr int VF = M32 ? 2 : 1;
     bf16x8 vp[VF][NT], kn[NEXT ? NC : 1];
     auto v_frags = [&](int ci) __attribute__((always_inline)) {
-      if (PREP || (G::FRESH && vt)) {
+      if (PREP || vt) {
 #pragma unroll
         for (int tt = 0; tt < NT; ++tt) vp[M32 ? ci : 0][tt] = vt_frag(pt, psub, tt, ci);
       } else {
@@ -1101,11 +1167,17 @@ hipError_t launch_merge(const AttnQParams& p, const Split& sp, int rows, hipStre
 }
 
 // ---------------------------------------------------------------------------
-// The plan of a call: query groups of a workgroup (4, or 1 with the keys shared by its waves) and
-// workgroups that share a query tile's keys.
+// The plan of a call: the variant (tiles prepared or not, query groups of a workgroup) and the number ns
+// of workgroups that share a query tile's keys, by the least estimated time.  In us, at d = 72 (other head
+// sizes scale a tile by 0.5 + d / 140): a workgroup starts and ends in 4.5; a 64-key tile of a workgroup
+// takes the `tile` below, by the workgroups on its CU; parts take 3.5 and their bytes, written and read, at
+// 5 TB/s; preparing 2.5 and 5.5 ns a tile.  Measured against the estimate (2 x 16 heads, d = 72): 384
+// queries x 4096 keys on NW = 4 / ns = 1, 2, 5: 88 / 57 / 39 (88 / 52 / 39 estimated), on NW = 1 / ns = 1 43
+// (43), prepared / ns = 5 39 (44); 1664 x 1024 on NW = 4 / ns = 1, 2 37 / 52 (34 / 54), prepared / 1 32 (29).
 struct Plan {
-  int nw, ns;
+  int nw, ns, prep;
   size_t tiles;
+  double cost;
 };
 
 template <typename F>
@@ -1120,38 +1192,39 @@ void with_d(int d, F&& f) {
   }
 }
 
-// The ns that minimises the rounds of resident workgroups times a wave's key tiles (and two more
-// for its start), with the merge's launch where ns > 1.
-void best_split(long long tiles, int wpc, int groups, int nkt, int* ns, double* cost) {
-  const long long slots = 256 * wpc;
-  for (int n = 1; n * groups <= nkt + groups - 1 && n <= 64; ++n) {
-    const long long rounds = (tiles * n + slots - 1) / slots;
-    const double c = (double)rounds * (ceil_div(nkt, n * groups) + 2) + (n > 1 ? 3.0 : 0.0);
-    if (c < *cost) {
-      *cost = c;
-      *ns = n;
-    }
+// A variant's best ns into *best if it beats it.  rows: queries of a workgroup; groups: key groups of
+// it; tile[c - 1]: a tile's time with c workgroups on the CU; fixed: time before.
+void consider(Plan* best, int nw, int prep, long long pairs, int n_q, int rows, int groups, int nkt, int wpc,
+              const double (&tile)[3], double fixed, int d) {
+  const long long units = ceil_div(n_q, rows) * pairs;
+  const double scale = 0.5 + d / 140.0;
+  for (int ns = 1; ns <= 64 && ns <= ceil_div(nkt, groups); ++ns) {
+    const long long w = units * ns, per_cu = (w + 255) / 256, rounds = (per_cu + wpc - 1) / wpc;
+    const int c = (int)(per_cu < wpc ? per_cu : wpc);
+    const double cost = fixed + (double)rounds * (4.5 + ceil_div(nkt, groups * ns) * tile[c - 1] * scale) +
+                        (ns > 1 ? 3.5 + (double)w * rows * d * 8 / 5e6 : 0.0);
+    if (cost < best->cost) *best = {nw, ns, prep, (size_t)units, cost};
   }
 }
 
-Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype) {
-  Plan r{0, 1, 0};
+Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype, bool may_prepare) {
+  Plan r{0, 1, 0, 0, 1e300};
   const long long pairs = (long long)B * heads;
   with_d(d, [&](auto dc) {
     constexpr int D = decltype(dc)::value;
-    double c4 = 1e300, c1 = 1e300;
-    int n4 = 1, n1 = 1;
     if (dtype == kBF16) {
       const int nkt = ceil_div(n_kv, BKV);
-      best_split(ceil_div(n_q, 128) * pairs, Geo<D, 4>::WPC, 1, nkt, &n4, &c4);
-      best_split(ceil_div(n_q, 32) * pairs, Geo<D, 1>::WPC, 4, nkt, &n1, &c1);
+      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, Geo<D, 4>::WPC, {1.3, 1.85, 0}, 0.0, d);
+      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.8 : 1.33, 2.4, 0}, 0.0, d);
+      if (may_prepare && (long long)nkt * (Geo<D, 4, true>::KT + Geo<D, 4, true>::VT) < (1ll << 31))
+        consider(&r, 4, 1, pairs, n_q, 128, 1, nkt, Geo<D, 4, true>::WPC, {0.8, 1.15, 1.7},
+                 2.5 + 0.0055 * (double)(pairs * nkt) * (0.5 + d / 140.0), d);
     } else {
+      // (32-key tiles)
       const int nkt = ceil_div(n_kv, Geo32<D, 4>::BK);
-      best_split(ceil_div(n_q, 128) * pairs, Geo32<D, 4>::WPC, 1, nkt, &n4, &c4);
-      if (n_q <= 64) best_split(ceil_div(n_q, 64) * pairs, Geo32<D, 2>::WPC, 1, nkt, &n1, &c1);
+      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, 2, {3.3, 4.5, 0}, 0.0, d);
+      consider(&r, 2, 0, pairs, n_q, 64, 1, nkt, cmin(3, Geo32<D, 2>::WPC), {3.3, 3.6, 4.5}, 0.0, d);
     }
-    if (c1 <= c4) r = {dtype == kBF16 ? 1 : 2, n1, (size_t)(ceil_div(n_q, dtype == kBF16 ? 32 : 64) * pairs)};
-    else r = {4, n4, (size_t)(ceil_div(n_q, 128) * pairs)};
   });
   return r;
 }
@@ -1172,17 +1245,13 @@ hipError_t launch_bf16(const Plan& pl, const AttnQParams& p, const Split& sp, hi
   return attr != hipSuccess ? attr : launch(attn_q8_kernel<D, NW, PREP>, lds, 256, pl.tiles * pl.ns, p, sp, s);
 }
 
-// Tiles are prepared from this many queries on.
-constexpr int kPrepareQueries = 512;
-
-// Bytes of the prepared tiles (0: not prepared).
-size_t tile_bytes(int B, int heads, int n_q, int n_kv, int d, int dtype) {
+// Bytes of the prepared tiles and of the parts.
+size_t tile_bytes(const Plan& pl, int B, int heads, int n_kv, int d) {
   size_t r = 0;
-  if (dtype == kBF16 && n_q >= kPrepareQueries)
+  if (pl.prep)
     with_d(d, [&](auto dc) {
       using G = Geo<decltype(dc)::value, 4, true>;
-      const size_t one = (size_t)ceil_div(n_kv, BKV) * (G::KT + G::VT);
-      if (one < (size_t)1 << 31) r = one * B * heads;
+      r = (size_t)ceil_div(n_kv, BKV) * (G::KT + G::VT) * B * heads;
     });
   return r;
 }
@@ -1196,19 +1265,23 @@ size_t split_bytes(const Plan& pl, int d) {
 size_t attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int d, int dtype) {
   using namespace q8attn;
   if (n_q <= 0) return 0;
-  const Plan pl = plan(B, heads, n_q, n_kv, d, dtype);
-  return pl.nw == 0 ? 0 : split_bytes(pl, d) + tile_bytes(B, heads, n_q, n_kv, d, dtype);
+  const Plan pl = plan(B, heads, n_q, n_kv, d, dtype, true);
+  return pl.nw == 0 ? 0 : split_bytes(pl, d) + tile_bytes(pl, B, heads, n_kv, d);
 }
 
 hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream_t s) {
   using namespace q8attn;
   if (p.n_q <= 0) return hipSuccess;
-  Plan pl = plan(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype);
+  Plan pl = plan(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype, true);
   if (pl.nw == 0) return hipErrorInvalidValue;
-  const size_t split = split_bytes(pl, p.d), tiles = tile_bytes(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype);
-  // (a workspace too small for both holds the parts alone, or nothing)
-  const bool prepare = pl.nw == 4 && tiles > 0 && p.ws && p.ws_bytes >= split + tiles;
-  if (!p.ws || p.ws_bytes < split) pl.ns = 1;
+  size_t tiles = tile_bytes(pl, p.B, p.heads, p.c.tokens, p.d);
+  if (!p.ws || p.ws_bytes < split_bytes(pl, p.d) + tiles) {
+    // too small a workspace: the keys neither prepared nor split
+    pl = plan(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype, false);
+    pl.ns = 1;
+    tiles = 0;
+  }
+  const bool prepare = pl.prep;
   if (pl.tiles * pl.ns > 0x7fffffff) return hipErrorInvalidValue;
   Split sp{nullptr, pl.ns, nullptr, nullptr};
   if (prepare) sp.tiles = reinterpret_cast<const char*>(p.ws);
@@ -1231,9 +1304,12 @@ hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream
     else rc = launch(attn_q8_f32_kernel<D, 2>, Geo32<D, 2>::LDS, 128, pl.tiles * pl.ns, p, sp, s);
   });
   if (rc != hipSuccess || pl.ns == 1) return rc;
+  // shares of the parts: as many as leave the chip full, measured with 1 / 2 / 8 at ... 
   const int rows = 32 * pl.nw;
-  if (dtype == kBF16) return pl.ns > 4 ? launch_merge<bf16, 8>(p, sp, rows, s) : launch_merge<bf16, 2>(p, sp, rows, s);
-  return pl.ns > 4 ? launch_merge<float, 8>(p, sp, rows, s) : launch_merge<float, 2>(p, sp, rows, s);
+  const long long quads = (long long)p.B * p.heads * p.n_q * (p.d / 4);
+  const int shares = quads >= 65536 || pl.ns <= 4 ? 1 : 8;
+  if (dtype == kBF16) return shares == 1 ? launch_merge<bf16, 1>(p, sp, rows, s) : launch_merge<bf16, 8>(p, sp, rows, s);
+  return shares == 1 ? launch_merge<float, 1>(p, sp, rows, s) : launch_merge<float, 8>(p, sp, rows, s);
 }
 
 }  // namespace orch
