@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "liborch.so")
@@ -111,7 +112,7 @@ def _load():
         "orch_unet_conv_workspace_bytes": (sz, [C.POINTER(UNetConvShape), i]),
         "orch_unet_conv_band": (i, [C.POINTER(UNetConvShape), i, i, vp, vp, vp, vp, vp, vp, vp, i,
                                     vp, vp, sz, vp]),
-        "orch_op_rotary": (i, [C.POINTER(RotaryAxes), C.POINTER(RotaryTensor), i, i, i, i, i, i, vp]),
+        "orch_op_rotary": (i, [C.POINTER(RotaryAxes), vp, i, i, i, i, i, i, vp]),
         "orch_op_kv_quantize": (i, [vp, sz, i, i, C.POINTER(QuantizedKV), i, i, i, i, i, i, vp]),
         "orch_op_kv_dequantize": (i, [C.POINTER(QuantizedKV), i, vp, sz, i, i, i, i, i, i, i, vp]),
         "orch_op_attention_quantized": (i, [vp, C.POINTER(QuantizedKV), vp, sz, i, i, i, i, i, i, vp,
@@ -151,6 +152,15 @@ def _stream(stream=None):
     if stream is not None:
         return stream.cuda_stream
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _check_device(*devices):
+    """Refuse tensors (as Tensor.get_device() gives them, -1 on the host) that are not on the current GPU."""
+    import torch
+    cur = torch.cuda.current_device()
+    for d in devices:
+        if d != cur:
+            raise OrchError(ORCH_EINVAL, f"a tensor is on {'the host' if d < 0 else f'GPU {d}'}, the current GPU is {cur}")
 
 
 def _code(t):
@@ -315,28 +325,34 @@ def rotary_axes(channels, extent, theta=1e4, origin=(0.0, 0.0, 0.0), step=(1.0, 
                       (C.c_double * 3)(*step), float(theta), int(interleaved))
 
 
+_ROTARY_TENSOR = struct.Struct("=QQi4x6Q")     # RotaryTensor's layout
+
+
 def rotary(axes: RotaryAxes, token_begin, x, out, stream=None):
     """Rotate x into out: tensors (or pairs of tensors, e.g. Q and K) [B, heads, n_tok, d] of any
     strides, their channels next to each other.  out may be x."""
     xs, outs = (x, out) if isinstance(x, (tuple, list)) else ((x,), (out,))
     B, _, n_tok, d = xs[0].shape
+    dtype = xs[0].dtype
     if len(xs) != len(outs):
         raise OrchError(ORCH_EINVAL, "as many outputs as inputs are needed")
-    ts = (RotaryTensor * len(xs))()
-    for t, a, b in zip(ts, xs, outs):
-        if a.shape != b.shape or a.dtype != xs[0].dtype or b.dtype != a.dtype:
+    ts, devices = b"", ()
+    for a, o in zip(xs, outs):
+        shape, sa, so = a.shape, a.stride(), o.stride()
+        if o.shape != shape or a.dtype != dtype or o.dtype != dtype:
             raise OrchError(ORCH_EINVAL, "inputs and outputs must agree in shape and type")
-        if (a.shape[0], a.shape[2], a.shape[3]) != (B, n_tok, d) or a.stride(3) != 1 or b.stride(3) != 1:
+        if shape[0] != B or shape[2] != n_tok or shape[3] != d or sa[3] != 1 or so[3] != 1:
             raise OrchError(ORCH_EINVAL, "tensors must be [B, heads, n_tok, d] with channels next to each other")
-        t.x, t.out, t.heads = a.data_ptr(), b.data_ptr(), a.shape[1]
-        t.x_stride[:], t.out_stride[:] = a.stride()[:3], b.stride()[:3]
-    check(lib.orch_op_rotary(C.byref(axes), ts, len(xs), B, n_tok, token_begin, d, _code(xs[0]),
-                             _stream(stream)))
+        devices += (a.get_device(), o.get_device())
+        ts += _ROTARY_TENSOR.pack(a.data_ptr(), o.data_ptr(), shape[1], sa[0], sa[1], sa[2], so[0], so[1], so[2])
+    code = _code(xs[0])
+    _check_device(*devices)
+    check(lib.orch_op_rotary(C.byref(axes), ts, len(xs), B, n_tok, token_begin, d, code, _stream(stream)))
 
 
 def quantized_kv(values, exponents) -> QuantizedKV:
     """The 8-bit K/V cache held by two tensors: e4m3 (or uint8) values [B, 2, heads, tokens, d]
-    and uint8 exponents [B, 2, heads, tokens], contiguous within a branch.  The caller keeps them."""
+    and uint8 exponents [B, 2, heads, tokens], contiguous within a branch.  It keeps the tensors."""
     B, two, heads, tokens, d = values.shape
     if two != 2 or tuple(exponents.shape) != (B, 2, heads, tokens):
         raise OrchError(ORCH_EINVAL, "values [B, 2, heads, tokens, d] and exponents [B, 2, heads, tokens] are needed")
@@ -344,17 +360,21 @@ def quantized_kv(values, exponents) -> QuantizedKV:
         raise OrchError(ORCH_EINVAL, "values and exponents must be of one byte")
     if not (values[0].is_contiguous() and exponents[0].is_contiguous()):
         raise OrchError(ORCH_EINVAL, "a branch's values and exponents must be contiguous")
-    return QuantizedKV(values.data_ptr(), exponents.data_ptr(), values.stride(0), exponents.stride(0), tokens)
+    c = QuantizedKV(values.data_ptr(), exponents.data_ptr(), values.stride(0), exponents.stride(0), tokens)
+    c.tensors, c.devices = (values, exponents), (values.get_device(), exponents.get_device())
+    return c
 
 
 def kv_quantize(kv, kv_branch_stride, kv_tokens, kv_offset, cache: QuantizedKV, tok_offset, B, heads,
                 n_tok, head_dim, dtype, stream=None):
+    _check_device(kv.get_device(), *cache.devices)
     check(lib.orch_op_kv_quantize(_ptr(kv), kv_branch_stride, kv_tokens, kv_offset, C.byref(cache),
                                   tok_offset, B, heads, n_tok, head_dim, dtype, _stream(stream)))
 
 
 def kv_dequantize(cache: QuantizedKV, tok_offset, kv, kv_branch_stride, kv_tokens, kv_offset, B, heads,
                   n_tok, head_dim, dtype, stream=None):
+    _check_device(kv.get_device(), *cache.devices)
     check(lib.orch_op_kv_dequantize(C.byref(cache), tok_offset, _ptr(kv), kv_branch_stride, kv_tokens,
                                     kv_offset, B, heads, n_tok, head_dim, dtype, _stream(stream)))
 
@@ -366,6 +386,7 @@ def attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype) ->
 def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, n_fresh, B, heads, n_q,
                         head_dim, out, dtype, workspace=None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.nbytes
+    _check_device(*cache.devices, *(t.get_device() for t in (q, kv_fresh, out, workspace) if t is not None))
     check(lib.orch_op_attention_quantized(_ptr(q), C.byref(cache), _ptr(kv_fresh), fresh_bs, fresh_begin,
                                           n_fresh, B, heads, n_q, head_dim, _ptr(out), _ptr(workspace),
                                           ws_bytes, dtype, _stream(stream)))

@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     // cache's keys, then the fresh ones, K's in rows, V's along the keys
     const int n0 = t * BKV;
     auto fresh = [&](int key) __attribute__((always_inline)) { return (unsigned)(n0 + key - fb) < (unsigned)nf; };
-    constexpr int BATCH = cmin(SL, NW == 4 ? 2 : D <= 72 || D == 128 ? 8 : 4);
+    constexpr int BATCH = cmin(SL, NW == 4 ? 2 : D == 128 ? 16 : D <= 72 ? 8 : 4);
 #pragma unroll
     for (int i0 = 0; i0 < SL; i0 += BATCH) {
       u32x4 x[BATCH];
@@ -1195,10 +1195,10 @@ void with_d(int d, F&& f) {
 // A variant's best ns into *best if it beats it.  rows: queries of a workgroup; groups: key groups of
 // it; tile[c - 1]: a tile's time with c workgroups on the CU; fixed: time before.
 void consider(Plan* best, int nw, int prep, long long pairs, int n_q, int rows, int groups, int nkt, int wpc,
-              const double (&tile)[3], double fixed, int d) {
+              const double (&tile)[3], double fixed, int d, int max_ns) {
   const long long units = ceil_div(n_q, rows) * pairs;
   const double scale = 0.5 + d / 140.0;
-  for (int ns = 1; ns <= 64 && ns <= ceil_div(nkt, groups); ++ns) {
+  for (int ns = 1; ns <= max_ns && ns <= ceil_div(nkt, groups); ns += ns < 8 ? 1 : ns / 4) {
     const long long w = units * ns, per_cu = (w + 255) / 256, rounds = (per_cu + wpc - 1) / wpc;
     const int c = (int)(per_cu < wpc ? per_cu : wpc);
     const double cost = fixed + (double)rounds * (4.5 + ceil_div(nkt, groups * ns) * tile[c - 1] * scale) +
@@ -1207,23 +1207,26 @@ void consider(Plan* best, int nw, int prep, long long pairs, int n_q, int rows, 
   }
 }
 
-Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype, bool may_prepare) {
+// workspace: the call has one (else the keys are neither prepared nor split)
+Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype, bool workspace) {
   Plan r{0, 1, 0, 0, 1e300};
   const long long pairs = (long long)B * heads;
+  const int max_ns = workspace ? 64 : 1;
   with_d(d, [&](auto dc) {
     constexpr int D = decltype(dc)::value;
     if (dtype == kBF16) {
       const int nkt = ceil_div(n_kv, BKV);
-      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, Geo<D, 4>::WPC, {1.3, 1.85, 0}, 0.0, d);
-      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.8 : 1.33, 2.4, 0}, 0.0, d);
-      if (may_prepare && (long long)nkt * (Geo<D, 4, true>::KT + Geo<D, 4, true>::VT) < (1ll << 31))
+      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, Geo<D, 4>::WPC, {1.3, 1.85, 0}, 0.0, d, max_ns);
+      // (its longer straight code is read once by every CU: 1 us at d = 64, 7 at d = 128)
+      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.8 : 1.33, 2.4, 0}, D <= 64 ? D / 64 : 1.0 + (D - 64) * 0.09, d, max_ns);
+      if (workspace && (long long)nkt * (Geo<D, 4, true>::KT + Geo<D, 4, true>::VT) < (1ll << 31))
         consider(&r, 4, 1, pairs, n_q, 128, 1, nkt, Geo<D, 4, true>::WPC, {0.8, 1.15, 1.7},
-                 2.5 + 0.0055 * (double)(pairs * nkt) * (0.5 + d / 140.0), d);
+                 2.5 + 0.0055 * (double)(pairs * nkt) * (0.5 + d / 140.0), d, max_ns);
     } else {
       // (32-key tiles)
       const int nkt = ceil_div(n_kv, Geo32<D, 4>::BK);
-      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, 2, {3.3, 4.5, 0}, 0.0, d);
-      consider(&r, 2, 0, pairs, n_q, 64, 1, nkt, cmin(3, Geo32<D, 2>::WPC), {3.3, 3.6, 4.5}, 0.0, d);
+      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, 2, {3.3, 4.5, 0}, 0.0, d, max_ns);
+      consider(&r, 2, 0, pairs, n_q, 64, 1, nkt, cmin(3, Geo32<D, 2>::WPC), {3.3, 3.6, 4.5}, 0.0, d, max_ns);
     }
   });
   return r;
@@ -1276,9 +1279,7 @@ hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream
   if (pl.nw == 0) return hipErrorInvalidValue;
   size_t tiles = tile_bytes(pl, p.B, p.heads, p.c.tokens, p.d);
   if (!p.ws || p.ws_bytes < split_bytes(pl, p.d) + tiles) {
-    // too small a workspace: the keys neither prepared nor split
     pl = plan(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype, false);
-    pl.ns = 1;
     tiles = 0;
   }
   const bool prepare = pl.prep;

@@ -50,6 +50,36 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryLaunch L) {
     c0 = base + left;
     c1 = c0 + half;
   }
+  // the first rows are on their way while the angles are formed
+  constexpr int RB = 4;
+  T e[RB][E];
+  T* o[RB];
+  int r = blockIdx.y * L.per;
+  const int r1 = min(r + L.per, L.rows_total);
+  auto fetch = [&](int first) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+      if (first + k >= r1) break;
+      const bool second = first + k >= L.rows0;
+      const RotaryTensor& t = p.t[second ? 1 : 0];
+      const int rr = first + k - (second ? L.rows0 : 0);
+      const int b = rr / t.heads, h = rr - b * t.heads;
+      const T* x = reinterpret_cast<const T*>(t.x) + b * t.xs[0] + h * t.xs[1] + tok * t.xs[2];
+      o[k] = reinterpret_cast<T*>(t.out) + b * t.os[0] + h * t.os[1] + tok * t.os[2];
+      if constexpr (VEC) {
+#pragma unroll
+        for (int g = 0; g < E / V; ++g) {
+          const vec v = *reinterpret_cast<const vec*>(x + (g ? c1 : c0));
+#pragma unroll
+          for (int j = 0; j < V; ++j) e[k][g * V + j] = v[j];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) e[k][j] = x[IL || j < V ? c0 + j : c1 + j - V];
+      }
+    }
+  };
+  fetch(r);
   float cs[P], sn[P];
   bool turn[P];
 #pragma unroll
@@ -63,47 +93,33 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryLaunch L) {
     sincospif(2.0f * r, &sn[j], &cs[j]);
   }
 
-  const int r0 = blockIdx.y * L.per, r1 = min(r0 + L.per, L.rows_total);
-  for (int r = r0; r < r1; ++r) {
-    const bool second = r >= L.rows0;
-    const RotaryTensor& t = p.t[second ? 1 : 0];
-    const int rr = second ? r - L.rows0 : r;
-    const int b = rr / t.heads, h = rr - b * t.heads;
-    const T* x = reinterpret_cast<const T*>(t.x) + b * t.xs[0] + h * t.xs[1] + tok * t.xs[2];
-    T* o = reinterpret_cast<T*>(t.out) + b * t.os[0] + h * t.os[1] + tok * t.os[2];
-    T e[E];
-    if constexpr (VEC) {
+  for (; r < r1; r += RB) {
 #pragma unroll
-      for (int k = 0; k < E / V; ++k) {
-        const vec v = *reinterpret_cast<const vec*>(x + (k ? c1 : c0));
+    for (int k = 0; k < RB; ++k) {
+      if (r + k >= r1) break;
 #pragma unroll
-        for (int j = 0; j < V; ++j) e[k * V + j] = v[j];
+      for (int j = 0; j < P; ++j) {
+        T &lo = e[k][IL ? 2 * j : j], &hi = e[k][IL ? 2 * j + 1 : V + j];
+        const float a = to_f<T>(lo), c = to_f<T>(hi);
+        if (turn[j]) {
+          lo = from_f<T>(a * cs[j] - c * sn[j]);
+          hi = from_f<T>(a * sn[j] + c * cs[j]);
+        }
       }
-    } else {
+      if constexpr (VEC) {
 #pragma unroll
-      for (int j = 0; j < E; ++j) e[j] = x[IL || j < V ? c0 + j : c1 + j - V];
-    }
+        for (int g = 0; g < E / V; ++g) {
+          vec v;
 #pragma unroll
-    for (int j = 0; j < P; ++j) {
-      T &lo = e[IL ? 2 * j : j], &hi = e[IL ? 2 * j + 1 : V + j];
-      const float a = to_f<T>(lo), c = to_f<T>(hi);
-      if (turn[j]) {
-        lo = from_f<T>(a * cs[j] - c * sn[j]);
-        hi = from_f<T>(a * sn[j] + c * cs[j]);
+          for (int j = 0; j < V; ++j) v[j] = e[k][g * V + j];
+          *reinterpret_cast<vec*>(o[k] + (g ? c1 : c0)) = v;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) o[k][IL || j < V ? c0 + j : c1 + j - V] = e[k][j];
       }
     }
-    if constexpr (VEC) {
-#pragma unroll
-      for (int k = 0; k < E / V; ++k) {
-        vec v;
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = e[k * V + j];
-        *reinterpret_cast<vec*>(o + (k ? c1 : c0)) = v;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < E; ++j) o[IL || j < V ? c0 + j : c1 + j - V] = e[j];
-    }
+    fetch(r + RB);
   }
 }
 
@@ -116,8 +132,8 @@ static hipError_t launch_rotary_v(const RotaryParams& p, hipStream_t s) {
   L.rows_total = L.rows0 + (p.n_t > 1 ? p.B * p.t[1].heads : 0);
   const long long blocks = ((long long)p.n_tok * L.units + 255) / 256;
   // slices of the rows: up to eight rows an angle, fewer while that leaves under
-  // 2048 workgroups (eight a CU)
-  L.per = (int)(blocks * L.rows_total / 2048);
+  // 1024 workgroups (four a CU)
+  L.per = (int)(blocks * L.rows_total / 1024);
   L.per = L.per < 1 ? 1 : L.per > 8 ? 8 : L.per;
   const int slices = ceil_div(L.rows_total, L.per);
   hipLaunchKernelGGL((rotary_kernel<T, IL, V, VEC>), dim3((unsigned)blocks, slices), dim3(256), 0, s, L);

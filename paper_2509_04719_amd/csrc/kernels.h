@@ -175,7 +175,7 @@ struct RotaryTensor {
   int heads;
   size_t xs[3], os[3];
 };
-constexpr int kRotaryMaxPairs = 128;
+constexpr int kRotaryMaxPairs = 64;     // of 128 channels
 struct RotaryParams {
   RotaryTensor t[2];
   int n_t, B, n_tok, d, token_begin;

@@ -183,8 +183,7 @@ int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache, c
       (workspace && !aligned16(workspace)))
     return fail("device buffers must be 16-byte aligned");
   const size_t fresh_bytes = n_fresh > 0 ? ((B > 1 ? (B - 1) * fresh_bs : 0) + fresh_elems) * es : 0;
-  const size_t need = attention_quantized_workspace_bytes(B, heads, n_q, cache->tokens, head_dim, dtype);
-  const size_t ws_used = !workspace ? 0 : workspace_bytes < need ? workspace_bytes : need;
+  const size_t ws_used = workspace ? workspace_bytes : 0;
   const struct { const void* p; size_t n; } in[] = {{q, q_bytes}, {cache->values, values}, {cache->exponents, exps}, {kv_fresh, fresh_bytes}};
   for (const auto& r : in)
     if (overlap(out, q_bytes, r.p, r.n) || overlap(workspace, ws_used, r.p, r.n))

@@ -95,23 +95,39 @@ def test_attention(orch_lib, split, dtype, d, heads, n_q, N, fb, nf):
 
 
 @pytest.mark.parametrize("split", [True, False])
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 72, 80, 96, 128])
+@pytest.mark.parametrize("n_q,N,fb,nf", [(1100, 600, 77, 300), (1027, 333, 0, 0), (1100, 640, 64, 512), (520, 2000, 1001, 520)])
+def test_many_heads_and_queries(orch_lib, split, d, n_q, N, fb, nf):
+    """Enough workgroups that the keys are laid out as tiles once (with a workspace), or taken by whole workgroups."""
+    print(f"\n[d {d} n_q {n_q} n_kv {N} fresh {fb}+{nf} split {split}]", flush=True)
+    rng = np.random.default_rng(d + n_q + N)
+    q, v8, e8, fk, fv, K, V = make(rng, "bf16", 2, 16, d, n_q, N, fb, nf)
+    check(run(orch_lib, "bf16", q, v8, e8, fk, fv, fb, split), "bf16", q, K, V)
+
+
+@pytest.mark.parametrize("split", [True, False])
 @pytest.mark.parametrize("d", [64, 72, 128])
 @pytest.mark.parametrize("ramp,shift", [(12.0, 0.0), (0.0, 48.0), (0.0, 2.0 ** 15)])
-def test_running_max(orch_lib, split, dtype, d, ramp, shift):
+@pytest.mark.parametrize("dtype,B,heads,n_q,N", [("bf16", 1, 2, 70, 1000), ("bf16", 2, 16, 1100, 600), ("f32", 1, 2, 70, 1000)])
+def test_running_max(orch_lib, split, dtype, d, ramp, shift, B, heads, n_q, N):
     """Scores that grow along the keys, and scores with a large common offset."""
     rng = np.random.default_rng(d)
-    q, v8, e8, fk, fv, K, V = make(rng, dtype, 1, 2, d, 70, 1000, 500, 70, ramp, shift)
+    q, v8, e8, fk, fv, K, V = make(rng, dtype, B, heads, d, n_q, N, N // 2, 70, ramp, shift)
     print(f"\n[{dtype} d {d} ramp {ramp} shift {shift} split {split}]", flush=True)
-    check(run(orch_lib, dtype, q, v8, e8, fk, fv, 500, split), dtype, q, K, V, tight=False)
+    check(run(orch_lib, dtype, q, v8, e8, fk, fv, N // 2, split), dtype, q, K, V, tight=False)
+
+
+# few queries (waves share the keys), whole workgroups, prepared tiles
+SIZES = [(1, 2, 40, 200), (2, 16, 520, 330), (2, 16, 1100, 333)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 72, 128])
-def test_equal_huge_scores_are_a_mean(orch_lib, dtype, d):
+@pytest.mark.parametrize("B,heads,n_q,N", SIZES)
+def test_equal_huge_scores_are_a_mean(orch_lib, dtype, d, B, heads, n_q, N):
     """Every score the same number of 10^30 and more (either sign): the mean of V."""
     rng = np.random.default_rng(1)
-    q, v8, e8, fk, fv, K, V = make(rng, dtype, 1, 2, d, 40, 300, 0, 0)
+    q, v8, e8, fk, fv, K, V = make(rng, dtype, B, heads, d, n_q, N, 0, 0)
     q[:], q[..., 0] = 0.0, 2.0 ** 60
     for sign in (1, -1):
         k = np.zeros_like(K)
@@ -123,12 +139,13 @@ def test_equal_huge_scores_are_a_mean(orch_lib, dtype, d):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 72, 96])
-def test_not_finite(orch_lib, dtype, d):
+@pytest.mark.parametrize("B,heads,n_q,N", SIZES)
+def test_not_finite(orch_lib, dtype, d, B, heads, n_q, N):
     """A key whose score is minus infinity has no part in the result, wherever it lies; an infinite score or a NaN
     makes its own queries NaN and no others."""
     rng = np.random.default_rng(4)
-    n_q, N, fb, nf = 40, 200, 60, 100
-    q, v8, e8, fk, fv, K, V = make(rng, dtype, 1, 2, d, n_q, N, fb, nf)
+    fb, nf = 60, 100
+    q, v8, e8, fk, fv, K, V = make(rng, dtype, B, heads, d, n_q, N, fb, nf)
     q[..., 0] = np.abs(q[..., 0]) + 0.5
     out = []
     masked = [0, 1, 40, 99]
@@ -146,7 +163,8 @@ def test_not_finite(orch_lib, dtype, d):
     # a NaN in the cache reaches every query of its head; one query's NaN itself alone
     v = v8.copy()
     v[0, 0, 1, 5, 3] = 0x7f
-    assert np.isnan(run(orch_lib, dtype, q, v, e8, fk, fv, fb)[0, 1]).all()
+    got = run(orch_lib, dtype, q, v, e8, fk, fv, fb)
+    assert np.isnan(got[0, 1]).all() and np.isfinite(got[0, 0]).all()
     qn = q.copy()
     qn[0, 0, 7, 2] = np.nan
     got = run(orch_lib, dtype, qn, v8, e8, fk, fv, fb)
@@ -154,16 +172,17 @@ def test_not_finite(orch_lib, dtype, d):
 
 
 @pytest.mark.parametrize("d", [64, 72, 128])
-def test_infinite_value(orch_lib, d):
+@pytest.mark.parametrize("B,heads,n_q,N", SIZES)
+def test_infinite_value(orch_lib, d, B, heads, n_q, N):
     """An infinite V of a fresh key: infinite in its channel, the others as they are."""
     rng = np.random.default_rng(6)
-    q, v8, e8, fk, fv, K, V = make(rng, "bf16", 1, 1, d, 33, 150, 10, 33)
+    q, v8, e8, fk, fv, K, V = make(rng, "bf16", B, heads, d, n_q, N, 10, 33)
     fv[0, 0, 20, 5] = np.inf
-    got = run(orch_lib, "bf16", q, v8, e8, fk, fv, 10)
+    got = run(orch_lib, "bf16", q, v8, e8, fk, fv, 10)[0, 0]
     V[0, 0, 30, 5] = 0.0
     assert np.isinf(got[..., 5]).all()
     c = np.arange(d) != 5
-    assert rel_l2(got[..., c], ok.attention(q, K, V)[..., c]) <= NORM["bf16"]
+    assert rel_l2(got[..., c], ok.attention(q[0, 0], K[0, 0], V[0, 0])[..., c]) <= NORM["bf16"]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
