@@ -154,13 +154,15 @@ def _stream(stream=None):
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
-def _check_device(*devices):
-    """Refuse tensors (as Tensor.get_device() gives them, -1 on the host) that are not on the current GPU."""
+def _stream_on(stream, *devices):
+    """The stream's handle, for tensors (their Tensor.get_device(), -1 on the host) that all have to
+    be on the current GPU."""
     import torch
     cur = torch.cuda.current_device()
     for d in devices:
         if d != cur:
             raise OrchError(ORCH_EINVAL, f"a tensor is on {'the host' if d < 0 else f'GPU {d}'}, the current GPU is {cur}")
+    return torch._C._cuda_getCurrentRawStream(cur) if stream is None else stream.cuda_stream
 
 
 def _code(t):
@@ -346,8 +348,8 @@ def rotary(axes: RotaryAxes, token_begin, x, out, stream=None):
         devices += (a.get_device(), o.get_device())
         ts += _ROTARY_TENSOR.pack(a.data_ptr(), o.data_ptr(), shape[1], sa[0], sa[1], sa[2], so[0], so[1], so[2])
     code = _code(xs[0])
-    _check_device(*devices)
-    check(lib.orch_op_rotary(C.byref(axes), ts, len(xs), B, n_tok, token_begin, d, code, _stream(stream)))
+    check(lib.orch_op_rotary(C.byref(axes), ts, len(xs), B, n_tok, token_begin, d, code,
+                             _stream_on(stream, *devices)))
 
 
 def quantized_kv(values, exponents) -> QuantizedKV:
@@ -367,16 +369,16 @@ def quantized_kv(values, exponents) -> QuantizedKV:
 
 def kv_quantize(kv, kv_branch_stride, kv_tokens, kv_offset, cache: QuantizedKV, tok_offset, B, heads,
                 n_tok, head_dim, dtype, stream=None):
-    _check_device(kv.get_device(), *cache.devices)
-    check(lib.orch_op_kv_quantize(_ptr(kv), kv_branch_stride, kv_tokens, kv_offset, C.byref(cache),
-                                  tok_offset, B, heads, n_tok, head_dim, dtype, _stream(stream)))
+    st = _stream_on(stream, kv.get_device(), *cache.devices)
+    check(lib.orch_op_kv_quantize(kv.data_ptr(), kv_branch_stride, kv_tokens, kv_offset, C.byref(cache),
+                                  tok_offset, B, heads, n_tok, head_dim, dtype, st))
 
 
 def kv_dequantize(cache: QuantizedKV, tok_offset, kv, kv_branch_stride, kv_tokens, kv_offset, B, heads,
                   n_tok, head_dim, dtype, stream=None):
-    _check_device(kv.get_device(), *cache.devices)
-    check(lib.orch_op_kv_dequantize(C.byref(cache), tok_offset, _ptr(kv), kv_branch_stride, kv_tokens,
-                                    kv_offset, B, heads, n_tok, head_dim, dtype, _stream(stream)))
+    st = _stream_on(stream, kv.get_device(), *cache.devices)
+    check(lib.orch_op_kv_dequantize(C.byref(cache), tok_offset, kv.data_ptr(), kv_branch_stride, kv_tokens,
+                                    kv_offset, B, heads, n_tok, head_dim, dtype, st))
 
 
 def attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype) -> int:
@@ -386,10 +388,10 @@ def attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype) ->
 def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, n_fresh, B, heads, n_q,
                         head_dim, out, dtype, workspace=None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.nbytes
-    _check_device(*cache.devices, *(t.get_device() for t in (q, kv_fresh, out, workspace) if t is not None))
+    st = _stream_on(stream, *cache.devices, *[t.get_device() for t in (q, kv_fresh, out, workspace) if t is not None])
     check(lib.orch_op_attention_quantized(_ptr(q), C.byref(cache), _ptr(kv_fresh), fresh_bs, fresh_begin,
                                           n_fresh, B, heads, n_q, head_dim, _ptr(out), _ptr(workspace),
-                                          ws_bytes, dtype, _stream(stream)))
+                                          ws_bytes, dtype, st))
 
 
 def unet_shape(cfg, eps: float = 1e-5) -> UNetConvShape:

@@ -727,6 +727,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     const bool vt1 = ty1 == kFresh;
     mask(t, 0, s0);
     step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
+    tiles_sync();      // V of the last tile came since the last one
     if constexpr (G::ST == 1) store(kV, vr, t, ty1);
     mask(t, 1, s1);
     step(std::false_type{}, false, s1, 0, 0, s0, t, 0, vt1, pb, pa);
@@ -915,37 +916,48 @@ __global__ __launch_bounds__(256) void attn_q8_prepare_kernel(AttnQParams p, cha
 // fp32: v_mfma_f32_32x32x2_f32, 32 keys a tile.  Its two k are channels 8 g + e and 8 g + 4 + e of the
 // scores, and keys 8 g + e and 8 g + 4 + e of the PV product, which score register 4 g + e holds in the two
 // lane halves: the probabilities need no movement, and V is read token-major, 32 channels of a key by 32 lanes.
-template <int D, int NW>
+// The MFMAs of a tile (64 cycles each) outweigh everything else, so every wave works alone: the KG
+// waves of a workgroup have the same 32 queries and each a share of the keys; their parts meet in LDS.
+template <int D>
 struct Geo32 {
-  static constexpr int BK = 32, NG = D / 8, DT = (D + 31) / 32, CPT = D / 8, THREADS = 64 * NW;
+  static constexpr int BK = 32, NG = D / 8, DT = (D + 31) / 32, CPT = D / 8;
+  static constexpr int KG = D <= 64 ? 8 : 4;
   static constexpr int KP = 4 * D + 16;          // bytes of a K row: an odd number of 16-byte chunks
   static constexpr int VP = 128 * DT + 32;       // of a V row: four rows apart are the other 32 banks
-  static constexpr int LDS = BK * (KP + VP);
-  static constexpr int SL = (BK * CPT + THREADS - 1) / THREADS;
-  static constexpr int WPC = cmin(8 / NW, 160 * 1024 / LDS);
+  static constexpr int TILE = BK * (KP + VP), LDS = KG * TILE;
+  static constexpr int SL = (BK * CPT + 63) / 64;
+  static constexpr int WPC = cmin(2, 160 * 1024 / LDS);
+  static_assert((DT * 16 + 2) * 256 <= TILE, "a group's part fits its tile's place");
+  // us of a tile in a wave: 64 cycles an MFMA, 1500 for the rest
+  static constexpr double tile_us = (32.0 * D + 1024.0 * DT + 1500.0) / 2400.0;
 };
 
-template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attn_q8_f32_kernel(AttnQParams p, Split sp) {
+template <int D>
+__global__ __launch_bounds__(64 * Geo32<D>::KG, Geo32<D>::KG / 4) void attn_q8_f32_kernel(AttnQParams p, Split sp) {
+#if defined(__HIP_DEVICE_COMPILE__)
 #pragma clang fp contract(off)
-  using G = Geo32<D, NW>;
-  constexpr int SL = G::SL, CPT = G::CPT, TH = G::THREADS, BK = G::BK, DT = G::DT;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  char* sk = smem;
-  char* sv = smem + BK * G::KP;
-  const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, h = lane >> 5, wave = tid >> 6;
-  const int n_qt = (p.n_q + 32 * NW - 1) / (32 * NW);
-  const int unit = blockIdx.x / sp.ns, part = blockIdx.x - unit * sp.ns;
-  const int pair = unit / n_qt, q0 = (unit - pair * n_qt) * 32 * NW + 32 * wave;
+  using G = Geo32<D>;
+  constexpr int SL = G::SL, CPT = G::CPT, BK = G::BK, DT = G::DT, KG = G::KG;
+  extern __shared__ __attribute__((aligned(1024))) char smem_all[];
+  const int lane = threadIdx.x & 63, lc = lane & 31, h = lane >> 5;
+  const int kg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  char* sk = smem_all + kg * G::TILE;
+  char* sv = sk + BK * G::KP;
+  const int n_qt = (p.n_q + 31) / 32;
+  const int NWG = gridDim.x;
+  int w = blockIdx.x;
+  if (w < NWG / 8 * 8) w = (w & 7) * (NWG / 8) + (w >> 3);
+  const int unit = w / sp.ns, part = w - unit * sp.ns;
+  const int pair = unit / n_qt, q0 = (unit - pair * n_qt) * 32;
   const int b = pair / p.heads, head = pair - b * p.heads;
-  const int N = p.c.tokens, fb = p.fresh_begin, nf = p.n_fresh;
-  const int nkt = (N + BK - 1) / BK;
-  const int t0 = (int)((long long)nkt * part / sp.ns), t1 = (int)((long long)nkt * (part + 1) / sp.ns);
+  const int N = p.c.tokens, nf = p.n_fresh, fb = nf > 0 ? p.fresh_begin : 0;
+  const int nkt = (N + BK - 1) / BK, shares = sp.ns * KG, share = part * KG + kg;
+  const int t0 = (int)((long long)nkt * share / shares), t1 = (int)((long long)nkt * (share + 1) / shares);
   const size_t H = (size_t)p.heads * D;
-  const unsigned char* k8 = p.c.values + b * p.c.values_bs + (size_t)head * N * D;
-  const unsigned char* v8 = p.c.values + b * p.c.values_bs + (size_t)(p.heads + head) * N * D;
-  const unsigned char* ke = p.c.exps + b * p.c.exps_bs + (size_t)head * N;
-  const unsigned char* ve = p.c.exps + b * p.c.exps_bs + (size_t)(p.heads + head) * N;
+  const __amdgpu_buffer_rsrc_t rk8 = buffer_rsrc(p.c.values + b * p.c.values_bs + (size_t)head * N * D, (size_t)N * D);
+  const __amdgpu_buffer_rsrc_t rv8 = buffer_rsrc(p.c.values + b * p.c.values_bs + (size_t)(p.heads + head) * N * D, (size_t)N * D);
+  const __amdgpu_buffer_rsrc_t rke = buffer_rsrc(p.c.exps + b * p.c.exps_bs + (size_t)head * N, N);
+  const __amdgpu_buffer_rsrc_t rve = buffer_rsrc(p.c.exps + b * p.c.exps_bs + (size_t)(p.heads + head) * N, N);
   const float *kf = nullptr, *vf = nullptr;
   if (nf > 0) {
     kf = reinterpret_cast<const float*>(p.kv_fresh) + b * p.fresh_bs + (size_t)head * nf * D;
@@ -953,57 +965,61 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attn_q8_f32_kernel(A
   }
   // V's padding channels: zero, never written again
   if constexpr (32 * DT > D)
-    for (int i = tid; i < BK * (32 * DT - D); i += TH)
+    for (int i = lane; i < BK * (32 * DT - D); i += 64)
       *reinterpret_cast<float*>(sv + i / (32 * DT - D) * G::VP + (D + i % (32 * DT - D)) * 4) = 0.0f;
 
-  // chunk i * TH + tid of a tile: channels 8 ch .. +8 of key `key`
-  auto chunk = [&](int i, int& key, int& ch) {
-    const int id = i * TH + tid;
-    key = id / CPT;
-    ch = id - key * CPT;
-    return key < BK;
+  // chunk i * 64 + lane of a tile: channels 8 ch .. +8 of key `key`; a key past the last reads zeros
+  u32x2 kr[SL], vr[SL];
+  unsigned ke[SL], ve[SL];
+  auto load = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < SL; ++i) {
+      const int id = i * 64 + lane;
+      const int off = id < BK * CPT ? id * 8 : 0x7fffffff - BK * D;
+      kr[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rk8, off, t * BK * D, 0));
+      vr[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rv8, off, t * BK * D, 0));
+      ke[i] = __builtin_amdgcn_raw_buffer_load_b8(rke, id / CPT, t * BK, 0);
+      ve[i] = __builtin_amdgcn_raw_buffer_load_b8(rve, id / CPT, t * BK, 0);
+    }
   };
-  u32x4 kr[SL][2], vr[SL][2];
-  auto wide = [](u32x2 x, unsigned e, u32x4(&r)[2]) {
+  auto put = [&](char* dst, u32x2 x, unsigned e) __attribute__((always_inline)) {
     const float s = scale_of(e);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x[i], s, false);
-      const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x[i], s, true);
-      r[i] = u32x4{__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(c[0]), __float_as_uint(c[1])};
+      const unsigned word = x[i];
+      const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, s, false);
+      const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, s, true);
+      reinterpret_cast<f32x4*>(dst)[i] = f32x4{a[0], a[1], c[0], c[1]};
     }
   };
-  auto load = [&](int t) {
+  auto store = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < SL; ++i) {
-      int key, ch;
-      if (!chunk(i, key, ch)) continue;
-      const int n = t * BK + key, f = n - fb;
-      kr[i][0] = kr[i][1] = vr[i][0] = vr[i][1] = u32x4{0, 0, 0, 0};
-      if ((unsigned)f < (unsigned)nf) {
-        const u32x4* src = reinterpret_cast<const u32x4*>(kf + (size_t)f * D + ch * 8);
-        kr[i][0] = src[0];
-        kr[i][1] = src[1];
-        const float* col = vf + (size_t)ch * 8 * nf + f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vr[i][e >> 2][e & 3] = __float_as_uint(col[(size_t)e * nf]);
-      } else if (n < N) {
-        wide(*reinterpret_cast<const u32x2*>(k8 + (size_t)n * D + ch * 8), ke[n], kr[i]);
-        wide(*reinterpret_cast<const u32x2*>(v8 + (size_t)n * D + ch * 8), ve[n], vr[i]);
+      const int id = i * 64 + lane, key = id / CPT, ch = id - key * CPT;
+      if (64 * SL == BK * CPT || i + 1 < SL || key < BK) {
+        put(sk + key * G::KP + ch * 32, kr[i], ke[i]);
+        put(sv + key * G::VP + ch * 32, vr[i], ve[i]);
       }
     }
-  };
-  auto store = [&]() {
+    // the band's own keys over them
+    const int n0 = t * BK;
+    if (n0 + BK > fb && n0 < fb + nf) {
+#pragma unroll 2
+      for (int i = 0; i < SL; ++i) {
+        const int id = i * 64 + lane, key = id / CPT, ch = id - key * CPT, f = n0 + key - fb;
+        if (key >= BK || (unsigned)f >= (unsigned)nf) continue;
+        const f32x4* src = reinterpret_cast<const f32x4*>(kf + (size_t)f * D + ch * 8);
+        const float* col = vf + (size_t)ch * 8 * nf + f;
+        f32x4* dk = reinterpret_cast<f32x4*>(sk + key * G::KP + ch * 32);
+        f32x4* dv = reinterpret_cast<f32x4*>(sv + key * G::VP + ch * 32);
+        f32x4 v[2];
 #pragma unroll
-    for (int i = 0; i < SL; ++i) {
-      int key, ch;
-      if (!chunk(i, key, ch)) continue;
-      u32x4* dk = reinterpret_cast<u32x4*>(sk + key * G::KP + ch * 32);
-      u32x4* dv = reinterpret_cast<u32x4*>(sv + key * G::VP + ch * 32);
-      dk[0] = kr[i][0];
-      dk[1] = kr[i][1];
-      dv[0] = vr[i][0];
-      dv[1] = vr[i][1];
+        for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = col[(size_t)e * nf];
+        dk[0] = src[0];
+        dk[1] = src[1];
+        dv[0] = v[0];
+        dv[1] = v[1];
+      }
     }
   };
 
@@ -1020,11 +1036,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attn_q8_f32_kernel(A
     for (int r = 0; r < 16; ++r) oo[t][r] = 0.0f;
   float m_run = -INFINITY, l_run = 0.0f;
 
-  load(t0);
+  if (t0 < t1) load(t0);
   for (int t = t0; t < t1; ++t) {
-    store();
-    __syncthreads();
-    if (t + 1 < t1) load(t + 1);
+    store(t);
+    load(min(t + 1, t1 - 1));
     f32x16 sc = {};
 #pragma unroll
     for (int g = 0; g < G::NG; ++g) {
@@ -1064,11 +1079,36 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attn_q8_f32_kernel(A
       for (int tt = 0; tt < DT; ++tt)
         oo[tt] = __builtin_amdgcn_mfma_f32_32x32x2f32(row[32 * tt], sc[r], oo[tt], 0, 0, 0);
     }
-    __syncthreads();
   }
   l_run += __shfl_xor(l_run, 32, kWave);
+
+  // key group 0 takes the others' parts, [register][lane] in their tiles' places, in their order
+  __syncthreads();
+  if (kg > 0) {
+    float* o = reinterpret_cast<float*>(sk) + lane;
+#pragma unroll
+    for (int tt = 0; tt < DT; ++tt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[(16 * tt + r) * 64] = oo[tt][r];
+    o[DT * 1024] = m_run;
+    o[DT * 1024 + 64] = l_run;
+  }
+  __syncthreads();
+  if (kg > 0) return;
+  auto weight = [](float a, float c) { return a == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a - c); };
+#pragma unroll 1
+  for (int g = 1; g < KG; ++g) {
+    const float* o = reinterpret_cast<const float*>(smem_all + g * G::TILE) + lane;
+    const float m2 = o[DT * 1024], mn = fmaxf(m_run, m2), f1 = weight(m_run, mn), f2 = weight(m2, mn);
+    l_run = l_run * f1 + o[DT * 1024 + 64] * f2;
+    m_run = mn;
+#pragma unroll
+    for (int tt = 0; tt < DT; ++tt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oo[tt][r] = oo[tt][r] * f1 + o[(16 * tt + r) * 64] * f2;
+  }
   if (q0 + lc >= p.n_q) return;
-  const size_t slot = ((size_t)unit * sp.ns + part) * (32 * NW) + 32 * wave + lc;
+  const size_t slot = ((size_t)unit * sp.ns + part) * 32 + lc;
   const float inv = sp.ns == 1 ? 1.0f / l_run : 1.0f;
   float* orow = sp.ns == 1 ? reinterpret_cast<float*>(p.out) + ((size_t)b * p.n_q + q0 + lc) * H + (size_t)head * D
                            : sp.part_o + slot * D;
@@ -1080,6 +1120,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attn_q8_f32_kernel(A
       if (c < D) *reinterpret_cast<f32x4*>(orow + c) = f32x4{oo[tt][4 * g] * inv, oo[tt][4 * g + 1] * inv, oo[tt][4 * g + 2] * inv, oo[tt][4 * g + 3] * inv};
     }
   if (sp.ns > 1 && h == 0) sp.part_ml[slot] = make_float2(m_run, l_run);
+#endif
 }
 
 // The parts of a query tile whose keys ns workgroups shared: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s
@@ -1223,10 +1264,10 @@ Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype, bool workspace)
         consider(&r, 4, 1, pairs, n_q, 128, 1, nkt, Geo<D, 4, true>::WPC, {0.8, 1.15, 1.7},
                  2.5 + 0.0055 * (double)(pairs * nkt) * (0.5 + d / 140.0), d, max_ns);
     } else {
-      // (32-key tiles)
-      const int nkt = ceil_div(n_kv, Geo32<D, 4>::BK);
-      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, 2, {3.3, 4.5, 0}, 0.0, d, max_ns);
-      consider(&r, 2, 0, pairs, n_q, 64, 1, nkt, cmin(3, Geo32<D, 2>::WPC), {3.3, 3.6, 4.5}, 0.0, d, max_ns);
+      // 32-key tiles; the matrix pipe of a SIMD is one wave's at a time
+      using G = Geo32<D>;
+      const double alone = G::tile_us * (G::KG / 4) / (0.5 + d / 140.0);
+      consider(&r, 1, 0, pairs, n_q, 32, G::KG, ceil_div(n_kv, G::BK), G::WPC, {alone, 2 * alone, 0}, 0.0, d, max_ns);
     }
   });
   return r;
@@ -1246,6 +1287,14 @@ hipError_t launch_bf16(const Plan& pl, const AttnQParams& p, const Split& sp, hi
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_q8_kernel<D, NW, PREP>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   return attr != hipSuccess ? attr : launch(attn_q8_kernel<D, NW, PREP>, lds, 256, pl.tiles * pl.ns, p, sp, s);
+}
+
+template <int D>
+hipError_t launch_f32(const Plan& pl, const AttnQParams& p, const Split& sp, hipStream_t s) {
+  using G = Geo32<D>;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_q8_f32_kernel<D>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
+  return attr != hipSuccess ? attr : launch(attn_q8_f32_kernel<D>, G::LDS, 64 * G::KG, pl.tiles * pl.ns, p, sp, s);
 }
 
 // Bytes of the prepared tiles and of the parts.
@@ -1301,8 +1350,7 @@ hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream
       return;
     }
     if (dtype == kBF16) rc = pl.nw == 4 ? launch_bf16<D, 4, false>(pl, p, sp, s) : launch_bf16<D, 1, false>(pl, p, sp, s);
-    else if (pl.nw == 4) rc = launch(attn_q8_f32_kernel<D, 4>, Geo32<D, 4>::LDS, 256, pl.tiles * pl.ns, p, sp, s);
-    else rc = launch(attn_q8_f32_kernel<D, 2>, Geo32<D, 2>::LDS, 128, pl.tiles * pl.ns, p, sp, s);
+    else rc = launch_f32<D>(pl, p, sp, s);
   });
   if (rc != hipSuccess || pl.ns == 1) return rc;
   // shares of the parts: as many as leave the chip full, measured with 1 / 2 / 8 at ... 
