@@ -400,10 +400,11 @@ typedef struct {
 /* Rotary positions of tokens [token_begin, token_begin + n_tok) of the grid, in
  * one launch for n_tensors (1 or 2, e.g. Q and K) tensors T of head_dim
  * channels.  Angles are reduced in fp64, so that far positions keep their
- * places; sines, cosines and products are fp32, rounded once to T.  Every
- * alignment and stride is taken; 16-byte aligned rows are fastest.  An out that
- * overlaps an x in any other way than in place is undefined.  Errors: ORCH_EINVAL
- * (axes, tokens outside the grid, strides shorter than head_dim, NULL). */
+ * places; sines, cosines and products are fp32, rounded once to T.  Any
+ * element-aligned address and stride is taken; 16-byte aligned rows are fastest.
+ * An out that overlaps an x or another out in any other way than in place gives
+ * undefined values.  Errors: ORCH_EINVAL (axes, tokens outside the grid, strides shorter
+ * than head_dim, NULL, the same buffer in both tensors). */
 int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tensors, int n_tensors,
                    int B, int n_tok, int token_begin, int head_dim, int dtype, void* hip_stream);
 
@@ -447,18 +448,23 @@ int orch_op_kv_dequantize(const orch_quantized_kv* cache, int tok_offset, void* 
 /* orch_op_attention with the stale K/V in the 8-bit cache: O = softmax(Q K^T /
  * sqrt(d)) V over cache->tokens keys, those of [fresh_begin, fresh_begin +
  * n_fresh) from kv_fresh (T, as there), the others from the cache.  q, out and the
- * branch layout as there.  Every key and query count and every band is taken at full width.  workspace: device
- * memory (16-byte aligned) of at least orch_attention_quantized_workspace_bytes() bytes lets few queries
- * split the keys over more workgroups; NULL (or fewer bytes) runs unsplit.  The
- * result does not depend on the split beyond rounding.  Errors: ORCH_EINVAL (as
- * orch_op_attention; alignment; tokens * head_dim of 2^31 or more), ORCH_EHIP. */
+ * branch layout as there.  Any number of keys and queries and any band runs on
+ * the matrix cores.  Scores, their running max and sum and the output are fp32; in
+ * bf16 the probabilities are rounded once for the PV product (Q is not rounded
+ * again) and the output once.  workspace: device memory (16-byte aligned) of at
+ * least orch_attention_quantized_workspace_bytes() bytes, one call's at a time,
+ * lets few queries split the keys over more workgroups, and many queries have the
+ * keys widened once for all; NULL (or fewer bytes) runs without either.  The
+ * result does not depend on that beyond rounding, and is the same bits at every
+ * call.  Errors: ORCH_EINVAL (as orch_op_attention; alignment; tokens * head_dim of
+ * 2^31 or more; out or workspace overlapping an input), ORCH_EHIP. */
 int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache,
                                 const void* kv_fresh, size_t fresh_branch_stride, int fresh_begin,
                                 int n_fresh, int B, int heads, int n_q, int head_dim, void* out,
                                 void* workspace, size_t workspace_bytes, int dtype,
                                 void* hip_stream);
 
-/* Workspace bytes orch_op_attention_quantized can use for this shape (0: never splits). */
+/* Workspace bytes orch_op_attention_quantized can use for this shape (0: none). */
 size_t orch_attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int head_dim,
                                                 int dtype);
 

@@ -94,11 +94,11 @@ struct Split {
 
 template <int D, int NW, bool PREP>
 __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(AttnQParams p, Split sp) {
+  // (the body uses device-only types; the host pass only needs the launch stub)
+#if defined(__HIP_DEVICE_COMPILE__)
   using G = Geo<D, NW, PREP>;
   constexpr int NC = G::NC, NT = G::NT, SL = G::SL, CPT = G::CPT, TH = G::THREADS, KG = G::KG;
   constexpr bool M32 = G::M32;
-  // (the body uses device-only types; the host pass only needs the launch stub)
-#if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ __attribute__((aligned(1024))) char smem_all[];
   const int lane = threadIdx.x & 63, lc = lane & 31, h = lane >> 5;
   const int i16 = lane & 15, g16 = lane >> 4;

@@ -138,6 +138,10 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
       p.t[k].os[a] = extent[a] > 1 ? t.out_stride[a] : 0;
     }
   }
+  if (n_tensors == 2 && n_tok > 0) {
+    const orch_rotary_tensor &a = tensors[0], &c = tensors[1];
+    if (a.out == c.out || a.out == c.x || a.x == c.out) return fail("the two tensors overlap");
+  }
   p.n_t = n_tensors; p.B = B; p.n_tok = n_tok; p.d = head_dim; p.token_begin = token_begin;
   p.rows = axes->extent[1]; p.cols = axes->extent[2]; p.interleaved = axes->interleaved != 0;
   return launched(launch_rotary(p, dtype, (hipStream_t)hip_stream), "rotary launch");

@@ -216,3 +216,39 @@ def test_rows_and_neighbours_untouched(orch_lib):
     orch_lib.attention_quantized(to_dev(q, "bf16"), cache, None, 0, 0, 0, 1, 2, 37, 72, out, 1)
     torch.cuda.synchronize()
     assert torch.all(out[37 * 144:] == 7) and not torch.any(out[:37 * 144] == 7)
+
+
+@pytest.mark.parametrize("dtype,B,heads,d,n_q,N", [("bf16", 2, 16, 72, 1100, 600), ("bf16", 1, 2, 64, 20, 5000), ("f32", 1, 2, 64, 20, 5000)])
+def test_a_workspace_is_used_whole_or_not_at_all(orch_lib, dtype, B, heads, d, n_q, N):
+    """Fewer bytes than asked for: the bits of a call without one, and nothing written past the bytes that are there."""
+    rng = np.random.default_rng(11)
+    q, v8, e8, fk, fv, K, V = make(rng, dtype, B, heads, d, n_q, N, 0, 0)
+    qd, values, exps = to_dev(q, dtype), torch.from_numpy(v8).to(DEV), torch.from_numpy(e8).to(DEV)
+    cache = orch_lib.quantized_kv(values, exps)
+    need = orch_lib.attention_quantized_workspace_bytes(B, heads, n_q, N, d, code(dtype))
+    assert need > 0
+    ws = torch.full((need + 256,), 0x5a, dtype=torch.uint8, device=DEV)
+    outs = []
+    for bytes_ in (None, 16, need - 1, need):
+        out = torch.empty((B, n_q, heads * d), dtype=qd.dtype, device=DEV)
+        orch_lib.attention_quantized(qd, cache, None, 0, 0, 0, B, heads, n_q, d, out, code(dtype),
+                                     workspace=None if bytes_ is None else ws[:bytes_])
+        outs.append(out)
+        if bytes_ != need:
+            assert torch.all(ws == 0x5a)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    assert torch.all(ws[need:] == 0x5a) and not torch.all(ws[:need] == 0x5a)
+    for out in (outs[0], outs[3]):
+        check(to_host(out).reshape(B, n_q, heads, d).transpose(0, 2, 1, 3), dtype, q, K, V)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [72, 128])
+def test_repeated_calls_give_the_same_bits(orch_lib, dtype, d):
+    """No order of waves or workgroups shows: ten calls of each variant, bit for bit."""
+    for B, heads, n_q, N, fb, nf in ((1, 2, 40, 330, 50, 40), (2, 16, 520, 333, 0, 0), (2, 16, 1100, 640, 64, 512)):
+        rng = np.random.default_rng(12)
+        q, v8, e8, fk, fv, K, V = make(rng, dtype, B, heads, d, n_q, N, fb, nf)
+        first = run(orch_lib, dtype, q, v8, e8, fk, fv, fb)
+        for _ in range(9):
+            np.testing.assert_array_equal(run(orch_lib, dtype, q, v8, e8, fk, fv, fb), first)

@@ -93,6 +93,9 @@ def _rotary(lib, tensors=None, n_tensors=1, B=1, n_tok=4, begin=0, d=32, dtype=B
     (dict(tensors=[dict(x=P[0] + 1)]), "aligned"), (dict(tensors=[dict(xs=(0, 128, 31))]), "strides"),
     (dict(tensors=[dict(os=(0, 16, 32))]), "strides"), (dict(B=2, tensors=[dict(os=(8, 128, 32))]), "strides"),
     (dict(n_tensors=2, tensors=[dict(), dict(out=None)]), "NULL"),
+    (dict(n_tensors=2, tensors=[dict(out=P[0]), dict(out=P[0])]), "overlap"),
+    (dict(n_tensors=2, tensors=[dict(), dict(x=P[2], out=P[0])]), "overlap"),
+    (dict(n_tensors=2, tensors=[dict(), dict(x=P[1], out=P[2])]), "overlap"),
 ])
 def test_rotary_refuses(orch_lib, kw, word):
     _refused(orch_lib, _rotary(orch_lib, **kw), word)
