@@ -86,7 +86,7 @@ struct Geo {
 
 struct Launch {
   KvCacheParams p;
-  int k_blocks;      // workgroups of one (branch, head) on K; the rest take V tiles
+  int v_blocks;      // workgroups of one (branch, head) on V tiles, first (they take longer); the rest take K
   int vec;           // V^T rows and offsets in whole 16-byte chunks
 };
 
@@ -99,8 +99,9 @@ __global__ __launch_bounds__(256) void kv_quantize_kernel(Launch L) {
   const T* kv = reinterpret_cast<const T*>(p.kv) + b * p.kv_bs;
   unsigned char* vals = p.c.values + b * p.c.values_bs;
   unsigned char* exps = p.c.exps + b * p.c.exps_bs;
-  if ((int)blockIdx.x < L.k_blocks) {
-    const int r = lane / G::LPR, j = lane - r * G::LPR, n = blockIdx.x * G::KROWS + wave * G::RPW + r;
+  if ((int)blockIdx.x >= L.v_blocks) {
+    const int kb = blockIdx.x - L.v_blocks;
+    const int r = lane / G::LPR, j = lane - r * G::LPR, n = kb * G::KROWS + wave * G::RPW + r;
     const bool on = n < p.n && r < G::RPW;
     const T* src = kv + ((size_t)h * p.kv_tokens + p.kv_off + (on ? n : 0)) * D + j * 8;
     float v[G::CPR][8];
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(256) void kv_quantize_kernel(Launch L) {
   // V: eight neighbouring lanes hold the same 8 tokens, 4 channels each
   __shared__ unsigned red[G::WAVES][kTile];
   __shared__ __attribute__((aligned(16))) unsigned char tile[kTile * G::PITCH];
-  const int n0 = (blockIdx.x - L.k_blocks) * kTile;
+  const int n0 = blockIdx.x * kTile;
   const int tg = lane >> 3, quad = wave * 8 + (lane & 7);
   const bool on = quad < G::QUADS;
   const int count = min(max(p.n - n0 - 8 * tg, 0), 8);
@@ -192,11 +193,12 @@ __global__ __launch_bounds__(256) void kv_dequantize_kernel(Launch L) {
   T* kv = reinterpret_cast<T*>(p.kv) + b * p.kv_bs;
   const unsigned char* vals = p.c.values + b * p.c.values_bs;
   const unsigned char* exps = p.c.exps + b * p.c.exps_bs;
-  if ((int)blockIdx.x < L.k_blocks) {
+  if ((int)blockIdx.x >= L.v_blocks) {
+    const int kb = blockIdx.x - L.v_blocks;
     // both sides contiguous: chunk after chunk
     const size_t row0 = (size_t)h * p.c.tokens + p.c_off;
     T* dst = kv + ((size_t)h * p.kv_tokens + p.kv_off) * D;
-    const int first = blockIdx.x * G::THREADS * G::KCH, total = p.n * G::CPT;
+    const int first = kb * G::THREADS * G::KCH, total = p.n * G::CPT;
     u32x2 w[G::KCH];
     float s[G::KCH];
 #pragma unroll
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(256) void kv_dequantize_kernel(Launch L) {
     return;
   }
   __shared__ __attribute__((aligned(16))) unsigned char tile[kTile * G::PITCH];
-  const int n0 = (blockIdx.x - L.k_blocks) * kTile;
+  const int n0 = blockIdx.x * kTile;
   const int total = min(kTile, p.n - n0) * G::CPT;
   const size_t row0 = (size_t)(p.heads + h) * p.c.tokens + p.c_off + n0;
   const int lane = tid & 63, tg = lane >> 3, quad = (tid >> 6) * 8 + (lane & 7);
@@ -259,9 +261,10 @@ hipError_t launch_d(const KvCacheParams& p, bool back, hipStream_t s) {
   using G = Geo<D>;
   Launch L;
   L.p = p;
-  L.k_blocks = back ? ceil_div(p.n * G::CPT, G::THREADS * G::KCH) : ceil_div(p.n, G::KROWS);
+  const int k_blocks = back ? ceil_div(p.n * G::CPT, G::THREADS * G::KCH) : ceil_div(p.n, G::KROWS);
+  L.v_blocks = ceil_div(p.n, kTile);
   L.vec = p.kv_tokens % 8 == 0 && p.kv_off % 8 == 0;
-  const dim3 grid(L.k_blocks + ceil_div(p.n, kTile), p.heads * p.B), block(G::THREADS);
+  const dim3 grid(L.v_blocks + k_blocks, p.heads * p.B), block(G::THREADS);
   if (back) hipLaunchKernelGGL((kv_dequantize_kernel<T, D>), grid, block, 0, s, L);
   else hipLaunchKernelGGL((kv_quantize_kernel<T, D>), grid, block, 0, s, L);
   return hipGetLastError();
