@@ -403,7 +403,7 @@ typedef struct {
  * places; sines, cosines and products are fp32, rounded once to T.  Any
  * element-aligned address and stride is taken; 16-byte aligned rows are fastest.
  * An out that overlaps an x or another out in any other way than in place gives
- * undefined values.  Errors: ORCH_EINVAL (axes, tokens outside the grid, strides shorter
+ * undefined values.  Errors: ORCH_EINVAL (axes, angles past fp64's range, tokens outside the grid, strides shorter
  * than head_dim, NULL, the same buffer in both tensors). */
 int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tensors, int n_tensors,
                    int B, int n_tok, int token_begin, int head_dim, int dtype, void* hip_stream);
@@ -411,8 +411,8 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
 /* The 8-bit K/V cache of `tokens` tokens.  Branch b holds, from values +
  * b * values_stride (bytes), e4m3 bytes (OCP: largest 448, no infinity) K
  * [heads][tokens][head_dim], then V [heads][tokens][head_dim]; from exponents +
- * b * exponents_stride (bytes) one E8M0 byte e for each of K [heads][tokens], then
- * V [heads][tokens]: an element stands for value * 2^(e - 127).  V is token-major
+ * b * exponents_stride (bytes) one E8M0 byte e (1 to 254) for each of K
+ * [heads][tokens], then V [heads][tokens]: an element stands for value * 2^(e - 127).  V is token-major
  * here, unlike in the buffer of the operand type: a token's values share one
  * scale, so a band of tokens is a set of contiguous runs (one per head for each of
  * K and V) whatever its offset, and a token's bytes depend on that token alone.

@@ -364,11 +364,19 @@ def quantized_kv(values, exponents) -> QuantizedKV:
         raise OrchError(ORCH_EINVAL, "a branch's values and exponents must be contiguous")
     c = QuantizedKV(values.data_ptr(), exponents.data_ptr(), values.stride(0), exponents.stride(0), tokens)
     c.tensors, c.devices = (values, exponents), (values.get_device(), exponents.get_device())
+    c.shape = (B, heads, d)
     return c
+
+
+def _check_cache(cache, B, heads, head_dim):
+    b, h, d = cache.shape
+    if heads != h or head_dim != d or B > b:
+        raise OrchError(ORCH_EINVAL, f"{B} branches of {heads} heads of {head_dim} channels, the cache holds {b} of {h} of {d}")
 
 
 def kv_quantize(kv, kv_branch_stride, kv_tokens, kv_offset, cache: QuantizedKV, tok_offset, B, heads,
                 n_tok, head_dim, dtype, stream=None):
+    _check_cache(cache, B, heads, head_dim)
     st = _stream_on(stream, kv.get_device(), *cache.devices)
     check(lib.orch_op_kv_quantize(kv.data_ptr(), kv_branch_stride, kv_tokens, kv_offset, C.byref(cache),
                                   tok_offset, B, heads, n_tok, head_dim, dtype, st))
@@ -376,6 +384,7 @@ def kv_quantize(kv, kv_branch_stride, kv_tokens, kv_offset, cache: QuantizedKV, 
 
 def kv_dequantize(cache: QuantizedKV, tok_offset, kv, kv_branch_stride, kv_tokens, kv_offset, B, heads,
                   n_tok, head_dim, dtype, stream=None):
+    _check_cache(cache, B, heads, head_dim)
     st = _stream_on(stream, kv.get_device(), *cache.devices)
     check(lib.orch_op_kv_dequantize(C.byref(cache), tok_offset, kv.data_ptr(), kv_branch_stride, kv_tokens,
                                     kv_offset, B, heads, n_tok, head_dim, dtype, st))
@@ -387,6 +396,7 @@ def attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype) ->
 
 def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, n_fresh, B, heads, n_q,
                         head_dim, out, dtype, workspace=None, stream=None):
+    _check_cache(cache, B, heads, head_dim)
     ws_bytes = 0 if workspace is None else workspace.nbytes
     st = _stream_on(stream, *cache.devices, *[t.get_device() for t in (q, kv_fresh, out, workspace) if t is not None])
     check(lib.orch_op_attention_quantized(_ptr(q), C.byref(cache), _ptr(kv_fresh), fresh_bs, fresh_begin,

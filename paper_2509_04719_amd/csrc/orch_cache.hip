@@ -116,7 +116,10 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
     // theta^(-2 i / channels), one multiplication a pair
     const double ratio = ch ? std::pow(axes->theta, -2.0 / ch) : 1.0;
     double f = axes->step[a] / 6.283185307179586476925286766559;
-    for (int i = 0; i < ch / 2; ++i, f *= ratio) p.turns[pair++] = f;
+    for (int i = 0; i < ch / 2; ++i, f *= ratio) {
+      if (!std::isfinite(f * (std::fabs(axes->origin[a]) + ext))) return fail("an angle of axis %d is past fp64's range", a);
+      p.turns[pair++] = f;
+    }
   }
   if (n_tok < 0 || token_begin < 0 || n_tok > tokens - token_begin)
     return fail("tokens [%d, %d + %d) not within the grid's %lld", token_begin, token_begin, n_tok, tokens);

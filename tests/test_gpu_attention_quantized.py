@@ -203,6 +203,31 @@ def test_agrees_with_attention_over_the_read_back_buffer(orch_lib, dtype):
     assert rel_l2(got, ref) <= 2 * NORM[dtype]
 
 
+@pytest.mark.parametrize("dtype,n_q", [("bf16", 1), ("bf16", 300), ("f32", 1)])
+def test_a_long_cache(orch_lib, dtype, n_q):
+    """More than 2^32 bytes from the first value to the last; all but a few keys, at both ends of it and between, at
+    scores 224 below 0, whose probabilities are 0 in fp32."""
+    heads, d, N, nf = 2, 64, 2 ** 24 + 70, 33
+    fb, at = N - 50, np.array([0, 1, 2 ** 23 + 5, 2 ** 24 - 1, N - 1])
+    values = torch.zeros((1, 2, heads, N, d), dtype=torch.uint8, device=DEV)
+    exps = torch.full((1, 2, heads, N), 127, dtype=torch.uint8, device=DEV)
+    assert values.numel() > 2 ** 32
+    values[:, 0, :, :, 0] = 0xfe                       # -448
+    values[:, 1] = 0x40                                # 2
+    q, v8, e8, fk, fv, K, V = make(np.random.default_rng(13), dtype, 1, heads, d, n_q, len(at) + nf, len(at), nf)
+    q[..., 0], K[..., 0], fk[..., 0] = 4.0, 0.0, 0.0
+    v8[:, 0, :, :, 0] = 0
+    for i, n in enumerate(at):
+        values[:, :, :, n], exps[:, :, :, n] = torch.from_numpy(v8[:, :, :, i]).to(DEV), torch.from_numpy(e8[:, :, :, i]).to(DEV)
+    cache = orch_lib.quantized_kv(values, exps)
+    fresh = to_dev(ok.to_buffer(fk, fv), dtype)
+    need = orch_lib.attention_quantized_workspace_bytes(1, heads, n_q, N, d, code(dtype))
+    for ws in (None, torch.empty(need, dtype=torch.uint8, device=DEV)):
+        out = torch.empty((1, n_q, heads * d), dtype=fresh.dtype, device=DEV)
+        orch_lib.attention_quantized(to_dev(q, dtype), cache, fresh, 0, fb, nf, 1, heads, n_q, d, out, code(dtype), workspace=ws)
+        check(to_host(out).reshape(1, n_q, heads, d).transpose(0, 2, 1, 3), dtype, q, K, V)
+
+
 def test_rows_and_neighbours_untouched(orch_lib):
     """No query, and what lies behind the output."""
     rng = np.random.default_rng(9)

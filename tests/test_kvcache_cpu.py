@@ -88,6 +88,7 @@ def _rotary(lib, tensors=None, n_tensors=1, B=1, n_tok=4, begin=0, d=32, dtype=B
     (dict(step=(0, 0, float("nan"))), "step"), (dict(n_tok=17), "grid"), (dict(begin=13), "grid"),
     (dict(begin=-1), "grid"), (dict(n_tok=-1), "grid"), (dict(begin=2 ** 31 - 1), "grid"),
     (dict(extent=(1 << 10, 1 << 10, 1 << 10), n_tok=1 << 27), "2^31"),
+    (dict(theta=1e-300, step=(1, 1, 1e50)), "angle"), (dict(origin=(0, 1e300, 0), step=(1, 1e300, 1)), "angle"),
     (dict(tensors=[dict(x=None)]), "NULL"), (dict(tensors=[dict(out=None)]), "NULL"),
     (dict(tensors=[dict(heads=0)]), "heads"), (dict(tensors=[dict(heads=40000)]), "heads"),
     (dict(tensors=[dict(x=P[0] + 1)]), "aligned"), (dict(tensors=[dict(xs=(0, 128, 31))]), "strides"),
@@ -175,6 +176,14 @@ def test_binding_of_the_cache_refuses(orch_lib):
     for bad in ((v, e[..., :4]), (v.float(), e), (v, e.short()), (v[..., :16], e), (v[:, :1], e[:, :1])):
         with pytest.raises(orch_lib.OrchError):
             orch_lib.quantized_kv(*bad)
+    # a call of other branches, heads or channels than the cache's
+    x = torch.zeros(4096, dtype=torch.bfloat16)
+    for B, heads, d in ((2, 3, 32), (1, 2, 32), (1, 4, 32), (1, 3, 64)):
+        for call in (lambda: orch_lib.kv_quantize(x, 0, 8, 0, c, 0, B, heads, 8, d, BF16),
+                     lambda: orch_lib.kv_dequantize(c, 0, x, 0, 8, 0, B, heads, 8, d, BF16),
+                     lambda: orch_lib.attention_quantized(x, c, None, 0, 0, 0, B, heads, 8, d, x, BF16)):
+            with pytest.raises(orch_lib.OrchError, match="the cache holds"):
+                call()
 
 
 @pytest.mark.parametrize("bad", [dict(B=0), dict(heads=0), dict(n_q=-1), dict(n_kv=0), dict(d=0), dict(d=40), dict(dtype=7)])
