@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
       return;
     }
     if (type == kFresh) {
-      constexpr int BATCH = G::AHEAD ? SL : cmin(SL, NW == 4 || D == 80 || D == 96 ? 4 : 6);
+      constexpr int BATCH = G::AHEAD ? SL : cmin(SL, NW == 4 || D == 80 || D == 96 ? 4 : D == 72 ? 9 : 6);
 #pragma unroll
       for (int i0 = 0; i0 < SL; i0 += BATCH) {
         u32x4 x[BATCH];
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     // cache's keys, then the fresh ones, K's in rows, V's along the keys
     const int n0 = t * BKV;
     auto fresh = [&](int key) __attribute__((always_inline)) { return (unsigned)(n0 + key - fb) < (unsigned)nf; };
-    constexpr int BATCH = cmin(SL, NW == 4 ? 2 : D == 128 ? 16 : D <= 72 ? 8 : 4);
+    constexpr int BATCH = cmin(SL, NW == 4 ? 2 : D == 128 ? 16 : D <= 72 ? 9 : 4);
 #pragma unroll
     for (int i0 = 0; i0 < SL; i0 += BATCH) {
       u32x4 x[BATCH];
@@ -311,8 +311,10 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
       }
     }
     if (!isk && n0 + BKV > fb && n0 < fb + nf) {
-      // chunk id: channel id / 8, keys 8 (id % 8) .. +8
-      const int kc = 8 * (vtid & 7), f = n0 + kc - fb;
+      // chunk id: channel id / 8, keys 8 (id % 8) .. +8.  Its fresh keys come from eight elements of the channel's row
+      // that lie in the band (all of it where it has fewer), element j of them key j + shift of the chunk.
+      const int kc = 8 * (vtid & 7), f = n0 + kc - fb, first = min(max(f, 0), max(nf - 8, 0)), shift = first - f;
+      const bool some = f > -8 && f < nf;
       unsigned short* col = reinterpret_cast<unsigned short*>(dst + G::ST * G::KS + vrow(kc) * G::VP) + (vtid >> 3);
 #pragma unroll
       for (int i0 = 0; i0 < SL; i0 += BATCH) {
@@ -320,43 +322,28 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
           const int i = cmin(i0 + k, SL - 1);
-          const unsigned short* src = reinterpret_cast<const unsigned short*>(vf) + (size_t)((vtid >> 3) + i * (TH / 8)) * nf + f;
-          x[k] = u32x4{0, 0, 0, 0};
-          if (i0 + k < SL && on(isk_c, i)) {
-            if (f >= 0 && f + 8 <= nf) {
+          const unsigned short* src = reinterpret_cast<const unsigned short*>(vf) + (size_t)((vtid >> 3) + i * (TH / 8)) * nf + first;
+          if (some && i0 + k < SL && on(isk_c, i)) {
+            if (nf >= 8) {
               const u32x4_u y = *reinterpret_cast<const u32x4_u*>(src);
               x[k] = u32x4{y[0], y[1], y[2], y[3]};
-            } else if (f > -8 && f < nf) {
-              // (all eight loads in flight: the ones outside the band read its nearest element)
-              unsigned y[8];
+            } else {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y[e] = src[min(max(f + e, 0), nf - 1) - f];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[k][e] = y[2 * e] | y[2 * e + 1] << 16;
+              for (int e = 0; e < 4; ++e) x[k][e] = src[min(2 * e, nf - 1)] | (unsigned)src[min(2 * e + 1, nf - 1)] << 16;
             }
           }
         }
-        if (f >= 0 && f + 8 <= nf) {
 #pragma unroll
-          for (int k = 0; k < BATCH; ++k) {
-            const int i = cmin(i0 + k, SL - 1);
-            if (i0 + k < SL && on(isk_c, i)) {
+        for (int j = 0; j < 8; ++j) {
+          const int key = j + shift;
+          unsigned short* to = col + ((key & 4) << 2 | (key & 3)) * (G::VP / 2);
+          if (some && (unsigned)key < 8u && j < nf) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                col[vrow(e) * (G::VP / 2) + i * (TH / 8)] = (unsigned short)(x[k][e >> 1] >> (16 * (e & 1)));
+            for (int k = 0; k < BATCH; ++k) {
+              const int i = cmin(i0 + k, SL - 1);
+              if (i0 + k < SL && on(isk_c, i)) to[i * (TH / 8)] = (unsigned short)(x[k][j >> 1] >> (16 * (j & 1)));
             }
           }
-        } else {
-#pragma unroll 1
-          for (int e = 0; e < 8; ++e)
-            if ((unsigned)(f + e) < (unsigned)nf) {
-#pragma unroll
-              for (int k = 0; k < BATCH; ++k) {
-                const int i = cmin(i0 + k, SL - 1);
-                const unsigned w = e & 4 ? (e & 2 ? x[k][3] : x[k][2]) : (e & 2 ? x[k][1] : x[k][0]);
-                if (i0 + k < SL && on(isk_c, i)) col[vrow(e) * (G::VP / 2) + i * (TH / 8)] = (unsigned short)(w >> (16 * (e & 1)));
-              }
-            }
         }
       }
     }
@@ -1258,8 +1245,9 @@ Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype, bool workspace)
     if (dtype == kBF16) {
       const int nkt = ceil_div(n_kv, BKV);
       consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, Geo<D, 4>::WPC, {1.3, 1.85, 0}, 0.0, d, max_ns);
-      // (its longer straight code is read once by every CU: 1 us at d = 64, 7 at d = 128)
-      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.8 : 1.33, 2.4, 0}, D <= 64 ? D / 64 : 1.0 + (D - 64) * 0.09, d, max_ns);
+      // (its longer straight code is read once by every CU: 1 us at d = 64, 7 at d = 128; two workgroups on a
+      // CU share its LDS best at small d: 2 x 8 heads, 1000 queries x 4096 keys at d = 32 in 28.6 us, prepared 33.9)
+      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.8 : 1.33, 1.8 + D / 120.0, 0}, D <= 64 ? D / 64 : 1.0 + (D - 64) * 0.09, d, max_ns);
       if (workspace && (long long)nkt * (Geo<D, 4, true>::KT + Geo<D, 4, true>::VT) < (1ll << 31))
         consider(&r, 4, 1, pairs, n_q, 128, 1, nkt, Geo<D, 4, true>::WPC, {0.8, 1.15, 1.7},
                  2.5 + 0.0055 * (double)(pairs * nkt) * (0.5 + d / 140.0), d, max_ns);
@@ -1353,7 +1341,9 @@ hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream
     else rc = launch_f32<D>(pl, p, sp, s);
   });
   if (rc != hipSuccess || pl.ns == 1) return rc;
-  // shares of the parts: as many as leave the chip full, measured with 1 / 2 / 8 at ... 
+  // shares of the parts: eight where few parts' threads would each walk many parts in turn (20 queries x 5000 keys,
+  // 40 parts), one where the chip is full without (384 queries x 4096 keys, 5 parts, 2 x 16 heads: 17 us with eight
+  // shares, most of them empty, 7 with one)
   const int rows = 32 * pl.nw;
   const long long quads = (long long)p.B * p.heads * p.n_q * (p.d / 4);
   const int shares = quads >= 65536 || pl.ns <= 4 ? 1 : 8;

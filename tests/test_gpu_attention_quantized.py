@@ -78,6 +78,8 @@ SHAPES = [  # heads, n_q, n_kv, fresh_begin, n_fresh
     (1, 1, 1, 0, 0), (1, 1, 1, 0, 1), (3, 1, 200, 7, 1), (2, 2, 65, 64, 1), (2, 31, 64, 0, 64), (2, 33, 63, 5, 33),
     (4, 40, 128, 40, 40), (2, 65, 321, 100, 65), (2, 96, 256, 80, 96), (3, 130, 1000, 333, 130), (1, 300, 2025, 1035, 45),
     (2, 17, 4100, 0, 0), (16, 129, 640, 0, 640), (1, 1, 9000, 8990, 10), (8, 260, 1024, 512, 260),
+    # short bands across chunks of eight keys and across tiles
+    (2, 40, 200, 6, 5), (2, 9, 130, 60, 8), (1, 600, 130, 62, 7), (2, 70, 150, 61, 9), (1, 3, 70, 64, 6),
     # many queries: keys laid out as tiles once
     (2, 513, 1001, 333, 513), (1, 600, 640, 0, 640), (3, 512, 65, 3, 1), (1, 1100, 192, 64, 128), (2, 700, 1, 0, 0),
 ]
