@@ -1,10 +1,25 @@
 // Attention of a band's queries over the whole image, K/V of the band's own tokens
 // fresh (operand type) and of every other token in the 8-bit cache.
 //
-// Flash style on the matrix cores.  A workgroup of NW waves takes 32 NW queries
-// of one (branch, head), a wave 32 of them, 64 keys a tile.  Scores are formed
-// transposed, S^T = K Q^T, so that a lane owns one query column and the running
-// max and sum of the softmax stay in the lane.
+// O = softmax(Q K^T / sqrt d) V in one pass over the keys, with a running max and sum.  Scores are formed transposed,
+// S^T = K Q^T, so that a lane owns one query column and its max and sum stay in the lane; 32 queries a wave, 64 keys a
+// tile (32 in fp32).  The cache's bytes are widened to the operand type on their way to LDS (exact: e4m3 times a
+// power of two is a bf16 number), and the band's own keys take the place of the cache's there.  Matrix products in 8
+// bits would need Q and the probabilities in 8 bits too.
+//
+// Bound by the matrix cores with many queries (4 B heads n_q n_kv d flops), else by a wave's own chain: widening a
+// key costs the VALU as much as a wave's softmax of it, and VALU and MFMA instructions of a SIMD do not overlap
+// freely.  So there are four forms, chosen by an estimate of their time (`plan` below):
+//   prepared    many queries: the keys are widened once, fresh and cached together, into tiles in the workspace, and
+//               four waves of 32 queries load each tile straight to LDS.  d = 72, 2 x 16 heads: 6144 queries x
+//               16384 keys 960 us (966 TFLOP/s; 51 of it preparing), 1664 x 4096 87 us; d = 128, 2 x 8 heads,
+//               4096 x 4096 134 us (1027).
+//   NW = 4      without a workspace, or too few queries to pay for it: four waves of 32 queries share each tile, each
+//               widens a quarter of it.  384 x 4096, keys split 5 ways: 33 us and 6 for the parts.
+//   NW = 1      few queries: four waves have the same 32 queries and each a quarter of the keys, without a barrier.
+//               384 x 1024: 16.7 us; one query x 16384 keys (75 MB of cache): 24 us and 4 for the parts, 3.1 TB/s.
+//   fp32        the same on v_mfma_f32_32x32x2: 512 x 1024 keys, 4 heads of 32: 8.4 us.
+// With a workspace each may also split the keys of a query tile over workgroups; a merge kernel joins the parts.
 #include <cfloat>
 
 #include "common.h"
@@ -811,7 +826,8 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
 // Prepared tiles.  Every 128 queries of a (branch, head) read the same keys, and a wave's VALU work is
 // paid in full next to its MFMAs: with many queries the keys are widened once, fresh and cached ones
 // together, into tiles that lie in memory as they will in LDS: K rows of KP bytes, V^T rows of 64 keys
-// with their 16-byte chunks swizzled by row (keys past the last are zeros).
+// with their 16-byte chunks swizzled by row (keys past the last are zeros).  Bound by memory: 16384 keys, 2 x 16 heads
+// of 72 (51 MB read of HBM, 148 written) in 50 us, 4.0 TB/s.
 template <int D>
 __global__ __launch_bounds__(256) void attn_q8_prepare_kernel(AttnQParams p, char* tiles) {
   using G = Geo<D, 4, true>;
@@ -1112,7 +1128,8 @@ __global__ __launch_bounds__(64 * Geo32<D>::KG, Geo32<D>::KG / 4) void attn_q8_f
 
 // The parts of a query tile whose keys ns workgroups shared: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s
 // - m) l_s, m = max_s m_s.  A thread per 4 channels of a query and share of the parts (part s of
-// share s % SG, four in flight), the shares met in LDS in their order.
+// share s % SG, four in flight), the shares met in LDS in their order.  Bound by its own launch and one chain of loads
+// for few parts (3.5 us), by their bytes for many (384 queries x 5 parts, 2 x 16 heads of 72: 18 MB in 5.5 us).
 template <typename T, int SG>
 __global__ __launch_bounds__(256) void attn_q8_merge_kernel(AttnQParams p, Split sp, int rows) {
   __shared__ float ml_s[256][2];

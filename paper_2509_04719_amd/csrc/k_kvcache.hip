@@ -8,7 +8,10 @@
 // there, takes one byte (E8M0), and is what the conversion instructions take as
 // their scale.  K rows are contiguous in both layouts; V is transposed (V^T
 // [d][tokens] in the buffer, token-major in the cache) through LDS in tiles of 64
-// tokens.  One read and one write of every element: bound by memory.
+// tokens, each lane with 8 tokens x 4 channels of it in registers.  One read and one write of every element: bound by
+// memory.  d = 72, 2 x 16 heads, bf16: 16384 tokens written in 51 us (228 MB, 4.5 TB/s) and read back in 35 (6.5,
+// part of it from the caches); 1664 tokens of 4096 written in 9.5-10 us (23 MB), 4096 read back in 9.5-10 (57 MB).
+// Workgroups of 64 tokens of one head: the V ones take longer and start first.
 #include "common.h"
 #include "kernels.h"
 
