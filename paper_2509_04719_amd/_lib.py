@@ -355,11 +355,12 @@ def rotary(axes: RotaryAxes, token_begin, x, out, stream=None):
 def quantized_kv(values, exponents) -> QuantizedKV:
     """The 8-bit K/V cache held by two tensors: e4m3 (or uint8) values [B, 2, heads, tokens, d]
     and uint8 exponents [B, 2, heads, tokens], contiguous within a branch.  It keeps the tensors."""
+    import torch
     B, two, heads, tokens, d = values.shape
     if two != 2 or tuple(exponents.shape) != (B, 2, heads, tokens):
         raise OrchError(ORCH_EINVAL, "values [B, 2, heads, tokens, d] and exponents [B, 2, heads, tokens] are needed")
-    if values.element_size() != 1 or exponents.element_size() != 1:
-        raise OrchError(ORCH_EINVAL, "values and exponents must be of one byte")
+    if values.dtype not in (torch.uint8, torch.float8_e4m3fn) or exponents.dtype != torch.uint8:
+        raise OrchError(ORCH_EINVAL, "values must be e4m3fn or uint8, exponents uint8")
     if not (values[0].is_contiguous() and exponents[0].is_contiguous()):
         raise OrchError(ORCH_EINVAL, "a branch's values and exponents must be contiguous")
     c = QuantizedKV(values.data_ptr(), exponents.data_ptr(), values.stride(0), exponents.stride(0), tokens)

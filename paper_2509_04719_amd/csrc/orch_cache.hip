@@ -167,7 +167,10 @@ int orch_op_kv_dequantize(const orch_quantized_kv* cache, int tok_off, void* kv,
 }
 
 size_t orch_attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int head_dim, int dtype) {
-  if (B < 1 || heads < 1 || n_q < 0 || n_kv < 1 || head_dim < 1 || (dtype != ORCH_F32 && dtype != ORCH_BF16)) return 0;
+  // (a shape that the call refuses needs none)
+  if (B < 1 || heads < 1 || (long long)B * heads > 32767 || n_q < 0 || n_kv < 1 || head_dim < 1 ||
+      (dtype != ORCH_F32 && dtype != ORCH_BF16) || (long long)n_q * head_dim >= 1ll << 31 || (long long)n_kv * head_dim >= 1ll << 31)
+    return 0;
   return attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype);
 }
 

@@ -173,7 +173,8 @@ def test_binding_of_the_cache_refuses(orch_lib):
     v, e = torch.zeros((1, 2, 3, 8, 32), dtype=torch.uint8), torch.zeros((1, 2, 3, 8), dtype=torch.uint8)
     c = orch_lib.quantized_kv(v, e)
     assert (c.values, c.exponents, c.tokens) == (v.data_ptr(), e.data_ptr(), 8)
-    for bad in ((v, e[..., :4]), (v.float(), e), (v, e.short()), (v[..., :16], e), (v[:, :1], e[:, :1])):
+    for bad in ((v, e[..., :4]), (v.float(), e), (v, e.short()), (v[..., :16], e), (v[:, :1], e[:, :1]), (v.view(torch.float8_e5m2), e),
+                (v.view(torch.float8_e4m3fnuz), e), (v.view(torch.int8), e), (v, e.view(torch.int8))):
         with pytest.raises(orch_lib.OrchError):
             orch_lib.quantized_kv(*bad)
     # a call of other branches, heads or channels than the cache's
@@ -186,7 +187,8 @@ def test_binding_of_the_cache_refuses(orch_lib):
                 call()
 
 
-@pytest.mark.parametrize("bad", [dict(B=0), dict(heads=0), dict(n_q=-1), dict(n_kv=0), dict(d=0), dict(d=40), dict(dtype=7)])
+@pytest.mark.parametrize("bad", [dict(B=0), dict(heads=0), dict(n_q=-1), dict(n_kv=0), dict(d=0), dict(d=40), dict(dtype=7),
+                                 dict(n_q=2 ** 31 - 1), dict(n_kv=2 ** 31 - 1), dict(n_q=1 << 25), dict(B=40000)])
 def test_no_workspace_for_bad_shapes(orch_lib, bad):
     a = dict(B=1, heads=2, n_q=1, n_kv=4096, d=64, dtype=BF16) | bad
     assert orch_lib.attention_quantized_workspace_bytes(*a.values()) == 0
