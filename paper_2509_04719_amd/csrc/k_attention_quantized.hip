@@ -12,12 +12,13 @@
 // freely.  So there are four forms, chosen by an estimate of their time (`plan` below):
 //   prepared    many queries: the keys are widened once, fresh and cached together, into tiles in the workspace, and
 //               four waves of 32 queries load each tile straight to LDS.  d = 72, 2 x 16 heads: 6144 queries x
-//               16384 keys 960 us (966 TFLOP/s; 51 of it preparing), 1664 x 4096 87 us; d = 128, 2 x 8 heads,
+//               16384 keys 920-970 us (960-1005 TFLOP/s; 51 of it preparing), 1664 x 4096 85 us; d = 128, 2 x 8 heads,
 //               4096 x 4096 134 us (1027).
 //   NW = 4      without a workspace, or too few queries to pay for it: four waves of 32 queries share each tile, each
-//               widens a quarter of it.  384 x 4096, keys split 5 ways: 33 us and 6 for the parts.
-//   NW = 1      few queries: four waves have the same 32 queries and each a quarter of the keys, without a barrier.
-//               384 x 1024: 16.7 us; one query x 16384 keys (75 MB of cache): 24 us and 4 for the parts, 3.1 TB/s.
+//               widens a quarter of it.  d = 128, 2 x 8 heads, 45 x 2025, 12 workgroups a head: 12 us, 4 for the parts.
+//   NW = 1      few queries: four waves have the same 32 queries and each a quarter of the keys, without a barrier,
+//               K from memory straight to the products' operand (through LDS: 4% longer at d = 72, 20% at 80 to 128).
+//               384 x 1024 keys 16.2 us, 384 x 4096 37; one query x 16384 (75 MB of cache) 25 with its parts, 3 TB/s.
 //   fp32        the same on v_mfma_f32_32x32x2: 512 x 1024 keys, 4 heads of 32: 8.4 us.
 // With a workspace each may also split the keys of a query tile over workgroups; a merge kernel joins the parts.
 #include <cfloat>
@@ -70,34 +71,30 @@ struct Geo {
   static constexpr bool M32 = D % 32 == 0;       // PV on 32x32x16, else on 16x16x32
   static constexpr int NT = M32 ? D / 32 : NC;   // row tiles of O^T
   static constexpr int CPT = D / 8;              // 8-channel chunks of a token
-  // bytes of a K row, an odd number of 16-byte chunks; TRIM: without padding channels
-  static constexpr bool TRIM = PREP || NW == 1;
-  static constexpr int KP = TRIM ? (CPT | 1) * 16 : NC * 32 + 16;
-  // of a V row: an odd multiple of 32 (16-row reads) or 64 (32-row reads; at D = 64 a wave alone
-  // takes 160, some conflicts, for a second workgroup on the CU)
-  static constexpr int VP = !M32 ? NC * 32 : NW == 1 && D == 64 ? 160 : D * 2 % 128 == 64 ? D * 2 : D * 2 + 64;
+  // bytes of a K row, an odd number of 16-byte chunks; PREP: without padding channels; NW = 1 keeps no K in LDS
+  static constexpr int KP = NW == 1 ? 0 : PREP ? (CPT | 1) * 16 : NC * 32 + 16;
+  // of a V row: an odd multiple of 32 (16-row reads) or 64 (32-row reads)
+  static constexpr int VP = !M32 ? NC * 32 : D * 2 % 128 == 64 ? D * 2 : D * 2 + 64;
   // PREP: tiles as they lie in memory, KT bytes of K rows, then VT of V^T rows
   static constexpr int KT = BKV * KP, VT = PREP ? (M32 ? D : 16 * NT) * 128 : BKV * VP;
-  static constexpr int ZERO = TRIM && D % 16 ? (PREP ? 1024 : 128) : 0;   // zeros behind a K stage: channels past the last
+  static constexpr int ZERO = PREP && D % 16 ? 1024 : 0;   // zeros behind a K stage: channels past the last
   static constexpr bool ONES = PREP && !M32 && 16 * NT > D;        // row D of V^T is ones: O^T's row D is the sum
   static constexpr int ST = NW == 4 ? 2 : 1;     // stages: a wave alone needs no second one
   static constexpr int KS = KT + ZERO;           // a K stage
-  static constexpr int GROUP = ST * (KS + VT);
+  static constexpr int NO = M32 ? NT : (2 * NT + 3) / 4;           // 16-register blocks of O^T
+  static constexpr int GROUP = cmax(ST * (KS + VT), KG > 1 ? (NO * 16 + 2) * 256 : 0);   // (a group's part takes its tile's place)
   static_assert(KS % 128 == 0 && VT % 128 == 0, "the swizzle of V^T rows is an XOR of the address");
   static constexpr int LDS = KG * GROUP;
   static constexpr int THREADS = 64 * NW;        // that share a tile
   static constexpr int SL = (BKV * CPT + THREADS - 1) / THREADS;   // chunks of a thread, K and V each
-  
   static constexpr int WPE = NW == 1 && D == 128 ? 1 : PREP && D <= 80 ? 3 : 2;          // waves of a SIMD that registers allow
   static constexpr int WPC = cmin(WPE, 160 * 1024 / LDS);          // workgroups of a CU
   static constexpr bool EVEN = THREADS % CPT == 0;                 // a thread's chunks are THREADS / CPT keys apart
-  // NW = 1: lanes of a key, each with CPL chunks in a row, keys 64 / LPK apart
+  // NW = 1: V's lanes of a key, each with CPL chunks in a row, keys 64 / LPK apart
   static constexpr int LPK = D == 128 ? 4 : D == 64 || D == 80 || D == 96 ? 2 : 1;
   static constexpr int CPL = CPT / LPK;
   static constexpr int NE = NW == 1 ? LPK : SL;  // scales of a thread
   static constexpr bool AHEAD = NW == 4 && !PREP && D <= 96;       // tiles of fresh keys alone are fetched ahead too
-  static constexpr int NO = M32 ? NT : (2 * NT + 3) / 4;           // 16-register blocks of O^T
-  static_assert(KG == 1 || (NO * 16 + 2) * 256 <= GROUP, "a group's part fits its tile's place");
 };
 
 struct Split {
@@ -150,7 +147,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   // hold anything, they end in rows of O^T that nobody reads)
   if constexpr (G::ZERO > 0) {
     if (tid < G::ST) *reinterpret_cast<u32x4*>(smem + tid * G::KS + G::KT) = u32x4{0, 0, 0, 0};
-  } else if constexpr (D % 16 != 0) {
+  } else if constexpr (NW == 4 && D % 16 != 0) {
     for (int i = tid; i < G::ST * BKV; i += TH)
       *reinterpret_cast<u32x4*>(smem + (i / BKV) * G::KS + (i % BKV) * G::KP + 2 * D) = u32x4{0, 0, 0, 0};
   }
@@ -163,7 +160,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   auto vrow = [](int k) __attribute__((always_inline)) { return (k & 32) | (k & 4) << 2 | (k & 24) >> 1 | (k & 3); };
   constexpr int KS = TH / CPT;                              // EVEN: keys from slot to slot
   static_assert(NW == 1 || !G::EVEN || (KS & (KS - 1)) == 0, "a slot's rows are a constant away");
-  // A wave alone has LPK lanes for each key, with CPL neighbouring chunks: few scales a lane, rows a
+  // V of a wave alone: LPK lanes for each key, with CPL neighbouring chunks: few scales a lane, rows a
   // constant apart, at the price of loads that touch more lines of the tile than they take from them.
   constexpr bool ROW = NW == 1;
   constexpr int LPK = G::LPK, CPL = G::CPL, KR = 64 / LPK;  // ROW: keys between a lane's rows
@@ -185,7 +182,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   auto chunk_of = [&](auto isk_c, int i) __attribute__((always_inline)) {
     return ROW ? lane % LPK * CPL + i % CPL : i * TH + (decltype(isk_c)::value ? tid : vtid) - key_of(isk_c, i) * CPT;
   };
-  auto k_dst = [&](int i) __attribute__((always_inline)) { return ROW ? k_dst_[0] + i / CPL * KR * G::KP + i % CPL * 16 : G::EVEN ? k_dst_[0] + i * KS * G::KP : k_dst_[i]; };
+  auto k_dst = [&](int i) __attribute__((always_inline)) { return G::EVEN ? k_dst_[0] + i * KS * G::KP : k_dst_[i]; };
   auto v_dst = [&](int i) __attribute__((always_inline)) { return ROW ? v_dst_[0] + vrow(i / CPL * KR) * G::VP + i % CPL * 16 : G::EVEN ? v_dst_[0] + vrow(i * KS) * G::VP : v_dst_[i]; };
   // fresh V^T: slot i holds chunk vtid % 8 (8 keys) of channel vtid / 8 + i TH / 8
   const int vt_src = (vtid >> 3) * nf + (vtid & 7) * 8;
@@ -300,7 +297,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
 #pragma unroll
         for (int k = 0; k < BATCH; ++k)
           if (i0 + k < SL && on(isk_c, i0 + k))
-            *reinterpret_cast<u32x4*>(dst + (isk ? (ROW ? (tid + 64 * (i0 + k)) / CPT * G::KP + (tid + 64 * (i0 + k)) % CPT * 16 : k_dst(i0 + k)) : vt_dst(i0 + k))) = x[k];
+            *reinterpret_cast<u32x4*>(dst + (isk ? k_dst(i0 + k) : vt_dst(i0 + k))) = x[k];
       }
       return;
     }
@@ -388,14 +385,58 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     asm volatile("" ::: "memory");
   };
 
-  // this lane's query (B operand): channels 16 c + 8 h .. +8
+  // K of a wave alone goes straight to the A operand: lane (lc, h) reads half of the channels of key kperm(lc) of a half
+  // tile, 8 a chunk, from channel 8 NC h on (the order of the products' channels is free), and widens them there.  Fresh
+  // keys take the place of the cache's in their lanes.
+  struct KHalf {
+    u32x2 x[NC];
+    unsigned e;
+  };
+  const int kd_key = kperm(lc), kd_off = kd_key * D + h * 8 * NC;
+  auto k_load = [&](KHalf& r, int t, int sub) __attribute__((always_inline)) {
+    const int so = (t * BKV + 32 * sub) * D;
+#pragma unroll
+    for (int c = 0; c < NC; c += 2) {
+      if (c + 1 < NC) {
+        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk8, kd_off + 8 * c, so, 0));
+        r.x[c] = u32x2{x[0], x[1]};
+        r.x[cmin(c + 1, NC - 1)] = u32x2{x[2], x[3]};
+      } else {
+        r.x[c] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rk8, kd_off + 8 * c, so, 0));
+      }
+    }
+    r.e = __builtin_amdgcn_raw_buffer_load_b8(rke, kd_key, t * BKV + 32 * sub, 0);
+  };
+  auto k_make = [&](const KHalf& r, int t, int sub, int type, bf16x8(&k)[NC]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      u32x2 x = r.x[c];
+      // (the upper half's last chunk is past the channels: it read the next key's)
+      if (CPT % 2 && c == NC - 1) x = h ? u32x2{0, 0} : x;
+      k[c] = __builtin_bit_cast(bf16x8, widen(x[0], x[1], r.e));
+    }
+    if (type != kStale) {
+      const int key = t * BKV + 32 * sub + kd_key - fb;
+      if ((unsigned)key < (unsigned)nf) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          // (at the last chunk of the upper half: no scale of the cache's either)
+          if (CPT % 2 && c == NC - 1 && h) k[c] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+          else k[c] = *reinterpret_cast<const bf16x8*>(kf + (size_t)key * D + h * 8 * NC + 8 * c);
+        }
+      }
+    }
+  };
+
+  // this lane's query (B operand): channels 16 c + 8 h .. +8, or as K's
   const int qrow = min(q0 + lc, p.n_q - 1);
   const bf16* qp = reinterpret_cast<const bf16*>(p.q) + (((size_t)b * p.heads + head) * p.n_q + qrow) * D;
   bf16x8 qf[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    if (16 * c + 8 * h < D) {
-      qf[c] = *reinterpret_cast<const bf16x8*>(qp + 16 * c + 8 * h);
+    const int ch = ROW ? 8 * (NC * h + c) : 16 * c + 8 * h;
+    if (ch < D) {
+      qf[c] = *reinterpret_cast<const bf16x8*>(qp + ch);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) qf[c][e] = (bf16)0.0f;
@@ -515,9 +556,10 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   };
   // One 32-key half: exponentials of its scores sc between the MFMAs of the next half's scores
   // (NEXT: tile nt, half nsub, into sn) and of the previous half's O^T += V^T P^T (pp; V
-  // of tile pt, half psub).  Its probabilities go to pc.
+  // of tile pt, half psub).  Its probabilities go to pc.  A wave alone has K of that half in kh (kind: of its tile),
+  // and reads that of tile nt + 1.
   auto step = [&](auto next_c, bool first, f32x16& sc, int nt, int nsub, f32x16& sn, int pt, int psub, bool vt,
-                  bf16x8(&pp)[2], bf16x8(&pc)[2]) __attribute__((always_inline)) {
+                  bf16x8(&pp)[2], bf16x8(&pc)[2], KHalf& kh, int kind) __attribute__((always_inline)) {
     constexpr bool NEXT = decltype(next_c)::value;
     constexpr int VF = M32 ? 2 : 1;
     bf16x8 vp[VF][NT], kn[NEXT ? NC : 1];
@@ -531,13 +573,16 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
       }
     };
     v_frags(0);
-    if constexpr (NEXT) {
+    if constexpr (NEXT && ROW) {
+      k_make(kh, nt, nsub, kind, kn);
+      k_load(kh, min(nt + 1, te - 1), nsub);
+    } else if constexpr (NEXT) {
 #pragma unroll
       for (int c = 0; c < NC / 2; ++c) kn[c] = k_frag(nt, nsub, c);
     }
     // (the rest between the MFMAs of the first chunk)
     auto later = [&]() __attribute__((always_inline)) {
-      if constexpr (NEXT) {
+      if constexpr (NEXT && !ROW) {
 #pragma unroll
         for (int c = NC / 2; c < NC; ++c) kn[c] = k_frag(nt, nsub, c);
       }
@@ -664,15 +709,15 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     }
   };
 
-  // Between the halves of tile t (behind a barrier where waves share tiles) K of tile t + KA
-  // takes the place of tile t's, and V of t + VA that of t - 1's; their loads were issued a whole
-  // tile earlier, into registers.  Two stages: KA = 2, VA = 1; one: KA = 1, VA = 0.
-  constexpr int KA = G::ST, VA = G::ST - 1;
+  // Between the halves of tile t, behind a barrier, K of tile t + 2 takes the place of tile t's, and V of t + 1
+  // that of t - 1's (a wave alone: V of t); their loads were issued a whole tile earlier, into registers.
+  constexpr int VA = G::ST - 1;
   // ty1 .. ty4: kinds of tiles t .. t + 3; vt0: tile t - 1 holds V^T
   auto tile = [&](int t) __attribute__((always_inline)) { return min(t, te - 1); };
   if (KG == 1 || t0 < te) {
     int ty1 = PREP ? 0 : type_of(t0), ty2 = PREP ? 0 : type_of(tile(t0 + 1)), ty3 = PREP ? 0 : type_of(tile(t0 + 2));
     Raw kr, vr;
+    KHalf kh0, kh1;
     if constexpr (PREP) {
       issue(kK, t0);
       issue(kV, t0);
@@ -688,16 +733,24 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
       load(kV, vr, tile(t0 + 1), ty2);
       if (t0 + 1 < te) store(kK, kr1, t0 + 1, ty2);
     } else {
-      load(kK, kr, t0, ty1);
+      k_load(kh0, t0, 0);
+      k_load(kh1, t0, 1);
       load(kV, vr, t0, ty1);
-      store(kK, kr, t0, ty1);
-      load(kK, kr, tile(t0 + 1), ty2);
     }
     tiles_sync();
     f32x16 s0, s1;
-    s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(t0, 0, 0), qf[0], zero16, 0, 0, 0);
+    {
+      bf16x8 k0[NC];
+      if constexpr (ROW) {
+        k_make(kh0, t0, 0, ty1, k0);
+        k_load(kh0, tile(t0 + 1), 0);
+      } else {
 #pragma unroll
-    for (int c = 1; c < NC; ++c) s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(t0, 0, c), qf[c], s0, 0, 0, 0);
+        for (int c = 0; c < NC; ++c) k0[c] = k_frag(t0, 0, c);
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c) s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0[c], qf[c], c == 0 ? zero16 : s0, 0, 0, 0);
+    }
     bf16x8 pa[2], pb[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -707,20 +760,22 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     int t = t0;
     for (; t + 1 < te; ++t) {
       const bool vt1 = ty1 == kFresh;
-      step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
+      step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb, kh1, ty1);
       tiles_sync();
       if constexpr (PREP) {
         if (t + 2 < te) issue(kK, t + 2);
         issue(kV, t + 1);
-        step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa);
+        step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa, kh0, ty2);
         continue;
       }
       const int t3 = tile(t + 3), ty4 = type_of(t3);
-      if (t + KA < te) store(kK, kr, t + KA, G::ST == 2 ? ty3 : ty2);
-      load(kK, kr, G::ST == 2 ? t3 : tile(t + 2), G::ST == 2 ? ty4 : ty3);
+      if constexpr (!ROW) {
+        if (t + 2 < te) store(kK, kr, t + 2, ty3);
+        load(kK, kr, t3, ty4);
+      }
       store(kV, vr, t + VA, G::ST == 2 ? ty2 : ty1);
       load(kV, vr, tile(t + VA + 1), G::ST == 2 ? ty3 : ty2);
-      step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa);
+      step(std::true_type{}, false, s1, t + 1, 0, s0, t, 0, vt1, pb, pa, kh0, ty2);
       vt0 = vt1;
       ty1 = ty2;
       ty2 = ty3;
@@ -728,11 +783,11 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     }
     const bool vt1 = ty1 == kFresh;
     mask(t, 0, s0);
-    step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb);
+    step(std::true_type{}, t == t0, s0, t, 1, s1, t == t0 ? t : t - 1, t == t0 ? 0 : 1, vt0, pa, pb, kh1, ty1);
     tiles_sync();      // V of the last tile came since the last one
     if constexpr (G::ST == 1) store(kV, vr, t, ty1);
     mask(t, 1, s1);
-    step(std::false_type{}, false, s1, 0, 0, s0, t, 0, vt1, pb, pa);
+    step(std::false_type{}, false, s1, 0, 0, s0, t, 0, vt1, pb, pa, kh0, kStale);
     p_swap(pa);
     static_for<0, NT>([&](auto tc) {
       constexpr int tt = decltype(tc)::value;
@@ -1215,10 +1270,10 @@ hipError_t launch_merge(const AttnQParams& p, const Split& sp, int rows, hipStre
 // The plan of a call: the variant (tiles prepared or not, query groups of a workgroup) and the number ns
 // of workgroups that share a query tile's keys, by the least estimated time.  In us, at d = 72 (other head
 // sizes scale a tile by 0.5 + d / 140): a workgroup starts and ends in 4.5; a 64-key tile of a workgroup
-// takes the `tile` below, by the workgroups on its CU; parts take 3.5 and their bytes, written and read, at
+// takes the `tile` below, by the workgroups on its CU; parts take 4.5 and their bytes, written and read, at
 // 5 TB/s; preparing 2.5 and 5.5 ns a tile.  Measured against the estimate (2 x 16 heads, d = 72): 384
-// queries x 4096 keys on NW = 4 / ns = 1, 2, 5: 88 / 57 / 39 (88 / 52 / 39 estimated), on NW = 1 / ns = 1 43
-// (43), prepared / ns = 5 39 (44); 1664 x 1024 on NW = 4 / ns = 1, 2 37 / 52 (34 / 54), prepared / 1 32 (29).
+// queries x 4096 keys on NW = 4 / ns = 1, 2, 5: 88 / 57 / 39 (88 / 53 / 40 estimated), on NW = 1 / ns = 1 37
+// (39), prepared / ns = 5 39 (45); 1664 x 1024 on NW = 4 / ns = 1, 2 37 / 52 (34 / 55), prepared / 1 32 (29).
 struct Plan {
   int nw, ns, prep;
   size_t tiles;
@@ -1247,7 +1302,7 @@ void consider(Plan* best, int nw, int prep, long long pairs, int n_q, int rows, 
     const long long w = units * ns, per_cu = (w + 255) / 256, rounds = (per_cu + wpc - 1) / wpc;
     const int c = (int)(per_cu < wpc ? per_cu : wpc);
     const double cost = fixed + (double)rounds * (4.5 + ceil_div(nkt, groups * ns) * tile[c - 1] * scale) +
-                        (ns > 1 ? 3.5 + (double)w * rows * d * 8 / 5e6 : 0.0);
+                        (ns > 1 ? 4.5 + (double)w * rows * d * 8 / 5e6 : 0.0);
     if (cost < best->cost) *best = {nw, ns, prep, (size_t)units, cost};
   }
 }
@@ -1262,9 +1317,9 @@ Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype, bool workspace)
     if (dtype == kBF16) {
       const int nkt = ceil_div(n_kv, BKV);
       consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, Geo<D, 4>::WPC, {1.3, 1.85, 0}, 0.0, d, max_ns);
-      // (its longer straight code is read once by every CU: 1 us at d = 64, 7 at d = 128; two workgroups on a
-      // CU share its LDS best at small d: 2 x 8 heads, 1000 queries x 4096 keys at d = 32 in 28.6 us, prepared 33.9)
-      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.8 : 1.33, 1.8 + D / 120.0, 0}, D <= 64 ? D / 64 : 1.0 + (D - 64) * 0.09, d, max_ns);
+      // (its longer straight code is read once by every CU: 1 us at d = 64, 7 at d = 128; 2 x 8
+      // heads, 1000 queries x 4096 keys at d = 32, 64: 27, 41 us, prepared 34, 40)
+      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.35 : 1.25, 2.0, 0}, D <= 64 ? D / 64 : 1.0 + (D - 64) * 0.09, d, max_ns);
       if (workspace && (long long)nkt * (Geo<D, 4, true>::KT + Geo<D, 4, true>::VT) < (1ll << 31))
         consider(&r, 4, 1, pairs, n_q, 128, 1, nkt, Geo<D, 4, true>::WPC, {0.8, 1.15, 1.7},
                  2.5 + 0.0055 * (double)(pairs * nkt) * (0.5 + d / 140.0), d, max_ns);
