@@ -15,7 +15,8 @@
 //               16384 keys 920-970 us (960-1005 TFLOP/s; 51 of it preparing), 1664 x 4096 85 us; d = 128, 2 x 8 heads,
 //               4096 x 4096 134 us (1027).
 //   NW = 4      without a workspace, or too few queries to pay for it: four waves of 32 queries share each tile, each
-//               widens a quarter of it.  d = 128, 2 x 8 heads, 45 x 2025, 12 workgroups a head: 12 us, 4 for the parts.
+//               widens a quarter of it.  1664 x 1024 keys 34 us; d = 128, 2 x 8 heads, 45 x 2025, keys split 12 ways:
+//               12 us and 4 for the parts (as much as on NW = 1, split 8 ways).
 //   NW = 1      few queries: four waves have the same 32 queries and each a quarter of the keys, without a barrier,
 //               K from memory straight to the products' operand (through LDS: 4% longer at d = 72, 20% at 80 to 128).
 //               384 x 1024 keys 16.2 us, 384 x 4096 37; one query x 16384 (75 MB of cache) 25 with its parts, 3 TB/s.
@@ -82,7 +83,8 @@ struct Geo {
   static constexpr int ST = NW == 4 ? 2 : 1;     // stages: a wave alone needs no second one
   static constexpr int KS = KT + ZERO;           // a K stage
   static constexpr int NO = M32 ? NT : (2 * NT + 3) / 4;           // 16-register blocks of O^T
-  static constexpr int GROUP = cmax(ST * (KS + VT), KG > 1 ? (NO * 16 + 2) * 256 : 0);   // (a group's part takes its tile's place)
+  // (a group's part takes its tile's place)
+  static constexpr int GROUP = cmax(ST * (KS + VT), KG > 1 ? (NO * 16 + 2) * 256 : 0);
   static_assert(KS % 128 == 0 && VT % 128 == 0, "the swizzle of V^T rows is an XOR of the address");
   static constexpr int LDS = KG * GROUP;
   static constexpr int THREADS = 64 * NW;        // that share a tile
@@ -1302,7 +1304,7 @@ void consider(Plan* best, int nw, int prep, long long pairs, int n_q, int rows, 
     const long long w = units * ns, per_cu = (w + 255) / 256, rounds = (per_cu + wpc - 1) / wpc;
     const int c = (int)(per_cu < wpc ? per_cu : wpc);
     const double cost = fixed + (double)rounds * (4.5 + ceil_div(nkt, groups * ns) * tile[c - 1] * scale) +
-                        (ns > 1 ? 4.5 + (double)w * rows * d * 8 / 5e6 : 0.0);
+                        (ns > 1 ? 4.5 + (double)(pairs * n_q) * ns * d * 8 / 5e6 : 0.0);
     if (cost < best->cost) *best = {nw, ns, prep, (size_t)units, cost};
   }
 }

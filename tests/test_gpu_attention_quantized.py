@@ -107,6 +107,16 @@ def test_many_heads_and_queries(orch_lib, split, d, n_q, N, fb, nf):
     check(run(orch_lib, "bf16", q, v8, e8, fk, fv, fb, split), "bf16", q, K, V)
 
 
+@pytest.mark.parametrize("d", [32, 64, 72, 80, 96, 128])
+def test_keys_laid_out_and_split(orch_lib, d):
+    """Tiles laid out once, and their keys over several workgroups."""
+    n_q, N, fb, nf = 1500, 2025, 333, 900
+    print(f"\n[d {d} n_q {n_q} n_kv {N} fresh {fb}+{nf}]", flush=True)
+    rng = np.random.default_rng(d + n_q + N)
+    q, v8, e8, fk, fv, K, V = make(rng, "bf16", 2, 6, d, n_q, N, fb, nf)
+    check(run(orch_lib, "bf16", q, v8, e8, fk, fv, fb), "bf16", q, K, V)
+
+
 @pytest.mark.parametrize("split", [True, False])
 @pytest.mark.parametrize("d", [64, 72, 128])
 @pytest.mark.parametrize("ramp,shift", [(12.0, 0.0), (0.0, 48.0), (0.0, 2.0 ** 15)])
