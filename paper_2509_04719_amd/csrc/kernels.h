@@ -216,7 +216,7 @@ struct AttnQParams {
   int fresh_begin, n_fresh;
   int B, heads, n_q, d;
   void* out;                  // T [B][n_q][heads * d]
-  void* ws;                   // parts of queries whose keys are split, see the .hip
+  void* ws;                   // prepared tiles, then the parts of split keys, see the .hip
   size_t ws_bytes;
 };
 size_t attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int d, int dtype);
