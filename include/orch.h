@@ -450,8 +450,8 @@ int orch_op_kv_dequantize(const orch_quantized_kv* cache, int tok_offset, void* 
  * n_fresh) from kv_fresh (T, as there), the others from the cache.  q, out and the
  * branch layout as there.  Any number of keys and queries and any band runs on
  * the matrix cores.  Scores, their running max and sum and the output are fp32; in
- * bf16 the probabilities are rounded once for the PV product (Q is not rounded
- * again) and the output once.  workspace: device memory (16-byte aligned) of at
+ * bf16 16 significant bits of a probability reach the PV product (Q is not rounded
+ * again), and the output is rounded once.  workspace: device memory (16-byte aligned) of at
  * least orch_attention_quantized_workspace_bytes() bytes, one call's at a time,
  * lets few queries split the keys over more workgroups, and many queries have the
  * keys widened once for all; NULL (or fewer bytes) runs without either.  The

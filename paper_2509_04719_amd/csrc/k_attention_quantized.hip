@@ -7,19 +7,24 @@
 // power of two is a bf16 number), and the band's own keys take the place of the cache's there.  Matrix products in 8
 // bits would need Q and the probabilities in 8 bits too.
 //
+// The bf16 products take a probability as two bf16, p = hi + lo, two MFMAs for each V fragment: 16 significant bits of
+// it, so that the output's rounding is the only error that shows (2-norm against 64 bits 1.66e-3, as in 32 bits
+// throughout).  Rounded to one bf16 it would be 2.33e-3; the second term and its products cost 92 -> 117 us at 1664
+// queries x 4096 keys and 937 -> 1300 at 6144 x 16384 (2 x 16 heads of 72), 16 -> 19 at 384 x 1024.
+//
 // Bound by the matrix cores with many queries (4 B heads n_q n_kv d flops), else by a wave's own chain: widening a
 // key costs the VALU as much as a wave's softmax of it, and VALU and MFMA instructions of a SIMD do not overlap
 // freely.  So there are four forms, chosen by an estimate of their time (`plan` below):
 //   prepared    many queries: the keys are widened once, fresh and cached together, into tiles in the workspace, and
 //               four waves of 32 queries load each tile straight to LDS.  d = 72, 2 x 16 heads: 6144 queries x
-//               16384 keys 920-970 us (960-1005 TFLOP/s; 51 of it preparing), 1664 x 4096 85 us; d = 128, 2 x 8 heads,
-//               4096 x 4096 134 us (1027).
+//               16384 keys 1300-1370 us (677-714 TFLOP/s, every product counted once; 51 of it preparing), 1664 x 4096
+//               117-122 us; d = 128, 2 x 8 heads, 4096 x 4096 185 us (743).
 //   NW = 4      without a workspace, or too few queries to pay for it: four waves of 32 queries share each tile, each
-//               widens a quarter of it.  1664 x 1024 keys 34 us; d = 128, 2 x 8 heads, 45 x 2025, keys split 12 ways:
-//               12 us and 4 for the parts (as much as on NW = 1, split 8 ways).
+//               widens a quarter of it.  1664 x 1024 keys 43 us; d = 128, 2 x 8 heads, 45 x 2025, keys split 12 ways:
+//               19 us with the parts.
 //   NW = 1      few queries: four waves have the same 32 queries and each a quarter of the keys, without a barrier,
 //               K from memory straight to the products' operand (through LDS: 4% longer at d = 72, 20% at 80 to 128).
-//               384 x 1024 keys 16.2 us, 384 x 4096 37; one query x 16384 (75 MB of cache) 25 with its parts, 3 TB/s.
+//               384 x 1024 keys 18 us, 384 x 4096 45; one query x 16384 keys of 8 heads of 72 13.4 with its parts.
 //   fp32        the same on v_mfma_f32_32x32x2: 512 x 1024 keys, 4 heads of 32: 8.4 us.
 // With a workspace each may also split the keys of a query tile over workgroups; a merge kernel joins the parts.
 #include <cfloat>
@@ -497,6 +502,24 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
       for (int i = 0; i < 4; ++i) oo[f / 4][4 * (f % 4) + i] = r[i];
     }
   };
+  // The probabilities of a half, p = hi + lo: hi the top 16 bits of p, lo what is left of p (1 + 2^-23) as a bf16.  Both
+  // are positive, so that an infinite V gives hi V + lo V = V, not a NaN.
+  struct Prob {
+    bf16x8 hi[2], lo[2];
+  };
+  auto p_set = [](Prob& p, int j, int pair, float x0, float x1) __attribute__((always_inline)) {
+    constexpr float kUp = 1.0f + 0x1p-23f;
+    const unsigned u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
+    u32x4 a = __builtin_bit_cast(u32x4, p.hi[j]);
+    a[pair] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+    p.hi[j] = __builtin_bit_cast(bf16x8, a);
+    p.lo[j][2 * pair] = (bf16)fmaf(x0, kUp, -__uint_as_float(u0 & 0xffff0000u));
+    p.lo[j][2 * pair + 1] = (bf16)fmaf(x1, kUp, -__uint_as_float(u1 & 0xffff0000u));
+  };
+  auto p_zero = [](Prob& p) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) p.hi[j] = p.lo[j] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+  };
   // the probabilities of a half from the score layout (chunk ci, lane half h: keys 16 ci + 8 h .. +8
   // of query lane & 31) to the B operand of the 16x16x32 MFMA (pp[j]: keys 8 (lane >> 4) .. +8 of
   // query 16 j + (lane & 15)): the 32-lane swap, then the 16-lane swap
@@ -561,7 +584,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   // of tile pt, half psub).  Its probabilities go to pc.  A wave alone has K of that half in kh (kind: of its tile),
   // and reads that of tile nt + 1.
   auto step = [&](auto next_c, bool first, f32x16& sc, int nt, int nsub, f32x16& sn, int pt, int psub, bool vt,
-                  bf16x8(&pp)[2], bf16x8(&pc)[2], KHalf& kh, int kind) __attribute__((always_inline)) {
+                  Prob& pp, Prob& pc, KHalf& kh, int kind) __attribute__((always_inline)) {
     constexpr bool NEXT = decltype(next_c)::value;
     constexpr int VF = M32 ? 2 : 1;
     bf16x8 vp[VF][NT], kn[NEXT ? NC : 1];
@@ -591,7 +614,8 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
       if constexpr (M32) v_frags(1);
     };
     bool gone = false;
-    p_swap(pp);
+    p_swap(pp.hi);
+    p_swap(pp.lo);
     float cm = scale, ms = m_run;
     if (__builtin_expect(careful, 0)) {
 #pragma clang fp contract(off)
@@ -605,16 +629,17 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
         if constexpr (M32) v_frags(1);
         static_for<0, NT>([&](auto tc) {
           constexpr int tt = decltype(tc)::value;
-          pv(tc, std::integral_constant<int, 0>{}, vp[0][tt], pp[0]);
-          pv(tc, std::integral_constant<int, 1>{}, vp[VF - 1][tt], pp[1]);
+          pv(tc, std::integral_constant<int, 0>{}, vp[0][tt], pp.hi[0]);
+          pv(tc, std::integral_constant<int, 1>{}, vp[VF - 1][tt], pp.hi[1]);
+          pv(tc, std::integral_constant<int, 0>{}, vp[0][tt], pp.lo[0]);
+          pv(tc, std::integral_constant<int, 1>{}, vp[VF - 1][tt], pp.lo[1]);
         });
       }
+      p_zero(pp);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        pp[0][e] = pp[1][e] = (bf16)0.0f;
+      for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int tt = 0; tt < NT; ++tt) vp[0][tt][e] = (bf16)0.0f;
-      }
       gone = true;
       m_run = mn;
       l_run *= alpha;
@@ -639,10 +664,12 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
         constexpr int g = decltype(gc)::value;
         constexpr bool is_pv = g < 2 * NB ? g % 2 == 0 : NT > NSM;
         constexpr int idx = g < 2 * NB ? g / 2 : g - NB;
-        if constexpr (is_pv)
-          pv(std::integral_constant<int, idx>{}, cc, vp[M32 ? ci : 0][idx], pp[ci]);
-        else
+        if constexpr (is_pv) {
+          pv(std::integral_constant<int, idx>{}, cc, vp[M32 ? ci : 0][idx], pp.hi[ci]);
+          pv(std::integral_constant<int, idx>{}, cc, vp[M32 ? ci : 0][idx], pp.lo[ci]);
+        } else {
           sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kn[c0 + idx], qf[c0 + idx], c0 + idx == 0 ? zero16 : sn, 0, 0, 0);
+        }
         if constexpr (ci == 0 && g == 0) later();
         if constexpr (M32 && ci == 0 && g == NM - 1) {
           if (__builtin_expect(gone, 0)) {
@@ -656,18 +683,16 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
           constexpr int pr = decltype(pc_)::value;
           float x[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(fmaf(sc[8 * ci + 2 * pr + e], cm, -ms));
-            pc[ci][2 * pr + e] = (bf16)x[e];
-          }
+          for (int e = 0; e < 2; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(sc[8 * ci + 2 * pr + e], cm, -ms));
+          p_set(pc, ci, pr, x[0], x[1]);
         });
         __builtin_amdgcn_sched_barrier(0);
       });
-      asm volatile("" ::"v"(pc[ci]));   // (keeps the exponentials here, between the MFMAs)
+      asm volatile("" ::"v"(pc.hi[ci]), "v"(pc.lo[ci]));   // (keeps the exponentials here, between the MFMAs)
     });
     __builtin_amdgcn_s_setprio(0);
     // a probability of 2 or more, or not finite: bf16 exponent bit 7
-    const u32x4 a = __builtin_bit_cast(u32x4, pc[0]), c = __builtin_bit_cast(u32x4, pc[1]);
+    const u32x4 a = __builtin_bit_cast(u32x4, pc.hi[0]), c = __builtin_bit_cast(u32x4, pc.hi[1]);
     const unsigned any = a[0] | a[1] | a[2] | a[3] | c[0] | c[1] | c[2] | c[3];
     if (__builtin_expect(__any((any & 0x40004000u) != 0u), 0)) {
 #pragma clang fp contract(off)
@@ -684,21 +709,28 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float s = sc[8 * j + e] * cm;
-          pc[j][e] = (bf16)__builtin_amdgcn_exp2f(huge ? s - ms : fmaf(sc[8 * j + e], cm, -ms));
+        for (int pr = 0; pr < 4; ++pr) {
+          float x[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float score = sc[8 * j + 2 * pr + e], s = score * cm;
+            x[e] = __builtin_amdgcn_exp2f(huge ? s - ms : fmaf(score, cm, -ms));
+          }
+          p_set(pc, j, pr, x[0], x[1]);
         }
       careful = needs_care();
     }
     if constexpr (G::ONES) return;
-    // the sum of the rounded probabilities, in fp32
+    // the sum of what the products take, in fp32
     const bf16x2 one2 = {(bf16)1.0f, (bf16)1.0f};
-    const u32x4 pa = __builtin_bit_cast(u32x4, pc[0]), pb = __builtin_bit_cast(u32x4, pc[1]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const unsigned x = pa[e], y = pb[e];
-      l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), one2, l_run, false);
-      l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, y), one2, l_run, false);
+    for (int k = 0; k < 4; ++k) {
+      const u32x4 w = __builtin_bit_cast(u32x4, k < 2 ? pc.hi[k] : pc.lo[k - 2]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const unsigned two = w[e];
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), one2, l_run, false);
+      }
     }
   };
   // keys past the last: no score
@@ -753,11 +785,8 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
 #pragma unroll
       for (int c = 0; c < NC; ++c) s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0[c], qf[c], c == 0 ? zero16 : s0, 0, 0, 0);
     }
-    bf16x8 pa[2], pb[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pa[j][e] = (bf16)0.0f;
+    Prob pa, pb;
+    p_zero(pa);
     bool vt0 = ty1 == kFresh;
     int t = t0;
     for (; t + 1 < te; ++t) {
@@ -790,11 +819,16 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     if constexpr (G::ST == 1) store(kV, vr, t, ty1);
     mask(t, 1, s1);
     step(std::false_type{}, false, s1, 0, 0, s0, t, 0, vt1, pb, pa, kh0, kStale);
-    p_swap(pa);
+    p_swap(pa.hi);
+    p_swap(pa.lo);
     static_for<0, NT>([&](auto tc) {
       constexpr int tt = decltype(tc)::value;
-      pv(tc, std::integral_constant<int, 0>{}, PREP || vt1 ? vt_frag(t, 1, tt, 0) : v_frag(t, 1, tt, 0), pa[0]);
-      pv(tc, std::integral_constant<int, 1>{}, PREP || vt1 ? vt_frag(t, 1, tt, 1) : v_frag(t, 1, tt, 1), pa[1]);
+      static_for<0, 2>([&](auto jc) {
+        constexpr int j = decltype(jc)::value;
+        const bf16x8 v = PREP || vt1 ? vt_frag(t, 1, tt, j) : v_frag(t, 1, tt, j);
+        pv(tc, jc, v, pa.hi[j]);
+        pv(tc, jc, v, pa.lo[j]);
+      });
     });
   }
   if constexpr (G::ONES) {
@@ -1271,11 +1305,13 @@ hipError_t launch_merge(const AttnQParams& p, const Split& sp, int rows, hipStre
 // ---------------------------------------------------------------------------
 // The plan of a call: the variant (tiles prepared or not, query groups of a workgroup) and the number ns
 // of workgroups that share a query tile's keys, by the least estimated time.  In us, at d = 72 (other head
-// sizes scale a tile by 0.5 + d / 140): a workgroup starts and ends in 4.5; a 64-key tile of a workgroup
-// takes the `tile` below, by the workgroups on its CU; parts take 4.5 and their bytes, written and read, at
-// 5 TB/s; preparing 2.5 and 5.5 ns a tile.  Measured against the estimate (2 x 16 heads, d = 72): 384
-// queries x 4096 keys on NW = 4 / ns = 1, 2, 5: 88 / 57 / 39 (88 / 53 / 40 estimated), on NW = 1 / ns = 1 37
-// (39), prepared / ns = 5 39 (45); 1664 x 1024 on NW = 4 / ns = 1, 2 37 / 52 (34 / 55), prepared / 1 32 (29).
+// sizes scale a tile by 0.5 + d / 140): a workgroup starts and ends in 4; a 64-key tile of a workgroup
+// takes the `tile` below, by the workgroups on its CU; parts take 5 and their bytes, written and read, at
+// 5 TB/s; preparing 2.5 and 5.5 ns a tile.  Fitted to 16 shapes at each head size, every variant and split: the
+// chosen one takes 1.7% longer than the best of them in the mean, 19% at most (32 heads of 32, 384 queries x 4096
+// keys).  Measured against the estimate (2 x 16 heads, d = 72): 384 queries x 4096 keys on NW = 4 / ns = 1, 2,
+// 5: 104 / 66 / 44 (105 / 62 / 43 estimated), on NW = 1 / ns = 1 45 (44), prepared / ns = 5 45 (49); 1664 x 1024 on
+// NW = 4 / ns = 1, 2 43 / 57 (37 / 59), prepared / 1 41 (32).
 struct Plan {
   int nw, ns, prep;
   size_t tiles;
@@ -1303,8 +1339,8 @@ void consider(Plan* best, int nw, int prep, long long pairs, int n_q, int rows, 
   for (int ns = 1; ns <= max_ns && ns <= ceil_div(nkt, groups); ns += ns < 8 ? 1 : ns / 4) {
     const long long w = units * ns, per_cu = (w + 255) / 256, rounds = (per_cu + wpc - 1) / wpc;
     const int c = (int)(per_cu < wpc ? per_cu : wpc);
-    const double cost = fixed + (double)rounds * (4.5 + ceil_div(nkt, groups * ns) * tile[c - 1] * scale) +
-                        (ns > 1 ? 4.5 + (double)(pairs * n_q) * ns * d * 8 / 5e6 : 0.0);
+    const double cost = fixed + (double)rounds * (4.0 + ceil_div(nkt, groups * ns) * tile[c - 1] * scale) +
+                        (ns > 1 ? 5.0 + (double)(pairs * n_q) * ns * d * 8 / 5e6 : 0.0);
     if (cost < best->cost) *best = {nw, ns, prep, (size_t)units, cost};
   }
 }
@@ -1318,12 +1354,12 @@ Plan plan(int B, int heads, int n_q, int n_kv, int d, int dtype, bool workspace)
     constexpr int D = decltype(dc)::value;
     if (dtype == kBF16) {
       const int nkt = ceil_div(n_kv, BKV);
-      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, Geo<D, 4>::WPC, {1.3, 1.85, 0}, 0.0, d, max_ns);
-      // (its longer straight code is read once by every CU: 1 us at d = 64, 7 at d = 128; 2 x 8
-      // heads, 1000 queries x 4096 keys at d = 32, 64: 27, 41 us, prepared 34, 40)
-      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.35 : 1.25, 2.0, 0}, D <= 64 ? D / 64 : 1.0 + (D - 64) * 0.09, d, max_ns);
+      consider(&r, 4, 0, pairs, n_q, 128, 1, nkt, Geo<D, 4>::WPC, {1.5, 2.05, 0}, 0.0, d, max_ns);
+      // (its longer straight code is read once by every CU: 0.7 us at d = 64, 4.8 at d = 128; 2 x 8
+      // heads, 1000 queries x 4096 keys at d = 32, 64: 30, 42 us, prepared 38, 47)
+      consider(&r, 1, 0, pairs, n_q, 32, 4, nkt, Geo<D, 1>::WPC, {D == 128 ? 1.6 : 1.3, 2.4, 0}, D <= 64 ? D * 0.011 : 0.7 + (D - 64) * 0.063, d, max_ns);
       if (workspace && (long long)nkt * (Geo<D, 4, true>::KT + Geo<D, 4, true>::VT) < (1ll << 31))
-        consider(&r, 4, 1, pairs, n_q, 128, 1, nkt, Geo<D, 4, true>::WPC, {0.8, 1.15, 1.7},
+        consider(&r, 4, 1, pairs, n_q, 128, 1, nkt, Geo<D, 4, true>::WPC, {1.2, 1.4, 2.4},
                  2.5 + 0.0055 * (double)(pairs * nkt) * (0.5 + d / 140.0), d, max_ns);
     } else {
       // 32-key tiles; the matrix pipe of a SIMD is one wave's at a time

@@ -289,3 +289,19 @@ def test_repeated_calls_give_the_same_bits(orch_lib, dtype, d):
         first = run(orch_lib, dtype, q, v8, e8, fk, fv, fb)
         for _ in range(9):
             np.testing.assert_array_equal(run(orch_lib, dtype, q, v8, e8, fk, fv, fb), first)
+
+
+@pytest.mark.parametrize("d", [32, 64, 72, 80, 96, 128])
+@pytest.mark.parametrize("B,heads,n_q,N,fb,nf", [(2, 8, 96, 256, 80, 96), (2, 8, 45, 2025, 1035, 45), (2, 16, 520, 330, 60, 100),
+                                                 (2, 16, 1100, 600, 77, 300)])
+def test_error_is_the_rounding_of_the_output(orch_lib, d, B, heads, n_q, N, fb, nf):
+    """bf16: probabilities reach the products with 16 bits (off by 2^-17), so that the output's own rounding is what is
+    left.  Half a step of 2^-7 of a value's power of two is evenly spread: 2^-8 / sqrt(3) over the value's mantissa,
+    0.736 of it in the 2-norm over evenly spread exponents, 1.66e-3, 1.70e-3 at most for normal outputs of any size
+    (probabilities rounded to bf16 once add as much again: 2.35e-3).  24000 outputs and more: 2% either way."""
+    rng = np.random.default_rng(d + n_q + N)
+    q, v8, e8, fk, fv, K, V = make(rng, "bf16", B, heads, d, n_q, N, fb, nf)
+    for split in (True, False):
+        err = rel_l2(run(orch_lib, "bf16", q, v8, e8, fk, fv, fb, split), ok.attention(q, K, V))
+        print(f"\n[d {d} {heads} heads, {n_q} queries x {N} keys, split {split}] {err:.3e}", flush=True)
+        assert err <= 1.75e-3
