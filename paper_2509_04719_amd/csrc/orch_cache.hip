@@ -104,6 +104,7 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
   long long tokens = 1;
   int channels = 0, pair = 0;
   if (!(axes->theta > 0.0) || !std::isfinite(axes->theta)) return fail("theta must be finite and > 0");
+  const long double log_theta = std::log((long double)axes->theta);
   for (int a = 0; a < 3; ++a) {
     const int ch = axes->channels[a], ext = axes->extent[a];
     if (ch < 0 || ch % 2 || ch > head_dim - channels) return fail("axis channels must be even, >= 0 and at most head_dim in all");
@@ -113,12 +114,14 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
     tokens *= ext;
     p.pairs[a] = ch / 2;
     p.origin[a] = axes->origin[a];
-    // theta^(-2 i / channels), one multiplication a pair
-    const double ratio = ch ? std::pow(axes->theta, -2.0 / ch) : 1.0;
-    double f = axes->step[a] / 6.283185307179586476925286766559;
+    // theta^(-2 i / channels), one multiplication a pair in 80 bits: 64 roundings of 2^-64 and the
+    // logarithm's (times its own size) leave fp64's rounding of the result alone (in fp64 the 64th would be off by 2^-46)
+    const long double ratio = ch > 2 ? std::exp(log_theta * (-2.0L / ch)) : 1.0L;
+    long double f = axes->step[a] / 6.283185307179586476925286766559L;
     for (int i = 0; i < ch / 2; ++i, f *= ratio) {
-      if (!std::isfinite(f * (std::fabs(axes->origin[a]) + ext))) return fail("an angle of axis %d is past fp64's range", a);
-      p.turns[pair++] = f;
+      const double turns = (double)f;
+      if (!std::isfinite(turns * (std::fabs(axes->origin[a]) + ext))) return fail("an angle of axis %d is past fp64's range", a);
+      p.turns[pair++] = turns;
     }
   }
   if (n_tok < 0 || token_begin < 0 || n_tok > tokens - token_begin)

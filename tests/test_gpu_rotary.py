@@ -129,3 +129,27 @@ def test_no_tokens(orch_lib):
     orch_lib.check(orch_lib.lib.orch_op_rotary(orch_lib.C.byref(ax), ts, 1, 2, 0, 16, 32, 0, None))
     torch.cuda.synchronize()
     assert torch.all(x == 1)
+
+
+@pytest.mark.parametrize("interleaved", [True, False])
+@pytest.mark.parametrize("theta", [1.0001, 2.0, 100.0])
+def test_far_origin(orch_lib, theta, interleaved):
+    """Positions of 10^12, 64 pairs of one axis: every pair's angle is off by two fp64 roundings (the pair's turns per
+    position, and their product with the position: 2^-52 of the angle) and what _check allows for, whatever its number.
+    Angles of the reference in 80 bits, where those two roundings are 2^-63."""
+    n, d, origin = 64, 128, 1e12
+    ax = orch_lib.rotary_axes((d, 0, 0), (n, 1, 1), theta, (origin, 0, 0), (1, 1, 1), interleaved)
+    x = np.random.default_rng(3).standard_normal((1, 2, n, d)).astype(np.float32)
+    out = torch.empty((1, 2, n, d), device=DEV)
+    orch_lib.rotary(ax, 0, to_dev(x), out)
+    assert np.finfo(np.longdouble).nmant >= 63
+    i = np.arange(d // 2).astype(np.longdouble)
+    phi = (np.longdouble(origin) + np.arange(n))[:, None] * np.longdouble(theta) ** (-2 * i / d)
+    a, b = (x[..., 0::2], x[..., 1::2]) if interleaved else (x[..., :d // 2], x[..., d // 2:])
+    u, v = np.cos(phi) * a - np.sin(phi) * b, np.sin(phi) * a + np.cos(phi) * b
+    got = to_host(out)
+    gu, gv = (got[..., 0::2], got[..., 1::2]) if interleaved else (got[..., :d // 2], got[..., d // 2:])
+    tol = (np.abs(a) + np.abs(b)) * (2.0 ** -21 + 2.0 ** -52 * phi) + 2.0 ** -24 * (np.abs(u) + np.abs(v))
+    for g, ref in ((gu, u), (gv, v)):
+        print(float((np.abs(g - ref) / tol).max()), flush=True)
+        assert (np.abs(g - ref) <= tol).all()
