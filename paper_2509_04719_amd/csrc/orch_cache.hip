@@ -36,9 +36,24 @@ int launched(hipError_t e, const char* what) {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  if (!a || !b || na == 0 || nb == 0) return false;
-  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+// `count` runs of `bytes` bytes, `stride` bytes apart: the branches of a buffer
+struct Runs {
+  const void* p;
+  size_t bytes, stride;
+  int count;
+};
+
+// A byte of both?  (The runs of one may lie between those of the other.)
+bool overlap(const Runs& a, const Runs& b) {
+  if (!a.p || !b.p || a.bytes == 0 || b.bytes == 0) return false;
+  const uintptr_t b0 = (uintptr_t)b.p;
+  for (int i = 0; i < a.count; ++i) {
+    const uintptr_t lo = (uintptr_t)a.p + (i ? i * a.stride : 0), hi = lo + a.bytes;
+    // the first run of b that ends past lo
+    const size_t j = lo < b0 + b.bytes ? 0 : b.count > 1 ? (lo - b0 - b.bytes) / b.stride + 1 : 1;
+    if (j < (size_t)b.count && b0 + (j ? j * b.stride : 0) < hi) return true;
+  }
+  return false;
 }
 
 // heads, branches, head size and type that every entry point takes
@@ -50,17 +65,17 @@ int check_common(int B, int heads, int head_dim, int dtype) {
   return ORCH_OK;
 }
 
-// a cache of B branches; its extents in bytes
-int check_cache(const orch_quantized_kv* c, int B, int heads, int d, size_t* values, size_t* exps) {
+// a cache of B branches; where its values and exponents lie
+int check_cache(const orch_quantized_kv* c, int B, int heads, int d, Runs* values, Runs* exps) {
   if (!c || !c->values || !c->exponents) return fail("NULL cache");
   if (c->tokens < 1) return fail("the cache's tokens must be >= 1");
   if ((long long)c->tokens * d >= 1ll << 31) return fail("cache tokens * head_dim must be below 2^31");
   const size_t e = (size_t)2 * heads * c->tokens, v = e * d;
   if (B > 1 && (c->values_stride < v || c->exponents_stride < e)) return fail("the cache's branch stride is too small");
   if (!aligned16(c->values) || (B > 1 && c->values_stride % 16)) return fail("cache values must be 16-byte aligned");
-  *values = (B > 1 ? (B - 1) * c->values_stride : 0) + v;
-  *exps = (B > 1 ? (B - 1) * c->exponents_stride : 0) + e;
-  if (overlap(c->values, *values, c->exponents, *exps)) return fail("the cache's values and exponents overlap");
+  *values = {c->values, v, c->values_stride, B};
+  *exps = {c->exponents, e, c->exponents_stride, B};
+  if (overlap(*values, *exps)) return fail("the cache's values and exponents overlap");
   return ORCH_OK;
 }
 
@@ -70,7 +85,7 @@ int kv_params(KvCacheParams* p, const void* kv, size_t kv_bs, int kv_tokens, int
   if (!kv) return fail("NULL pointer");
   int rc = check_common(B, heads, d, dtype);
   if (rc) return rc;
-  size_t values, exps;
+  Runs values, exps;
   rc = check_cache(c, B, heads, d, &values, &exps);
   if (rc) return rc;
   if (n < 0 || kv_off < 0 || c_off < 0 || kv_tokens < 1 || n > kv_tokens - kv_off || n > c->tokens - c_off)
@@ -80,8 +95,8 @@ int kv_params(KvCacheParams* p, const void* kv, size_t kv_bs, int kv_tokens, int
   const size_t es = dtype == ORCH_BF16 ? 2 : 4, H = (size_t)heads * d, elems = 2 * (size_t)kv_tokens * H;
   if (B > 1 && kv_bs < elems) return fail("branch stride too small");
   if (!aligned16(kv) || (B > 1 && kv_bs * es % 16)) return fail("the K/V buffer must be 16-byte aligned");
-  const size_t bytes = ((B > 1 ? (B - 1) * kv_bs : 0) + elems) * es;
-  if (overlap(kv, bytes, c->values, values) || overlap(kv, bytes, c->exponents, exps))
+  const Runs buffer = {kv, elems * es, kv_bs * es, B};
+  if (overlap(buffer, values) || overlap(buffer, exps))
     return fail("the K/V buffer and the cache overlap");
   p->c.values = (unsigned char*)c->values; p->c.exps = (unsigned char*)c->exponents;
   p->c.values_bs = c->values_stride; p->c.exps_bs = c->exponents_stride; p->c.tokens = c->tokens;
@@ -183,7 +198,7 @@ int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache, c
   if (!q || !out || (n_fresh > 0 && !kv_fresh)) return fail("NULL pointer");
   int rc = check_common(B, heads, head_dim, dtype);
   if (rc) return rc;
-  size_t values, exps;
+  Runs values, exps;
   rc = check_cache(cache, B, heads, head_dim, &values, &exps);
   if (rc) return rc;
   if (n_q < 0 || n_fresh < 0 || fresh_begin < 0 || n_fresh > cache->tokens - fresh_begin)
@@ -195,13 +210,12 @@ int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache, c
   if (!aligned16(q) || !aligned16(out) || (n_fresh > 0 && (!aligned16(kv_fresh) || (B > 1 && fresh_bs * es % 16))) ||
       (workspace && !aligned16(workspace)))
     return fail("device buffers must be 16-byte aligned");
-  const size_t fresh_bytes = n_fresh > 0 ? ((B > 1 ? (B - 1) * fresh_bs : 0) + fresh_elems) * es : 0;
   const size_t ws_used = workspace ? workspace_bytes : 0;
-  const struct { const void* p; size_t n; } in[] = {{q, q_bytes}, {cache->values, values}, {cache->exponents, exps}, {kv_fresh, fresh_bytes}};
-  for (const auto& r : in)
-    if (overlap(out, q_bytes, r.p, r.n) || overlap(workspace, ws_used, r.p, r.n))
-      return fail("out or workspace overlaps an input");
-  if (overlap(workspace, ws_used, out, q_bytes)) return fail("out and workspace overlap");
+  const Runs o = {out, q_bytes, 0, 1}, w = {workspace, ws_used, 0, 1};
+  const Runs in[] = {{q, q_bytes, 0, 1}, values, exps, {kv_fresh, fresh_elems * es, fresh_bs * es, B}};
+  for (const Runs& r : in)
+    if (overlap(r, o) || overlap(r, w)) return fail("out or workspace overlaps an input");
+  if (overlap(w, o)) return fail("out and workspace overlap");
   AttnQParams p{};
   p.q = q; p.out = out; p.kv_fresh = kv_fresh; p.fresh_bs = fresh_bs; p.fresh_begin = fresh_begin; p.n_fresh = n_fresh;
   p.c.values = (unsigned char*)cache->values; p.c.exps = (unsigned char*)cache->exponents;

@@ -138,3 +138,27 @@ def test_a_large_cache(orch_lib):
         np.testing.assert_array_equal(values[:, i, :, N - n:].cpu().numpy(), wv)
         np.testing.assert_array_equal(exps[:, i, :, N - n:].cpu().numpy(), we)
         np.testing.assert_array_equal(g, ok.dequantize(wv, we))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_branch_in_one_record(orch_lib, dtype):
+    """Values and exponents of a branch one behind the other, as a peer would get them: the bytes and results of a cache in
+    two tensors, nothing between the records touched."""
+    B, heads, d, N, n = 3, 4, 72, 75, 33
+    rng = np.random.default_rng(2)
+    buf = to_dev(ok.to_buffer(*_kv(rng, B, heads, N, d, dtype)), dtype)
+    v, e = 2 * heads * N * d, 2 * heads * N
+    rec = torch.full((B, (v + e + 15) // 16 * 16 + 32), 0x55, dtype=torch.uint8, device=DEV)
+    pairs = [_empty(B, heads, N, d), (rec[:, :v].unflatten(1, (2, heads, N, d)), rec[:, v:v + e].unflatten(1, (2, heads, N)))]
+    q = to_dev(rng.standard_normal((B, heads, n, d)), dtype)
+    results = []
+    for values, exps in pairs:
+        cache = orch_lib.quantized_kv(values, exps)
+        orch_lib.kv_quantize(buf, 2 * N * heads * d, N, 0, cache, 0, B, heads, N, d, code(dtype))
+        back = torch.empty_like(buf)
+        orch_lib.kv_dequantize(cache, 0, back, 2 * N * heads * d, N, 0, B, heads, N, d, code(dtype))
+        out = torch.empty((B, n, heads * d), dtype=buf.dtype, device=DEV)
+        orch_lib.attention_quantized(q, cache, None, 0, 0, 0, B, heads, n, d, out, code(dtype))
+        results.append((values.clone(), exps.clone(), back, out))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert torch.all(rec[:, v + e:] == 0x55)

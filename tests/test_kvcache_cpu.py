@@ -192,3 +192,41 @@ def test_binding_of_the_cache_refuses(orch_lib):
 def test_no_workspace_for_bad_shapes(orch_lib, bad):
     a = dict(B=1, heads=2, n_q=1, n_kv=4096, d=64, dtype=BF16) | bad
     assert orch_lib.attention_quantized_workspace_bytes(*a.values()) == 0
+
+
+def _record(lib, kv=P[0], B=3, exponents=4096 * 2, stride=4096 * 2 + 256, bs=1 << 20, out=P[4], n=0):
+    """Caches [values of a branch][its exponents] of 64 tokens, 2 heads of 32 (8192 + 256 bytes), called for no tokens."""
+    c = dict(vs=stride, es=stride, exponents=P[2] + exponents)
+    return [_move(lib, False, kv=kv, bs=bs, B=B, n=n, cache=c), _move(lib, True, kv=kv, bs=bs, B=B, n=n, cache=c),
+            _attend(lib, B=B, n_q=n, fresh=kv, bs=bs, out=out, cache=c)]
+
+
+def test_branches_may_lie_between_each_other(orch_lib):
+    """Values and exponents of a branch in one record, records anywhere, K/V buffers between them: no byte is shared."""
+    assert _record(orch_lib) == [0, 0, 0]
+    assert _record(orch_lib, stride=1 << 20) == [0, 0, 0]
+    assert _record(orch_lib, exponents=-256) == [0, 0, 0]                       # exponents first
+    # K/V of 40 tokens (10240 bytes) behind each of the first branches' records
+    assert _record(orch_lib, stride=1 << 16, kv=P[2] + 8448 + 64, bs=1 << 15) == [0, 0, 0]
+    assert _record(orch_lib, stride=1 << 16, kv=P[2] + (1 << 16) - 10240, bs=1 << 15) == [0, 0, 0]
+
+
+@pytest.mark.parametrize("kw", [
+    dict(exponents=8192 - 16), dict(exponents=-240), dict(stride=1 << 16, exponents=(1 << 16) - 16),
+    dict(stride=1 << 16, exponents=2 * (1 << 16) + 8191), dict(stride=1 << 16, exponents=-2 * (1 << 16) - 16),
+])
+def test_branches_that_share_bytes_are_refused(orch_lib, kw):
+    for rc in _record(orch_lib, **kw):
+        _refused(orch_lib, rc, "values and exponents overlap")
+
+
+@pytest.mark.parametrize("at", [8448 - 16, -2 * 65536 + 8448 - 16, 2 * 65536 - 16, 65536 - 10240 + 16])
+def test_buffers_that_share_bytes_with_a_branch_are_refused(orch_lib, at):
+    """(At those places every other branch of the two is apart.)"""
+    quantize, back, _ = _record(orch_lib, stride=1 << 16, kv=P[2] + at, bs=1 << 15)
+    assert quantize == back == orch_lib.ORCH_EINVAL
+    assert "overlap" in orch_lib.last_error()
+    # the output of an attention (2 x 3 branches of 8 queries of 2 x 32 channels: 3072 bytes)
+    c = dict(vs=1 << 16, es=1 << 16, exponents=P[2] + 8192)
+    _refused(orch_lib, _attend(orch_lib, B=3, n_q=8, out=P[2] + 65536 + 8448 - 16, cache=c), "overlap")
+    _refused(orch_lib, _attend(orch_lib, B=3, n_q=8, out=P[2] + 2 * 65536 - 3072 + 16, cache=c), "overlap")
