@@ -368,7 +368,8 @@ int orch_op_attention_noalloc(const void* q, const void* kv_stale, size_t stale_
  * Q and K, the stale K/V of the image held in 8 bits (half of bf16's bytes, a
  * quarter of fp32's, to hold and to exchange with a peer), and the attention
  * that reads it.  head_dim as in orch_dit_config.  Device pointers of K/V
- * buffers, Q, cache values and outputs are 16-byte aligned. */
+ * buffers, Q, cache values and outputs are 16-byte aligned.  No tokens (n_tok or
+ * n_q 0) is no error: nothing is done, and their buffers may be NULL. */
 
 /* Rotary positions on a grid of frames x rows x columns (extent[0..2]): token n
  * lies at frame f, row r, column c with n = (f * rows + r) * columns + c.  Axis

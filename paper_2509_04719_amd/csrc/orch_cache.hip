@@ -82,7 +82,7 @@ int check_cache(const orch_quantized_kv* c, int B, int heads, int d, Runs* value
 // checks and parameters of writing and reading back
 int kv_params(KvCacheParams* p, const void* kv, size_t kv_bs, int kv_tokens, int kv_off, const orch_quantized_kv* c,
               int c_off, int B, int heads, int n, int d, int dtype) {
-  if (!kv) return fail("NULL pointer");
+  if (n != 0 && !kv) return fail("NULL pointer");
   int rc = check_common(B, heads, d, dtype);
   if (rc) return rc;
   Runs values, exps;
@@ -145,7 +145,7 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
   const size_t es = dtype == ORCH_BF16 ? 2 : 4;
   for (int k = 0; k < n_tensors; ++k) {
     const orch_rotary_tensor& t = tensors[k];
-    if (!t.x || !t.out) return fail("NULL pointer");
+    if (n_tok > 0 && (!t.x || !t.out)) return fail("NULL pointer");
     if (t.heads < 1 || (long long)t.heads * B > 32767) return fail("bad shape: heads must be >= 1, B * heads <= 32767");
     if ((uintptr_t)t.x % es || (uintptr_t)t.out % es) return fail("tensors must be aligned to their elements");
     const int extent[3] = {B, t.heads, n_tok};
@@ -195,7 +195,7 @@ size_t orch_attention_quantized_workspace_bytes(int B, int heads, int n_q, int n
 int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache, const void* kv_fresh, size_t fresh_bs,
                                 int fresh_begin, int n_fresh, int B, int heads, int n_q, int head_dim, void* out,
                                 void* workspace, size_t workspace_bytes, int dtype, void* hip_stream) {
-  if (!q || !out || (n_fresh > 0 && !kv_fresh)) return fail("NULL pointer");
+  if ((n_q != 0 && (!q || !out)) || (n_fresh > 0 && !kv_fresh)) return fail("NULL pointer");
   int rc = check_common(B, heads, head_dim, dtype);
   if (rc) return rc;
   Runs values, exps;

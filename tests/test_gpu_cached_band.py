@@ -202,3 +202,19 @@ def test_host_tensors_are_refused(orch_lib):
         orch_lib.rotary(x.axes, 0, q.cpu(), q)
     with pytest.raises(orch_lib.OrchError):
         orch_lib.kv_quantize(kv, 0, 8, 0, orch_lib.quantized_kv(x.values.cpu(), x.exps), 0, 1, 2, 8, 32, 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_empty_band(orch_lib, dtype):
+    """No tokens, in torch's empty tensors (address 0): nothing is done, and the cache stays as it was."""
+    x = Band(orch_lib, dtype, 2, 2, 32, 4, 4, 1)
+    before = x.values.view(torch.uint8).clone()
+    q, out, none = empty((2, 2, 0, 32), dtype), empty((2, 0, 64), dtype), empty((2, 0), dtype)
+    assert q.data_ptr() == 0
+    orch_lib.rotary(x.axes, 3, (q, q), (q, q.clone()))
+    orch_lib.rotary(x.axes, 16, q, q)
+    for fresh in (None, none):
+        orch_lib.attention_quantized(q, x.cache, fresh, 0, 5, 0, 2, 2, 0, 32, out, code(dtype))
+    orch_lib.kv_quantize(empty((2, 8 * 128), dtype), 8 * 128, 8, 3, x.cache, 5, 2, 2, 0, 32, code(dtype))
+    torch.cuda.synchronize()
+    assert torch.equal(before, x.values.view(torch.uint8))

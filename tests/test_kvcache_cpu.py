@@ -230,3 +230,17 @@ def test_buffers_that_share_bytes_with_a_branch_are_refused(orch_lib, at):
     c = dict(vs=1 << 16, es=1 << 16, exponents=P[2] + 8192)
     _refused(orch_lib, _attend(orch_lib, B=3, n_q=8, out=P[2] + 65536 + 8448 - 16, cache=c), "overlap")
     _refused(orch_lib, _attend(orch_lib, B=3, n_q=8, out=P[2] + 2 * 65536 - 3072 + 16, cache=c), "overlap")
+
+
+def test_no_tokens_need_no_buffers(orch_lib):
+    """An empty tensor has address 0: no tokens and no queries are no error, whatever the addresses."""
+    assert _rotary(orch_lib, n_tok=0, tensors=[dict(x=None, out=None)]) == 0
+    assert _rotary(orch_lib, n_tok=0, n_tensors=2, tensors=[dict(x=None, out=None), dict(x=None, out=None)]) == 0
+    assert _attend(orch_lib, n_q=0, q=None, out=None) == 0
+    assert _attend(orch_lib, n_q=0, q=None, out=None, fresh=None, fb=0, nf=0) == 0
+    assert _move(orch_lib, False, n=0, kv=None) == 0 and _move(orch_lib, True, n=0, kv=None) == 0
+    # the rest is checked all the same
+    _refused(orch_lib, _rotary(orch_lib, n_tok=0, d=40, tensors=[dict(x=None, out=None)]), "head_dim")
+    _refused(orch_lib, _attend(orch_lib, n_q=0, q=None, out=None, fresh=None), "NULL")
+    _refused(orch_lib, _attend(orch_lib, n_q=0, q=None, out=None, cache=dict(values=None)), "cache")
+    _refused(orch_lib, _move(orch_lib, True, n=0, kv=None, off=65), "tokens")
