@@ -157,6 +157,7 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
       // (the stride of an extent of one is never used)
       p.t[k].xs[a] = extent[a] > 1 ? t.x_stride[a] : 0;
       p.t[k].os[a] = extent[a] > 1 ? t.out_stride[a] : 0;
+      if (n_tok > 0 && t.x == t.out && p.t[k].xs[a] != p.t[k].os[a]) return fail("in place needs the same strides");
     }
   }
   if (n_tensors == 2 && n_tok > 0) {

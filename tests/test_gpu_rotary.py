@@ -153,3 +153,13 @@ def test_far_origin(orch_lib, theta, interleaved):
     for g, ref in ((gu, u), (gv, v)):
         print(float((np.abs(g - ref) / tol).max()), flush=True)
         assert (np.abs(g - ref) <= tol).all()
+
+
+def test_in_place_whatever_the_stride_of_one(orch_lib):
+    """The stride of an extent of one has no meaning: in place with another one there."""
+    ax = orch_lib.rotary_axes((0, 16, 16), (1, 4, 4))
+    x = torch.randn((1, 2, 1, 32), device=DEV)
+    want = torch.empty_like(x)
+    orch_lib.rotary(ax, 5, x, want)
+    orch_lib.rotary(ax, 5, x, x.as_strided(x.shape, (999, 32, 7, 1)))
+    assert torch.equal(x, want)

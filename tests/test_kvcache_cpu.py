@@ -244,3 +244,14 @@ def test_no_tokens_need_no_buffers(orch_lib):
     _refused(orch_lib, _attend(orch_lib, n_q=0, q=None, out=None, fresh=None), "NULL")
     _refused(orch_lib, _attend(orch_lib, n_q=0, q=None, out=None, cache=dict(values=None)), "cache")
     _refused(orch_lib, _move(orch_lib, True, n=0, kv=None, off=65), "tokens")
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=2, tensors=[dict(out=P[0], xs=(256, 128, 32), os=(512, 128, 32))]),
+    dict(tensors=[dict(out=P[0], xs=(256, 128, 32), os=(256, 256, 32))]),
+    dict(tensors=[dict(out=P[0], xs=(256, 128, 32), os=(256, 128, 64))]),
+    dict(tensors=[dict(out=P[0], heads=4, xs=(512, 128, 32), os=(512, 32, 128))]),        # a transpose
+    dict(n_tensors=2, tensors=[dict(), dict(x=P[2], out=P[2], os=(256, 256, 32))]),
+])
+def test_in_place_needs_the_same_strides(orch_lib, kw):
+    _refused(orch_lib, _rotary(orch_lib, **kw), "in place")
