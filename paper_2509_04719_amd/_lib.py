@@ -165,12 +165,19 @@ def _stream_on(stream, *devices):
     return torch._C._cuda_getCurrentRawStream(cur) if stream is None else stream.cuda_stream
 
 
+_CODES = {}             # by torch type, filled at the first use (torch is not imported before)
+
+
 def _code(t):
     """The library's code of a tensor's type."""
-    import torch
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise OrchError(ORCH_EINVAL, f"type {t.dtype} not supported")
-    return ORCH_F32 if t.dtype == torch.float32 else ORCH_BF16
+    code = _CODES.get(t.dtype)
+    if code is None:
+        import torch
+        _CODES.update({torch.float32: ORCH_F32, torch.bfloat16: ORCH_BF16})
+        code = _CODES.get(t.dtype)
+        if code is None:
+            raise OrchError(ORCH_EINVAL, f"type {t.dtype} not supported")
+    return code
 
 
 def schedule_coefficients(cfg, t: int, t_prev: int, eta: float = 0.0):
@@ -375,9 +382,28 @@ def _check_cache(cache, B, heads, head_dim):
         raise OrchError(ORCH_EINVAL, f"{B} branches of {heads} heads of {head_dim} channels, the cache holds {b} of {h} of {d}")
 
 
+def _check_buffer(name, t, dtype, elements, branch_stride=0):
+    """t is of the code's type and holds `elements` elements from its first on, one behind the other within a branch."""
+    if _code(t) != dtype:
+        raise OrchError(ORCH_EINVAL, f"{name} is {t.dtype}, the call's type code {dtype}")
+    if t.is_contiguous():
+        held = t.numel()
+    elif t.dim() > 1 and t.stride(0) == branch_stride and t[0].is_contiguous():
+        held = (t.shape[0] - 1) * branch_stride + t[0].numel()
+    else:
+        raise OrchError(ORCH_EINVAL, f"{name} must be contiguous (a K/V buffer: within a branch)")
+    if held < elements:
+        raise OrchError(ORCH_EINVAL, f"{name} holds {held} elements, the call needs {elements}")
+
+
+def _check_kv(name, kv, dtype, branch_stride, tokens, B, heads, head_dim):
+    _check_buffer(name, kv, dtype, (B - 1) * branch_stride + 2 * tokens * heads * head_dim, branch_stride)
+
+
 def kv_quantize(kv, kv_branch_stride, kv_tokens, kv_offset, cache: QuantizedKV, tok_offset, B, heads,
                 n_tok, head_dim, dtype, stream=None):
     _check_cache(cache, B, heads, head_dim)
+    _check_kv("kv", kv, dtype, kv_branch_stride, kv_tokens, B, heads, head_dim)
     st = _stream_on(stream, kv.get_device(), *cache.devices)
     check(lib.orch_op_kv_quantize(kv.data_ptr(), kv_branch_stride, kv_tokens, kv_offset, C.byref(cache),
                                   tok_offset, B, heads, n_tok, head_dim, dtype, st))
@@ -386,6 +412,7 @@ def kv_quantize(kv, kv_branch_stride, kv_tokens, kv_offset, cache: QuantizedKV, 
 def kv_dequantize(cache: QuantizedKV, tok_offset, kv, kv_branch_stride, kv_tokens, kv_offset, B, heads,
                   n_tok, head_dim, dtype, stream=None):
     _check_cache(cache, B, heads, head_dim)
+    _check_kv("kv", kv, dtype, kv_branch_stride, kv_tokens, B, heads, head_dim)
     st = _stream_on(stream, kv.get_device(), *cache.devices)
     check(lib.orch_op_kv_dequantize(C.byref(cache), tok_offset, kv.data_ptr(), kv_branch_stride, kv_tokens,
                                     kv_offset, B, heads, n_tok, head_dim, dtype, st))
@@ -398,6 +425,12 @@ def attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype) ->
 def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, n_fresh, B, heads, n_q,
                         head_dim, out, dtype, workspace=None, stream=None):
     _check_cache(cache, B, heads, head_dim)
+    _check_buffer("q", q, dtype, B * n_q * heads * head_dim)
+    _check_buffer("out", out, dtype, B * n_q * heads * head_dim)
+    if n_fresh > 0 and kv_fresh is not None:
+        _check_kv("kv_fresh", kv_fresh, dtype, fresh_bs, n_fresh, B, heads, head_dim)
+    if workspace is not None and not workspace.is_contiguous():
+        raise OrchError(ORCH_EINVAL, "workspace must be contiguous")
     ws_bytes = 0 if workspace is None else workspace.nbytes
     st = _stream_on(stream, *cache.devices, *[t.get_device() for t in (q, kv_fresh, out, workspace) if t is not None])
     check(lib.orch_op_attention_quantized(_ptr(q), C.byref(cache), _ptr(kv_fresh), fresh_bs, fresh_begin,

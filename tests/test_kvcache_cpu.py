@@ -255,3 +255,58 @@ def test_no_tokens_need_no_buffers(orch_lib):
 ])
 def test_in_place_needs_the_same_strides(orch_lib, kw):
     _refused(orch_lib, _rotary(orch_lib, **kw), "in place")
+
+
+def _bound(lib, kv=None, q=None, out=None, fresh=None, ws=None, dtype=BF16, bs=2 * 8 * 96, tokens=8, n_q=5, B=2):
+    """The binding's three calls on host tensors (refused for that if for nothing else): 2 branches of 3 heads of 32."""
+    t = torch.bfloat16
+    cache = lib.quantized_kv(torch.zeros((2, 2, 3, 16, 32), dtype=torch.uint8), torch.zeros((2, 2, 3, 16), dtype=torch.uint8))
+    kv = torch.zeros((2, 2 * 8 * 96), dtype=t) if kv is None else kv
+    fresh = torch.zeros((2, 2 * 8 * 96), dtype=t) if fresh is None else fresh
+    q = torch.zeros((2, 3, 5, 32), dtype=t) if q is None else q
+    out = torch.zeros((2, 5, 96), dtype=t) if out is None else out
+    return (lambda: lib.kv_quantize(kv, bs, tokens, 0, cache, 0, B, 3, 8, 32, dtype),
+            lambda: lib.kv_dequantize(cache, 0, kv, bs, tokens, 0, B, 3, 8, 32, dtype),
+            lambda: lib.attention_quantized(q, cache, fresh, bs, 0, tokens, B, 3, n_q, 32, out, dtype, workspace=ws))
+
+
+ROWS = torch.zeros((2, 2 * 8 * 96 + 32), dtype=torch.bfloat16)
+REFUSED_BUFFERS = [      # calls, arguments, message
+    ((0, 1), dict(kv=torch.zeros((2, 2 * 8 * 96))), "type"), ((0, 1, 2), dict(dtype=F32), "type"),
+    ((0, 1), dict(kv=torch.zeros((2, 2 * 8 * 96), dtype=torch.half)), "type"),
+    ((0, 1), dict(kv=torch.zeros(2 * 2 * 8 * 96 - 1, dtype=torch.bfloat16)), "holds"),
+    ((0, 1), dict(tokens=9), "holds"), ((0, 1, 2), dict(bs=2 * 8 * 96 + 8), "holds"), ((2,), dict(tokens=9), "holds"),
+    ((0, 1), dict(kv=ROWS[:, :2 * 8 * 96]), "contiguous"), ((0, 1), dict(kv=torch.zeros((2, 8 * 96, 4), dtype=torch.bfloat16)[..., ::2]), "contiguous"),
+    ((2,), dict(fresh=ROWS[:, :2 * 8 * 96]), "contiguous"), ((2,), dict(fresh=torch.zeros((2, 2 * 8 * 96))), "type"),
+    ((2,), dict(q=torch.zeros((2, 3, 4, 32), dtype=torch.bfloat16)), "q holds"), ((2,), dict(n_q=6), "holds"),
+    ((2,), dict(q=torch.zeros((2, 5, 3, 32), dtype=torch.bfloat16).transpose(1, 2)), "q must be contiguous"),
+    ((2,), dict(q=torch.zeros((2, 3, 5, 32))), "q is"), ((2,), dict(out=torch.zeros((2, 5, 96))), "out is"),
+    ((2,), dict(out=torch.zeros((2, 4, 96), dtype=torch.bfloat16)), "out holds"),
+    ((2,), dict(out=torch.zeros((5, 2, 96), dtype=torch.bfloat16).transpose(0, 1)), "out must be contiguous"),
+    ((2,), dict(ws=torch.zeros((64, 64), dtype=torch.uint8).t()[:, :3]), "workspace must be contiguous"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(REFUSED_BUFFERS)))
+def test_binding_refuses_buffers(orch_lib, i):
+    """Tensors of another type than the code's, too small for the extents, or with other strides than the kernels read."""
+    calls, kw, word = REFUSED_BUFFERS[i]
+    for c in calls:
+        with pytest.raises(orch_lib.OrchError, match=word):
+            _bound(orch_lib, **kw)[c]()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(kv=ROWS[:, :2 * 8 * 96], fresh=ROWS[:, :2 * 8 * 96], bs=2 * 8 * 96 + 32),
+                                dict(kv=ROWS.view(-1), fresh=ROWS.view(-1)), dict(B=1, bs=0), dict(out=ROWS, q=ROWS)])
+def test_binding_takes_buffers(orch_lib, monkeypatch, kw):
+    """What they hold is enough: the next check, of the devices, is reached."""
+    class Reached(Exception):
+        pass
+
+    def on(*_):
+        raise Reached
+
+    monkeypatch.setattr(orch_lib, "_stream_on", on)
+    for call in _bound(orch_lib, **kw):
+        with pytest.raises(Reached):
+            call()
