@@ -471,6 +471,14 @@ int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache,
 size_t orch_attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int head_dim,
                                                 int dtype);
 
+/* The form in which orch_op_attention_quantized runs a shape (n_q >= 1) with that
+ * many bytes of workspace, host only: whether the keys are widened once, the
+ * groups of 32 queries of a workgroup (1: its waves share the keys), and the
+ * workgroups that share a query's keys.  ORCH_EINVAL: a shape that it refuses. */
+int orch_attention_quantized_plan(int B, int heads, int n_q, int n_kv, int head_dim, int dtype,
+                                  size_t workspace_bytes, int* prepared, int* query_groups,
+                                  int* key_parts);
+
 /* Conditioning of the loaded model: out fp32 [cfg_batch][6*H*n_blocks + 2*H],
  * the adaLN vectors of every block followed by the final layer's
  * (shift, scale), for timestep t and host labels[cfg_batch]. */

@@ -30,7 +30,7 @@ SYMBOLS = (
     "orch_op_attention_noalloc", "orch_speeds_from_profiles", "orch_unet_conv_band",
     "orch_unet_conv_workspace_bytes", "orch_op_rotary", "orch_op_kv_quantize",
     "orch_op_kv_dequantize", "orch_op_attention_quantized",
-    "orch_attention_quantized_workspace_bytes",
+    "orch_attention_quantized_workspace_bytes", "orch_attention_quantized_plan",
 )
 KCLASSES = ("conditioning", "patch_embed", "layernorm", "qkv_gemm", "attention", "proj_gemm",
             "fc1_gemm", "fc2_gemm", "final_layer", "update")
@@ -118,6 +118,7 @@ def _load():
         "orch_op_attention_quantized": (i, [vp, C.POINTER(QuantizedKV), vp, sz, i, i, i, i, i, i, vp,
                                             vp, sz, i, vp]),
         "orch_attention_quantized_workspace_bytes": (sz, [i, i, i, i, i, i]),
+        "orch_attention_quantized_plan": (i, [i, i, i, i, i, i, sz] + [C.POINTER(i)] * 3),
         "orch_sample_patch_parallel": (i, [vp, vp, i, C.POINTER(i), C.POINTER(i), C.POINTER(i), i, i,
                                            C.POINTER(i), f, vp, vp, vp]),
     }
@@ -420,6 +421,13 @@ def kv_dequantize(cache: QuantizedKV, tok_offset, kv, kv_branch_stride, kv_token
 
 def attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype) -> int:
     return lib.orch_attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype)
+
+
+def attention_quantized_plan(B, heads, n_q, n_kv, head_dim, dtype, workspace_bytes):
+    """(prepared, query_groups, key_parts) of a call, see orch_attention_quantized_plan."""
+    r = [C.c_int() for _ in range(3)]
+    check(lib.orch_attention_quantized_plan(B, heads, n_q, n_kv, head_dim, dtype, workspace_bytes, *map(C.byref, r)))
+    return bool(r[0].value), r[1].value, r[2].value
 
 
 def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, n_fresh, B, heads, n_q,

@@ -1410,31 +1410,45 @@ size_t split_bytes(const Plan& pl, int d) {
   return pl.ns == 1 ? 0 : part_floats(pl, d) * 4 + pl.tiles * pl.ns * 32 * pl.nw * sizeof(float2);
 }
 
+size_t need_bytes(const Plan& pl, int B, int heads, int n_kv, int d) {
+  return split_bytes(pl, d) + tile_bytes(pl, B, heads, n_kv, d);
+}
+
+// The plan of a call with ws_bytes of workspace (0: none): that of the whole workspace, or that of none.
+Plan plan_within(int B, int heads, int n_q, int n_kv, int d, int dtype, size_t ws_bytes) {
+  const Plan pl = plan(B, heads, n_q, n_kv, d, dtype, true);
+  return pl.nw == 0 || (ws_bytes > 0 && ws_bytes >= need_bytes(pl, B, heads, n_kv, d)) ? pl : plan(B, heads, n_q, n_kv, d, dtype, false);
+}
+
 }  // namespace q8attn
 
 size_t attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int d, int dtype) {
   using namespace q8attn;
   if (n_q <= 0) return 0;
   const Plan pl = plan(B, heads, n_q, n_kv, d, dtype, true);
-  return pl.nw == 0 ? 0 : split_bytes(pl, d) + tile_bytes(pl, B, heads, n_kv, d);
+  return pl.nw == 0 ? 0 : need_bytes(pl, B, heads, n_kv, d);
+}
+
+bool attention_quantized_plan(int B, int heads, int n_q, int n_kv, int d, int dtype, size_t ws_bytes, int* prepared,
+                              int* query_groups, int* key_parts) {
+  const q8attn::Plan pl = q8attn::plan_within(B, heads, n_q, n_kv, d, dtype, ws_bytes);
+  *prepared = pl.prep;
+  *query_groups = pl.nw;
+  *key_parts = pl.ns;
+  return pl.nw != 0;
 }
 
 hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream_t s) {
   using namespace q8attn;
   if (p.n_q <= 0) return hipSuccess;
-  Plan pl = plan(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype, true);
+  const Plan pl = plan_within(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype, p.ws ? p.ws_bytes : 0);
   if (pl.nw == 0) return hipErrorInvalidValue;
-  size_t tiles = tile_bytes(pl, p.B, p.heads, p.c.tokens, p.d);
-  if (!p.ws || p.ws_bytes < split_bytes(pl, p.d) + tiles) {
-    pl = plan(p.B, p.heads, p.n_q, p.c.tokens, p.d, dtype, false);
-    tiles = 0;
-  }
   const bool prepare = pl.prep;
   if (pl.tiles * pl.ns > 0x7fffffff) return hipErrorInvalidValue;
   Split sp{nullptr, pl.ns, nullptr, nullptr};
   if (prepare) sp.tiles = reinterpret_cast<const char*>(p.ws);
   if (pl.ns > 1) {
-    sp.part_o = reinterpret_cast<float*>((char*)p.ws + (prepare ? tiles : 0));
+    sp.part_o = reinterpret_cast<float*>((char*)p.ws + tile_bytes(pl, p.B, p.heads, p.c.tokens, p.d));
     sp.part_ml = reinterpret_cast<float2*>(sp.part_o + part_floats(pl, p.d));
   }
   hipError_t rc = hipErrorInvalidValue;

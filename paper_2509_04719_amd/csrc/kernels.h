@@ -220,6 +220,9 @@ struct AttnQParams {
   size_t ws_bytes;
 };
 size_t attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int d, int dtype);
+// what a call with ws_bytes of workspace runs as; false: not supported
+bool attention_quantized_plan(int B, int heads, int n_q, int n_kv, int d, int dtype, size_t ws_bytes, int* prepared,
+                              int* query_groups, int* key_parts);
 hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream_t stream);
 
 }  // namespace orch

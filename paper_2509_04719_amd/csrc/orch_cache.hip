@@ -185,12 +185,24 @@ int orch_op_kv_dequantize(const orch_quantized_kv* cache, int tok_off, void* kv,
   return launched(launch_kv_dequantize(p, dtype, (hipStream_t)hip_stream), "K/V read-back launch");
 }
 
+// (a shape that the call refuses needs no workspace and has no plan)
+static bool attention_shape(int B, int heads, int n_q, int n_kv, int head_dim, int dtype) {
+  return B >= 1 && heads >= 1 && (long long)B * heads <= 32767 && n_q >= 0 && n_kv >= 1 && head_dim >= 1 &&
+         (dtype == ORCH_F32 || dtype == ORCH_BF16) && (long long)n_q * head_dim < 1ll << 31 && (long long)n_kv * head_dim < 1ll << 31;
+}
+
 size_t orch_attention_quantized_workspace_bytes(int B, int heads, int n_q, int n_kv, int head_dim, int dtype) {
-  // (a shape that the call refuses needs none)
-  if (B < 1 || heads < 1 || (long long)B * heads > 32767 || n_q < 0 || n_kv < 1 || head_dim < 1 ||
-      (dtype != ORCH_F32 && dtype != ORCH_BF16) || (long long)n_q * head_dim >= 1ll << 31 || (long long)n_kv * head_dim >= 1ll << 31)
-    return 0;
+  if (!attention_shape(B, heads, n_q, n_kv, head_dim, dtype)) return 0;
   return attention_quantized_workspace_bytes(B, heads, n_q, n_kv, head_dim, dtype);
+}
+
+int orch_attention_quantized_plan(int B, int heads, int n_q, int n_kv, int head_dim, int dtype, size_t workspace_bytes,
+                                  int* prepared, int* query_groups, int* key_parts) {
+  if (!prepared || !query_groups || !key_parts) return fail("NULL pointer");
+  if (!attention_shape(B, heads, n_q, n_kv, head_dim, dtype) || n_q < 1 ||
+      !attention_quantized_plan(B, heads, n_q, n_kv, head_dim, dtype, workspace_bytes, prepared, query_groups, key_parts))
+    return fail("bad shape");
+  return ORCH_OK;
 }
 
 int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache, const void* kv_fresh, size_t fresh_bs,

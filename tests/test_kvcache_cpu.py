@@ -8,6 +8,7 @@ import pytest
 import torch
 
 from oracle import kvcache as ok
+from tests import _attention_forms as forms
 
 F32, BF16 = 0, 1
 P = [0x10000000 * (i + 1) for i in range(8)]      # addresses far apart, 16-byte aligned
@@ -310,3 +311,28 @@ def test_binding_takes_buffers(orch_lib, monkeypatch, kw):
     for call in _bound(orch_lib, **kw):
         with pytest.raises(Reached):
             call()
+
+
+@pytest.mark.parametrize("d", forms.SIZES)
+@pytest.mark.parametrize("form", forms.FORMS, ids=str)
+def test_every_form_of_the_attention_has_a_shape(orch_lib, form, d):
+    """What the GPU tests of the forms run; a shape with a workspace a byte short runs as without one."""
+    assert forms.shape_for(orch_lib, form, d) is not None
+    for shape in forms.CANDIDATES:
+        a = (*shape, d, forms.CODE[form[0]])
+        need = orch_lib.attention_quantized_workspace_bytes(*a)
+        prepared, _, parts = whole = orch_lib.attention_quantized_plan(*a, need)
+        without = orch_lib.attention_quantized_plan(*a, 0)
+        assert (need > 0) == (prepared or parts > 1) and not without[0] and without[2] == 1
+        assert orch_lib.attention_quantized_plan(*a, need + 1) == whole
+        if need:
+            assert orch_lib.attention_quantized_plan(*a, need - 1) == without
+
+
+@pytest.mark.parametrize("bad", [dict(B=0), dict(heads=0), dict(n_q=0), dict(n_kv=0), dict(d=40), dict(dtype=7), dict(n_q=1 << 25),
+                                 dict(B=40000)])
+def test_no_plan_for_bad_shapes(orch_lib, bad):
+    a = dict(B=1, heads=2, n_q=1, n_kv=4096, d=64, dtype=BF16) | bad
+    with pytest.raises(orch_lib.OrchError, match="shape"):
+        orch_lib.attention_quantized_plan(*a.values(), 0)
+    assert orch_lib.lib.orch_attention_quantized_plan(1, 2, 1, 4096, 64, BF16, 0, None, None, None) == orch_lib.ORCH_EINVAL
