@@ -166,6 +166,12 @@ def _stream_on(stream, *devices):
     return torch._C._cuda_getCurrentRawStream(cur) if stream is None else stream.cuda_stream
 
 
+def _check_ints(*values):
+    """What a C int holds: ctypes wraps the rest silently."""
+    if max(values) > 0x7fffffff or min(values) < -0x80000000:
+        raise OrchError(ORCH_EINVAL, f"{values}: past an int's range")
+
+
 _CODES = {}             # by torch type, filled at the first use (torch is not imported before)
 
 
@@ -331,6 +337,7 @@ def attention(q, kv_stale, stale_bs, kv_fresh, fresh_bs, fresh_begin, n_fresh, B
 def rotary_axes(channels, extent, theta=1e4, origin=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0),
                 interleaved=True) -> RotaryAxes:
     """Rotary positions of a (frames, rows, columns) grid, see orch_rotary_axes."""
+    _check_ints(*channels, *extent)
     return RotaryAxes((C.c_int * 3)(*channels), (C.c_int * 3)(*extent), (C.c_double * 3)(*origin),
                       (C.c_double * 3)(*step), float(theta), int(interleaved))
 
@@ -341,6 +348,7 @@ _ROTARY_TENSOR = struct.Struct("=QQi4x6Q")     # RotaryTensor's layout
 def rotary(axes: RotaryAxes, token_begin, x, out, stream=None):
     """Rotate x into out: tensors (or pairs of tensors, e.g. Q and K) [B, heads, n_tok, d] of any
     strides, their channels next to each other.  out may be x."""
+    _check_ints(token_begin, 0)
     xs, outs = (x, out) if isinstance(x, (tuple, list)) else ((x,), (out,))
     B, _, n_tok, d = xs[0].shape
     dtype = xs[0].dtype
@@ -405,6 +413,7 @@ def kv_quantize(kv, kv_branch_stride, kv_tokens, kv_offset, cache: QuantizedKV, 
                 n_tok, head_dim, dtype, stream=None):
     _check_cache(cache, B, heads, head_dim)
     _check_kv("kv", kv, dtype, kv_branch_stride, kv_tokens, B, heads, head_dim)
+    _check_ints(kv_offset, tok_offset, n_tok, kv_tokens)
     st = _stream_on(stream, kv.get_device(), *cache.devices)
     check(lib.orch_op_kv_quantize(kv.data_ptr(), kv_branch_stride, kv_tokens, kv_offset, C.byref(cache),
                                   tok_offset, B, heads, n_tok, head_dim, dtype, st))
@@ -414,6 +423,7 @@ def kv_dequantize(cache: QuantizedKV, tok_offset, kv, kv_branch_stride, kv_token
                   n_tok, head_dim, dtype, stream=None):
     _check_cache(cache, B, heads, head_dim)
     _check_kv("kv", kv, dtype, kv_branch_stride, kv_tokens, B, heads, head_dim)
+    _check_ints(kv_offset, tok_offset, n_tok, kv_tokens)
     st = _stream_on(stream, kv.get_device(), *cache.devices)
     check(lib.orch_op_kv_dequantize(C.byref(cache), tok_offset, kv.data_ptr(), kv_branch_stride, kv_tokens,
                                     kv_offset, B, heads, n_tok, head_dim, dtype, st))
@@ -437,6 +447,7 @@ def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, 
     _check_buffer("out", out, dtype, B * n_q * heads * head_dim)
     if n_fresh > 0 and kv_fresh is not None:
         _check_kv("kv_fresh", kv_fresh, dtype, fresh_bs, n_fresh, B, heads, head_dim)
+    _check_ints(n_q, fresh_begin, n_fresh)
     if workspace is not None and not workspace.is_contiguous():
         raise OrchError(ORCH_EINVAL, "workspace must be contiguous")
     ws_bytes = 0 if workspace is None else workspace.nbytes

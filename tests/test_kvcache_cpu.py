@@ -336,3 +336,35 @@ def test_no_plan_for_bad_shapes(orch_lib, bad):
     with pytest.raises(orch_lib.OrchError, match="shape"):
         orch_lib.attention_quantized_plan(*a.values(), 0)
     assert orch_lib.lib.orch_attention_quantized_plan(1, 2, 1, 4096, 64, BF16, 0, None, None, None) == orch_lib.ORCH_EINVAL
+
+
+@pytest.mark.parametrize("big", [2 ** 31, 2 ** 32, 2 ** 32 + 4, -2 ** 31 - 1, -2 ** 32, 2 ** 64])
+def test_binding_refuses_what_a_c_int_does_not_hold(orch_lib, monkeypatch, big):
+    """ctypes would wrap it: 2^32 + 4 would be token 4."""
+    class Reached(Exception):
+        pass
+
+    def on(*_):
+        raise Reached
+
+    monkeypatch.setattr(orch_lib, "_stream_on", on)
+    x = torch.zeros((1, 2, 4, 32))
+    for axes in (dict(extent=(1, 4, big)), dict(extent=(big, 1, 4)), dict(channels=(0, big, 16))):
+        with pytest.raises(orch_lib.OrchError, match="int"):
+            orch_lib.rotary_axes(**(dict(channels=(0, 16, 16), extent=(1, 4, 4)) | axes))
+    with pytest.raises(orch_lib.OrchError, match="int"):
+        orch_lib.rotary(orch_lib.rotary_axes((0, 16, 16), (1, 4, 4)), big, x, x)
+    cache = orch_lib.quantized_kv(torch.zeros((1, 2, 2, 8, 32), dtype=torch.uint8), torch.zeros((1, 2, 2, 8), dtype=torch.uint8))
+    kv, q, out = torch.zeros(2 * 8 * 64), torch.zeros((1, 2, 4, 32)), torch.zeros((1, 4, 64))
+    for kv_off, off, n in ((big, 0, 4), (0, big, 4), (0, 0, big)):
+        with pytest.raises(orch_lib.OrchError, match="int"):
+            orch_lib.kv_quantize(kv, 0, 8, kv_off, cache, off, 1, 2, n, 32, F32)
+        with pytest.raises(orch_lib.OrchError, match="int"):
+            orch_lib.kv_dequantize(cache, off, kv, 0, 8, kv_off, 1, 2, n, 32, F32)
+    for fb, nf, n_q in ((big, 4, 4), (0, 4, big), (0, big, 4)):
+        with pytest.raises(orch_lib.OrchError, match="int|holds"):
+            orch_lib.attention_quantized(q, cache, kv, 0, fb, nf, 1, 2, n_q, 32, out, F32)
+    for call in (lambda: orch_lib.kv_quantize(kv, 0, 8, 2, cache, 3, 1, 2, 4, 32, F32),
+                 lambda: orch_lib.attention_quantized(q, cache, kv, 0, 4, 4, 1, 2, 4, 32, out, F32)):
+        with pytest.raises(Reached):
+            call()
