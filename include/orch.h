@@ -419,7 +419,7 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
  * scale, so a band of tokens is a set of contiguous runs (one per head for each of
  * K and V) whatever its offset, and a token's bytes depend on that token alone.
  * values_stride % 16 == 0.  A branch's exponents may lie behind its values (both strides the same), so
- * that a branch is one run of bytes. */
+ * that a branch is one run of bytes.  Strides here and below are under 2^40. */
 typedef struct {
   void* values;
   void* exponents;

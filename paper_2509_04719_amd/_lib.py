@@ -406,6 +406,8 @@ def _check_buffer(name, t, dtype, elements, branch_stride=0):
 
 
 def _check_kv(name, kv, dtype, branch_stride, tokens, B, heads, head_dim):
+    if branch_stride < 0:
+        raise OrchError(ORCH_EINVAL, f"{name}: branch stride {branch_stride}")
     _check_buffer(name, kv, dtype, (B - 1) * branch_stride + 2 * tokens * heads * head_dim, branch_stride)
 
 

@@ -56,6 +56,9 @@ bool overlap(const Runs& a, const Runs& b) {
   return false;
 }
 
+// No stride is as long as this (elements or bytes: 1 TB and more); below it no offset wraps.
+constexpr size_t kFar = (size_t)1 << 40;
+
 // heads, branches, head size and type that every entry point takes
 int check_common(int B, int heads, int head_dim, int dtype) {
   if (B < 1 || heads < 1 || (long long)B * heads > 32767) return fail("bad shape: B and heads must be >= 1, B * heads <= 32767");
@@ -71,7 +74,8 @@ int check_cache(const orch_quantized_kv* c, int B, int heads, int d, Runs* value
   if (c->tokens < 1) return fail("the cache's tokens must be >= 1");
   if ((long long)c->tokens * d >= 1ll << 31) return fail("cache tokens * head_dim must be below 2^31");
   const size_t e = (size_t)2 * heads * c->tokens, v = e * d;
-  if (B > 1 && (c->values_stride < v || c->exponents_stride < e)) return fail("the cache's branch stride is too small");
+  if (B > 1 && (c->values_stride < v || c->exponents_stride < e || c->values_stride >= kFar || c->exponents_stride >= kFar))
+    return fail("the cache's branch stride is too small or past 2^40");
   if (!aligned16(c->values) || (B > 1 && c->values_stride % 16)) return fail("cache values must be 16-byte aligned");
   *values = {c->values, v, c->values_stride, B};
   *exps = {c->exponents, e, c->exponents_stride, B};
@@ -93,7 +97,7 @@ int kv_params(KvCacheParams* p, const void* kv, size_t kv_bs, int kv_tokens, int
                 c_off, n, c->tokens);
   if ((long long)kv_tokens * d >= 1ll << 31) return fail("kv_tokens * head_dim must be below 2^31");
   const size_t es = dtype == ORCH_BF16 ? 2 : 4, H = (size_t)heads * d, elems = 2 * (size_t)kv_tokens * H;
-  if (B > 1 && kv_bs < elems) return fail("branch stride too small");
+  if (B > 1 && (kv_bs < elems || kv_bs >= kFar)) return fail("branch stride too small or past 2^40");
   if (!aligned16(kv) || (B > 1 && kv_bs * es % 16)) return fail("the K/V buffer must be 16-byte aligned");
   const Runs buffer = {kv, elems * es, kv_bs * es, B};
   if (overlap(buffer, values) || overlap(buffer, exps))
@@ -150,8 +154,9 @@ int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tenso
     if ((uintptr_t)t.x % es || (uintptr_t)t.out % es) return fail("tensors must be aligned to their elements");
     const int extent[3] = {B, t.heads, n_tok};
     for (int a = 0; a < 3; ++a)
-      if (n_tok > 0 && extent[a] > 1 && (t.x_stride[a] < (size_t)head_dim || t.out_stride[a] < (size_t)head_dim))
-        return fail("strides must be at least head_dim");
+      if (n_tok > 0 && extent[a] > 1 && (t.x_stride[a] < (size_t)head_dim || t.out_stride[a] < (size_t)head_dim ||
+                                         t.x_stride[a] >= kFar || t.out_stride[a] >= kFar))
+        return fail("strides must be at least head_dim and below 2^40");
     p.t[k].x = t.x; p.t[k].out = t.out; p.t[k].heads = t.heads;
     for (int a = 0; a < 3; ++a) {
       // (the stride of an extent of one is never used)
@@ -219,7 +224,7 @@ int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache, c
   if ((long long)n_q * head_dim >= 1ll << 31) return fail("n_q * head_dim must be below 2^31");
   const size_t es = dtype == ORCH_BF16 ? 2 : 4, H = (size_t)heads * head_dim;
   const size_t fresh_elems = 2 * (size_t)n_fresh * H, q_bytes = (size_t)B * n_q * H * es;
-  if (n_fresh > 0 && B > 1 && fresh_bs < fresh_elems) return fail("branch stride too small");
+  if (n_fresh > 0 && B > 1 && (fresh_bs < fresh_elems || fresh_bs >= kFar)) return fail("branch stride too small or past 2^40");
   if (!aligned16(q) || !aligned16(out) || (n_fresh > 0 && (!aligned16(kv_fresh) || (B > 1 && fresh_bs * es % 16))) ||
       (workspace && !aligned16(workspace)))
     return fail("device buffers must be 16-byte aligned");

@@ -368,3 +368,25 @@ def test_binding_refuses_what_a_c_int_does_not_hold(orch_lib, monkeypatch, big):
                  lambda: orch_lib.attention_quantized(q, cache, kv, 0, 4, 4, 1, 2, 4, 32, out, F32)):
         with pytest.raises(Reached):
             call()
+
+
+@pytest.mark.parametrize("stride", [2 ** 40, 2 ** 63, 2 ** 64 - 16 * 1024, 2 ** 61 + 2048, 2 ** 62 + 4096])
+def test_strides_that_wrap_are_refused(orch_lib, stride):
+    """No branch lies 2^40 away; past 2^61 or so the offsets would wrap, before the buffer's start too."""
+    for back in (False, True):
+        _refused(orch_lib, _move(orch_lib, back, B=2, bs=stride), "stride")
+        for c in (dict(vs=stride), dict(es=stride)):
+            _refused(orch_lib, _move(orch_lib, back, B=2, cache=c), "stride")
+    _refused(orch_lib, _attend(orch_lib, B=2, bs=stride), "stride")
+    _refused(orch_lib, _attend(orch_lib, B=2, cache=dict(vs=stride)), "stride")
+    for a in range(3):
+        xs = [256, 128, 32]
+        xs[a] = stride
+        _refused(orch_lib, _rotary(orch_lib, B=2, tensors=[dict(xs=xs)]), "strides")
+        _refused(orch_lib, _rotary(orch_lib, B=2, tensors=[dict(os=xs)]), "strides")
+
+
+def test_negative_branch_strides_are_refused(orch_lib):
+    for call in _bound(orch_lib, bs=-2 * 8 * 96):
+        with pytest.raises(orch_lib.OrchError, match="stride"):
+            call()
