@@ -163,7 +163,11 @@ def _stream_on(stream, *devices):
     for d in devices:
         if d != cur:
             raise OrchError(ORCH_EINVAL, f"a tensor is on {'the host' if d < 0 else f'GPU {d}'}, the current GPU is {cur}")
-    return torch._C._cuda_getCurrentRawStream(cur) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(cur)
+    if stream.device_index != cur:
+        raise OrchError(ORCH_EINVAL, f"the stream is on GPU {stream.device_index}, the current GPU is {cur}")
+    return stream.cuda_stream
 
 
 def _check_ints(*values):

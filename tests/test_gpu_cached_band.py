@@ -218,3 +218,22 @@ def test_an_empty_band(orch_lib, dtype):
     orch_lib.kv_quantize(empty((2, 8 * 128), dtype), 8 * 128, 8, 3, x.cache, 5, 2, 2, 0, 32, code(dtype))
     torch.cuda.synchronize()
     assert torch.equal(before, x.values.view(torch.uint8))
+
+
+def test_a_stream_given(orch_lib):
+    """The stream argument: the same bits as on the current stream."""
+    x = Band(orch_lib, "bf16", 2, 4, 72, 8, 8, 5)
+    q, kv, _, ws = x.buffers(3)
+    x.project(x.inputs(3), 3, q, kv)
+    torch.cuda.synchronize()
+    results = []
+    for stream in (None, torch.cuda.Stream()):
+        qo, out, back = torch.zeros_like(q), empty((2, 24, x.H), "bf16"), torch.zeros_like(kv)
+        torch.cuda.synchronize()
+        orch_lib.rotary(x.axes, 8, q, qo, stream=stream)
+        orch_lib.kv_quantize(kv, 2 * 24 * x.H, 24, 0, x.cache, 8, 2, 4, 24, 72, 1, stream=stream)
+        orch_lib.attention_quantized(qo, x.cache, kv, 2 * 24 * x.H, 8, 24, 2, 4, 24, 72, out, 1, workspace=ws, stream=stream)
+        orch_lib.kv_dequantize(x.cache, 8, back, 2 * 24 * x.H, 24, 0, 2, 4, 24, 72, 1, stream=stream)
+        torch.cuda.synchronize()
+        results.append((qo, out, back))
+    assert all(torch.equal(a, b) for a, b in zip(*results))

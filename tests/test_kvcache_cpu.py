@@ -390,3 +390,17 @@ def test_negative_branch_strides_are_refused(orch_lib):
     for call in _bound(orch_lib, bs=-2 * 8 * 96):
         with pytest.raises(orch_lib.OrchError, match="stride"):
             call()
+
+
+def test_binding_refuses_a_stream_of_another_gpu(orch_lib, monkeypatch):
+    class Stream:
+        cuda_stream = 7
+
+        def __init__(self, device):
+            self.device_index = device
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    assert orch_lib._stream_on(Stream(0), 0, 0) == 7
+    for stream, device in ((Stream(1), 0), (Stream(0), 1), (Stream(1), 1), (Stream(0), -1)):
+        with pytest.raises(orch_lib.OrchError, match="current GPU"):
+            orch_lib._stream_on(stream, device)
