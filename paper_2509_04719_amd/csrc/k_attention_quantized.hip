@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
   auto k_dst = [&](int i) __attribute__((always_inline)) { return G::EVEN ? k_dst_[0] + i * KS * G::KP : k_dst_[i]; };
   auto v_dst = [&](int i) __attribute__((always_inline)) { return ROW ? v_dst_[0] + vrow(i / CPL * KR) * G::VP + i % CPL * 16 : G::EVEN ? v_dst_[0] + vrow(i * KS) * G::VP : v_dst_[i]; };
   // fresh V^T: slot i holds chunk vtid % 8 (8 keys) of channel vtid / 8 + i TH / 8
-  const int vt_src = (vtid >> 3) * nf + (vtid & 7) * 8;
+  const unsigned vt_src = 2u * ((unsigned)(vtid >> 3) * (unsigned)nf + (vtid & 7) * 8);     // bytes, below 2^32
   const int vt_dst_ = G::ST * G::KS + (vtid >> 3) * 128 + ((vtid & 7) ^ ((vtid >> 4) & 7)) * 16;
   auto vt_dst = [&](int i) __attribute__((always_inline)) {
     return (TH % 128 == 0 || i % 2 == 0 ? vt_dst_ : vt_dst_ ^ 64) + i * TH * 16;   // (64 threads: 8 rows on, 4 in the swizzle)
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     } else {
       // (rows of V^T start at any element)
       const char* base = reinterpret_cast<const char*>(vf + (t * BKV - fb) + (size_t)i * (TH / 8) * nf);
-      const u32x4_u x = *reinterpret_cast<const u32x4_u*>(base + (unsigned)(vt_src * 2));
+      const u32x4_u x = *reinterpret_cast<const u32x4_u*>(base + vt_src);
       return u32x4{x[0], x[1], x[2], x[3]};
     }
   };

@@ -305,3 +305,28 @@ def test_error_is_the_rounding_of_the_output(orch_lib, d, B, heads, n_q, N, fb, 
         err = rel_l2(run(orch_lib, "bf16", q, v8, e8, fk, fv, fb, split), ok.attention(q, K, V))
         print(f"\n[d {d} {heads} heads, {n_q} queries x {N} keys, split {split}] {err:.3e}", flush=True)
         assert err <= 1.75e-3
+
+
+@pytest.mark.parametrize("n_q,groups", [(2, 1), (1000, 4)])
+def test_a_long_band(orch_lib, n_q, groups):
+    """A band of nearly 2^31 channels a head, its rows of V^T more than 2^31 bytes apart within a workgroup's reach; all but a
+    few keys at scores 224 below 0, whose probabilities are 0 in fp32."""
+    d, N = 32, 2 ** 26 - 64
+    at = np.array([0, 1, 77, 2 ** 25 + 5, 2 ** 26 - 200, N - 1])
+    values = torch.full((1, 2, 1, N, d), 0x7f, dtype=torch.uint8, device=DEV)           # not to be read
+    exps = torch.full((1, 2, 1, N), 127, dtype=torch.uint8, device=DEV)
+    fresh = torch.zeros(2 * N * d, dtype=torch.bfloat16, device=DEV)
+    k, vt = fresh[:N * d].view(N, d), fresh[N * d:].view(d, N)
+    k[:, 0] = -448.0 * 2 ** 0.5 / 2                                                     # times 4 / sqrt(32): -224
+    vt[:] = 2.0
+    q, _, _, fk, fv, K, V = make(np.random.default_rng(14), "bf16", 1, 1, d, n_q, len(at), 0, len(at))
+    q[..., 0], K[..., 0], fk[..., 0] = 4.0, 0.0, 0.0
+    for i, n in enumerate(at):
+        k[n], vt[:, n] = to_dev(fk[0, 0, i], "bf16"), to_dev(fv[0, 0, i], "bf16")
+    cache = orch_lib.quantized_kv(values, exps)
+    need = orch_lib.attention_quantized_workspace_bytes(1, 1, n_q, N, d, 1)
+    assert orch_lib.attention_quantized_plan(1, 1, n_q, N, d, 1, need)[1] == groups
+    for ws in (None, torch.empty(need, dtype=torch.uint8, device=DEV)):
+        out = torch.empty((1, n_q, d), dtype=torch.bfloat16, device=DEV)
+        orch_lib.attention_quantized(to_dev(q, "bf16"), cache, fresh, 0, 0, N, 1, 1, n_q, d, out, 1, workspace=ws)
+        check(to_host(out).reshape(1, n_q, 1, d).transpose(0, 2, 1, 3), "bf16", q, K, V)
