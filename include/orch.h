@@ -457,9 +457,11 @@ int orch_op_kv_dequantize(const orch_quantized_kv* cache, int tok_offset, void* 
  * again), and the output is rounded once.  workspace: device memory (16-byte aligned) of at
  * least orch_attention_quantized_workspace_bytes() bytes, one call's at a time,
  * lets few queries split the keys over more workgroups, and many queries have the
- * keys widened once for all; NULL (or fewer bytes) runs without either.  The
- * result does not depend on that beyond rounding, and is the same bits at every
- * call.  Errors: ORCH_EINVAL (as orch_op_attention; alignment; tokens * head_dim of
+ * keys widened once for all (4.1 to 4.5 bytes an element of the cache's K); NULL
+ * (or fewer bytes) runs without either.  Which form runs, and with it the order
+ * of a query's sums, goes by the shape, with NULL too (in fp32 with NULL it is
+ * fixed by the keys alone).  The result does not depend on that beyond rounding,
+ * and is the same bits at every call.  Errors: ORCH_EINVAL (as orch_op_attention; alignment; tokens * head_dim of
  * 2^31 or more; out or workspace overlapping an input), ORCH_EHIP. */
 int orch_op_attention_quantized(const void* q, const orch_quantized_kv* cache,
                                 const void* kv_fresh, size_t fresh_branch_stride, int fresh_begin,

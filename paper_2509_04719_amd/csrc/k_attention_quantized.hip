@@ -21,11 +21,11 @@
 //               117-122 us; d = 128, 2 x 8 heads, 4096 x 4096 185 us (743).
 //   NW = 4      without a workspace, or too few queries to pay for it: four waves of 32 queries share each tile, each
 //               widens a quarter of it.  1664 x 1024 keys 43 us; d = 128, 2 x 8 heads, 45 x 2025, keys split 12 ways:
-//               19 us with the parts.
+//               14.6 us and 5 for the parts.
 //   NW = 1      few queries: four waves have the same 32 queries and each a quarter of the keys, without a barrier,
 //               K from memory straight to the products' operand (through LDS: 4% longer at d = 72, 20% at 80 to 128).
-//               384 x 1024 keys 18 us, 384 x 4096 45; one query x 16384 keys of 8 heads of 72 13.4 with its parts.
-//   fp32        the same on v_mfma_f32_32x32x2: 512 x 1024 keys, 4 heads of 32: 8.4 us.
+//               384 x 1024 keys 17.5 us, 384 x 4096 45; one query x 16384 keys of 8 heads of 72 13.4 with its parts.
+//   fp32        the same on v_mfma_f32_32x32x2: 512 x 1024 keys, 4 heads of 32: 8.5 us.
 // With a workspace each may also split the keys of a query tile over workgroups; a merge kernel joins the parts.
 #include <cfloat>
 
@@ -918,7 +918,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
 // paid in full next to its MFMAs: with many queries the keys are widened once, fresh and cached ones
 // together, into tiles that lie in memory as they will in LDS: K rows of KP bytes, V^T rows of 64 keys
 // with their 16-byte chunks swizzled by row (keys past the last are zeros).  Bound by memory: 16384 keys, 2 x 16 heads
-// of 72 (51 MB read of HBM, 148 written) in 50 us, 4.0 TB/s.
+// of 72 (53 MB read of HBM, 152 written) in 50 us, 4.1 TB/s.
 template <int D>
 __global__ __launch_bounds__(256) void attn_q8_prepare_kernel(AttnQParams p, char* tiles) {
   using G = Geo<D, 4, true>;
@@ -1220,7 +1220,7 @@ __global__ __launch_bounds__(64 * Geo32<D>::KG, Geo32<D>::KG / 4) void attn_q8_f
 // The parts of a query tile whose keys ns workgroups shared: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s
 // - m) l_s, m = max_s m_s.  A thread per 4 channels of a query and share of the parts (part s of
 // share s % SG, four in flight), the shares met in LDS in their order.  Bound by its own launch and one chain of loads
-// for few parts (3.5 us), by their bytes for many (384 queries x 5 parts, 2 x 16 heads of 72: 18 MB in 5.5 us).
+// for few parts (3.5-5 us), by their bytes for many (384 queries x 5 parts, 2 x 16 heads of 72: 18 MB in 5.5 us).
 template <typename T, int SG>
 __global__ __launch_bounds__(256) void attn_q8_merge_kernel(AttnQParams p, Split sp, int rows) {
   __shared__ float ml_s[256][2];
