@@ -406,7 +406,7 @@ typedef struct {
  * An out that overlaps an x or another out in any other way than in place, or
  * whose rows overlap each other, gives undefined values.  Errors: ORCH_EINVAL
  * (axes, angles past fp64's range, tokens outside the grid, strides shorter than
- * head_dim, out at x with other strides, NULL, the same buffer in both tensors). */
+ * head_dim or of 2^40, out at x with other strides, NULL, the same buffer in both tensors). */
 int orch_op_rotary(const orch_rotary_axes* axes, const orch_rotary_tensor* tensors, int n_tensors,
                    int B, int n_tok, int token_begin, int head_dim, int dtype, void* hip_stream);
 

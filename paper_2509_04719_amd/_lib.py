@@ -449,8 +449,9 @@ def attention_quantized_plan(B, heads, n_q, n_kv, head_dim, dtype, workspace_byt
 def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, n_fresh, B, heads, n_q,
                         head_dim, out, dtype, workspace=None, stream=None):
     _check_cache(cache, B, heads, head_dim)
-    _check_buffer("q", q, dtype, B * n_q * heads * head_dim)
-    _check_buffer("out", out, dtype, B * n_q * heads * head_dim)
+    for name, t in (("q", q), ("out", out)):
+        if t is not None:
+            _check_buffer(name, t, dtype, B * n_q * heads * head_dim)
     if n_fresh > 0 and kv_fresh is not None:
         _check_kv("kv_fresh", kv_fresh, dtype, fresh_bs, n_fresh, B, heads, head_dim)
     _check_ints(n_q, fresh_begin, n_fresh)

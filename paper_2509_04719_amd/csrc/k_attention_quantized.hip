@@ -503,7 +503,7 @@ __global__ __launch_bounds__(256, (Geo<D, NW, PREP>::WPE)) void attn_q8_kernel(A
     }
   };
   // The probabilities of a half, p = hi + lo: hi the top 16 bits of p, lo what is left of p (1 + 2^-23) as a bf16.  Both
-  // are positive, so that an infinite V gives hi V + lo V = V, not a NaN.
+  // are positive (down to p = 2^-103), so that an infinite V gives hi V + lo V = V, not a NaN.
   struct Prob {
     bf16x8 hi[2], lo[2];
   };

@@ -404,3 +404,13 @@ def test_binding_refuses_a_stream_of_another_gpu(orch_lib, monkeypatch):
     for stream, device in ((Stream(1), 0), (Stream(0), 1), (Stream(1), 1), (Stream(0), -1)):
         with pytest.raises(orch_lib.OrchError, match="current GPU"):
             orch_lib._stream_on(stream, device)
+
+
+def test_binding_without_a_tensor(orch_lib, monkeypatch):
+    """None is the library's to refuse, as a NULL pointer."""
+    monkeypatch.setattr(orch_lib, "_stream_on", lambda *_: 0)
+    cache = orch_lib.quantized_kv(torch.zeros((1, 2, 2, 8, 32), dtype=torch.uint8), torch.zeros((1, 2, 2, 8), dtype=torch.uint8))
+    x = torch.zeros((1, 2, 4, 32))
+    for q, out, fresh in ((None, x, x), (x, None, x), (x, x, None)):
+        with pytest.raises(orch_lib.OrchError, match="NULL"):
+            orch_lib.attention_quantized(q, cache, fresh, 0, 0, 1, 1, 2, 4, 32, out, F32)
