@@ -227,10 +227,10 @@ def test_buffers_that_share_bytes_with_a_branch_are_refused(orch_lib, at):
     quantize, back, _ = _record(orch_lib, stride=1 << 16, kv=P[2] + at, bs=1 << 15)
     assert quantize == back == orch_lib.ORCH_EINVAL
     assert "overlap" in orch_lib.last_error()
-    # the output of an attention (2 x 3 branches of 8 queries of 2 x 32 channels: 3072 bytes)
+    # the output of an attention (3 branches of 9 queries of 2 x 32 channels: 3456 bytes)
     c = dict(vs=1 << 16, es=1 << 16, exponents=P[2] + 8192)
-    _refused(orch_lib, _attend(orch_lib, B=3, n_q=8, out=P[2] + 65536 + 8448 - 16, cache=c), "overlap")
-    _refused(orch_lib, _attend(orch_lib, B=3, n_q=8, out=P[2] + 2 * 65536 - 3072 + 16, cache=c), "overlap")
+    _refused(orch_lib, _attend(orch_lib, B=3, n_q=9, out=P[2] + 65536 + 8448 - 16, cache=c), "overlap")
+    _refused(orch_lib, _attend(orch_lib, B=3, n_q=9, out=P[2] + 2 * 65536 - 3456 + 16, cache=c), "overlap")
 
 
 def test_no_tokens_need_no_buffers(orch_lib):
