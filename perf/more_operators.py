@@ -211,7 +211,7 @@ def prepare(case, seed):
         if c["kind"] != "norms":
             s["W8"] = _lib.int8_rows(s["w"], s["w_s"])
             s["A8"] = _lib.int8_rows(s["a"], s["a_s"])
-            need = _lib.linear_int8_workspace_bytes(rows, c["N"], c["K"])
+            need = _lib.linear_quantized_workspace_bytes(rows, c["N"], c["K"])
             s["workspace"] = torch.empty(need, dtype=torch.uint8, device=DEV) if need else None
     return s
 
@@ -288,15 +288,15 @@ def _run_plain(s):
 def _own_product(lib, s):
     c = s["case"]
     if c["epilogue"] == "qkv":
-        lib.qkv_projection_int8(s["A8"], s["W8"], s["bias"], s["q"], s["kv"], c["tokens"], c["tok_offset"],
+        lib.qkv_projection_quantized(s["A8"], s["W8"], s["bias"], s["q"], s["kv"], c["tokens"], c["tok_offset"],
                                 workspace=s["workspace"])
         return [s["q"], s["kv"]]
     if c["epilogue"] == "residual":
         s["prod"].copy_(s["res"])
-        lib.linear_int8(s["A8"], s["W8"], s["bias"], lib.EPI_RESIDUAL, s["prod"], gate=s["gate"],
+        lib.linear_quantized(s["A8"], s["W8"], s["bias"], lib.EPI_RESIDUAL, s["prod"], gate=s["gate"],
                         rows_per_batch=c["n_tok"], workspace=s["workspace"])
     else:
-        lib.linear_int8(s["A8"], s["W8"], s["bias"], lib.EPI_GELU if c["epilogue"] == "gelu" else lib.EPI_STORE,
+        lib.linear_quantized(s["A8"], s["W8"], s["bias"], lib.EPI_GELU if c["epilogue"] == "gelu" else lib.EPI_STORE,
                         s["prod"], workspace=s["workspace"])
     return [s["prod"]]
 
