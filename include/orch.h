@@ -481,6 +481,106 @@ int orch_attention_quantized_plan(int B, int heads, int n_q, int n_kv, int head_
                                   size_t workspace_bytes, int* prepared, int* query_groups,
                                   int* key_parts);
 
+/* ---- norms around a block, products in 8-bit integers ------------------------
+ * For blocks that normalise what they read and what they write: one pass between two
+ * blocks in place of a gated residual and a LayerNorm.  For projections at twice the
+ * bf16 matrix rate and half its bytes: int8 rows with a scale each (a token's
+ * activations, an output channel's weights), written by orch_op_quantize_rows or
+ * by the norms themselves, and their products.  A block's MLP is orch_op_block_norms ->
+ * orch_op_linear_quantized (GELU) -> orch_op_quantize_rows -> orch_op_linear_quantized ->
+ * orch_op_block_norms of the next one. */
+
+/* int8 rows with a scale each: element (r, c) stands for values[r * stride + c] *
+ * scales[r].  values 16-byte aligned, stride in bytes, a multiple of 16 below 2^23
+ * (not used for a single row).  Bytes between a row's end and the next row are
+ * neither read as values nor written. */
+typedef struct {
+  void* values;
+  float* scales;
+  size_t stride;
+} orch_int8_rows;
+
+enum { ORCH_NORM_NONE = 0, ORCH_NORM_LAYER = 1, ORCH_NORM_RMS = 2 };
+
+/* A norm over a row's `hidden` channels: LAYER (x - mean) / sqrt(var + eps), biased
+ * variance; RMS x / sqrt(mean x^2 + eps); NONE x (eps not used); then times weight plus
+ * bias, fp32 [hidden], each NULL for none.  eps finite and > 0. */
+typedef struct {
+  int kind;
+  float eps;
+  const float* weight;
+  const float* bias;
+} orch_norm;
+
+/* The pass between two blocks on `rows` tokens of `hidden` channels:
+ *   h' = residual_scale * h + gate[b] * post(y)      written to h_out
+ *   u  = pre(h') * (1 + scale[b]) + shift[b]         written to out, or to out8
+ * with b = row / rows_per_batch.  y is the output of the block that ends; NULL: none
+ * does, h' = residual_scale * h, and post and gate are not used.  h_out NULL: h' is not
+ * wanted.  out and out8 both NULL: no block follows; pre, shift and scale are not used.
+ * gate, shift and scale: fp32 rows b of mod_stride elements each, NULL for 1, 0 and 0
+ * (a learned scale per channel is a gate of one row, rows_per_batch = rows).
+ * Strides are those of the rows, in elements, at least hidden and below 2^40 (out8's
+ * are its own); y and out are T, the rest fp32. */
+typedef struct {
+  orch_norm post, pre;
+  float residual_scale;
+  int rows, hidden, rows_per_batch;
+  const float* h;
+  const void* y;
+  const float *gate, *shift, *scale;
+  float* h_out;
+  void* out;
+  const orch_int8_rows* out8;
+  size_t h_stride, y_stride, mod_stride, h_out_stride, out_stride;
+} orch_block_norms;
+
+/* One pass over memory, everything in fp32 (statistics of two passes over the row in
+ * registers), one rounding to T.  out8: as orch_op_quantize_rows of u, which is not
+ * rounded to T before.  h_out may be h and out may be y, with the same strides.  Any
+ * element-aligned address and stride is taken; four channels an access where all
+ * rows are aligned to it.  No rows are no error.  Errors: ORCH_EINVAL (kinds, eps, hidden
+ * outside 1 .. 32768, 2^24 rows or more, strides, alignment, neither h_out nor out nor out8, both
+ * out and out8, an output that overlaps another buffer otherwise), ORCH_EHIP. */
+int orch_op_block_norms(const orch_block_norms* p, int dtype, void* hip_stream);
+
+/* Rows of x (T, x_stride elements apart) to int8 with a scale each: q = x * (127 / m) to
+ * nearest, ties to even, m the row's largest magnitude, quotient and product rounded to
+ * fp32 (of 2^64 x where m < 2^-64); scale m / 127.  A row of zeros: codes and scale 0.  A row with
+ * an infinity or NaN: codes 0 and scale NaN, so that every product of it is NaN.  For activations
+ * the rows are tokens, for weights output channels.  No rows are no error.  Errors:
+ * ORCH_EINVAL (cols outside 1 .. 131071, 2^24 rows or more, strides, alignment, overlap), ORCH_EHIP. */
+int orch_op_quantize_rows(const void* x, size_t x_stride, int rows, int cols,
+                          const orch_int8_rows* out, int dtype, void* hip_stream);
+
+/* orch_op_linear in 8-bit integers: y[m][n] = (sum_k A[m][k] W[n][k]) * A's scale of m *
+ * W's scale of n + bias[n], M rows of A and N of W, K channels; epilogues, gate, out and its
+ * type T as there.  The sums are exact: an output depends on its rows alone, never on M or
+ * on how the work is split, and is the same bits at every call.  bias may be NULL.  Any M,
+ * N and K; N a multiple of 8 (4 for fp32) with out (and gate) 16-byte aligned is fastest.
+ * workspace (16-byte aligned, one call's at a time): orch_linear_quantized_workspace_bytes()
+ * bytes let products of few outputs split K over more workgroups; NULL or fewer bytes run
+ * without.  Errors: ORCH_EINVAL (as orch_op_linear; K above 131071, where sums could pass 32 bits; 2^24
+ * tiles of 256 x 128 outputs or more; alignment; out or workspace overlapping an input), ORCH_EHIP. */
+int orch_op_linear_quantized(const orch_int8_rows* A, int M, int K, const orch_int8_rows* W, int N,
+                        const float* bias, int epilogue, const float* gate, size_t gate_stride,
+                        int rows_per_batch, void* out, void* workspace, size_t workspace_bytes,
+                        int dtype, void* hip_stream);
+
+/* Workspace bytes that orch_op_linear_quantized and orch_op_qkv_projection_quantized (N = 3 * hidden)
+ * can use for this shape (0: none). */
+size_t orch_linear_quantized_workspace_bytes(int M, int N, int K);
+
+/* orch_op_qkv_projection in 8-bit integers: A of B * n_tok rows, W of 3 * heads * head_dim
+ * rows, outputs of type T as there; head_dim as in orch_dit_config, heads * head_dim below
+ * 65536, q_out and kv_out 16-byte aligned, kv_branch_stride a multiple of 16 bytes.  Tokens
+ * outside [tok_offset, tok_offset + n_tok) of kv_out are not touched.  Errors as above. */
+int orch_op_qkv_projection_quantized(const orch_int8_rows* A, int B, int n_tok, int K,
+                                const orch_int8_rows* W, const float* bias, int heads,
+                                int head_dim, void* q_out, void* kv_out, size_t kv_branch_stride,
+                                int kv_tokens, int tok_offset, void* workspace,
+                                size_t workspace_bytes, int dtype, void* hip_stream);
+
 /* Conditioning of the loaded model: out fp32 [cfg_batch][6*H*n_blocks + 2*H],
  * the adaLN vectors of every block followed by the final layer's
  * (shift, scale), for timestep t and host labels[cfg_batch]. */

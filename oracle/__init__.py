@@ -26,6 +26,8 @@ Modules:
               with stale halo rows and stale group statistics (§II-B).
   kvcache  -- rotary positions on a grid, the 8-bit K/V cache (e4m3 values,
               power-of-two scales) and attention over it.
+  integer  -- norms around a block with gate and residual scale, rows in
+              8-bit integers with a scale each, and their products.
 
 Parity status: the scheduler, attention, LayerNorm, GELU, sinusoid, patch
 embedding and unpatchify are pinned by the CPU tests; the DiT block as a

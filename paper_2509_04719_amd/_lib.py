@@ -18,6 +18,7 @@ ORCH_OK, ORCH_EINVAL, ORCH_ENOWEIGHTS, ORCH_EHIP, ORCH_ENOMEM = 0, -1, -2, -3, -
 ORCH_F32, ORCH_BF16 = 0, 1
 EPI_STORE, EPI_GELU, EPI_RESIDUAL = 0, 1, 2
 DTYPE_CODE = {"f32": ORCH_F32, "bf16": ORCH_BF16}
+NORM_CODE = {"none": 0, "layer": 1, "rms": 2}
 
 SYMBOLS = (
     "orch_create", "orch_destroy", "orch_load_dit_weights", "orch_stale_kv_bytes",
@@ -31,6 +32,8 @@ SYMBOLS = (
     "orch_unet_conv_workspace_bytes", "orch_op_rotary", "orch_op_kv_quantize",
     "orch_op_kv_dequantize", "orch_op_attention_quantized",
     "orch_attention_quantized_workspace_bytes", "orch_attention_quantized_plan",
+    "orch_op_block_norms", "orch_op_quantize_rows", "orch_op_linear_quantized",
+    "orch_linear_quantized_workspace_bytes", "orch_op_qkv_projection_quantized",
 )
 KCLASSES = ("conditioning", "patch_embed", "layernorm", "qkv_gemm", "attention", "proj_gemm",
             "fc1_gemm", "fc2_gemm", "final_layer", "update")
@@ -60,6 +63,23 @@ class RotaryTensor(C.Structure):
 class QuantizedKV(C.Structure):
     _fields_ = [("values", C.c_void_p), ("exponents", C.c_void_p), ("values_stride", C.c_size_t),
                 ("exponents_stride", C.c_size_t), ("tokens", C.c_int)]
+
+
+class Int8Rows(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("stride", C.c_size_t)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("kind", C.c_int), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class BlockNorms(C.Structure):
+    _fields_ = [("post", Norm), ("pre", Norm), ("residual_scale", C.c_float), ("rows", C.c_int),
+                ("hidden", C.c_int), ("rows_per_batch", C.c_int), ("h", C.c_void_p), ("y", C.c_void_p),
+                ("gate", C.c_void_p), ("shift", C.c_void_p), ("scale", C.c_void_p), ("h_out", C.c_void_p),
+                ("out", C.c_void_p), ("out8", C.POINTER(Int8Rows)), ("h_stride", C.c_size_t),
+                ("y_stride", C.c_size_t), ("mod_stride", C.c_size_t), ("h_out_stride", C.c_size_t),
+                ("out_stride", C.c_size_t)]
 
 
 class OrchConfig(C.Structure):
@@ -119,6 +139,12 @@ def _load():
                                             vp, sz, i, vp]),
         "orch_attention_quantized_workspace_bytes": (sz, [i, i, i, i, i, i]),
         "orch_attention_quantized_plan": (i, [i, i, i, i, i, i, sz] + [C.POINTER(i)] * 3),
+        "orch_op_block_norms": (i, [C.POINTER(BlockNorms), i, vp]),
+        "orch_op_quantize_rows": (i, [vp, sz, i, i, C.POINTER(Int8Rows), i, vp]),
+        "orch_op_linear_quantized": (i, [C.POINTER(Int8Rows), i, i, C.POINTER(Int8Rows), i, vp, i, vp, sz, i, vp, vp, sz, i, vp]),
+        "orch_linear_quantized_workspace_bytes": (sz, [i, i, i]),
+        "orch_op_qkv_projection_quantized": (i, [C.POINTER(Int8Rows), i, i, i, C.POINTER(Int8Rows), vp, i, i, vp, vp, sz, i, i,
+                                            vp, sz, i, vp]),
         "orch_sample_patch_parallel": (i, [vp, vp, i, C.POINTER(i), C.POINTER(i), C.POINTER(i), i, i,
                                            C.POINTER(i), f, vp, vp, vp]),
     }
@@ -462,6 +488,168 @@ def attention_quantized(q, cache: QuantizedKV, kv_fresh, fresh_bs, fresh_begin, 
     check(lib.orch_op_attention_quantized(_ptr(q), C.byref(cache), _ptr(kv_fresh), fresh_bs, fresh_begin,
                                           n_fresh, B, heads, n_q, head_dim, _ptr(out), _ptr(workspace),
                                           ws_bytes, dtype, st))
+
+
+def int8_rows(values, scales) -> Int8Rows:
+    """int8 rows with a scale each, held by two tensors: int8 values [rows, cols], their columns next to
+    each other and rows a multiple of 16 bytes apart, and fp32 scales [rows].  It keeps the tensors."""
+    import torch
+    rows, cols = values.shape
+    if values.dtype != torch.int8 or scales.dtype != torch.float32:
+        raise OrchError(ORCH_EINVAL, "values must be int8, scales fp32")
+    if tuple(scales.shape) != (rows,) or not scales.is_contiguous():
+        raise OrchError(ORCH_EINVAL, f"scales [{rows}] are needed, next to each other")
+    if cols > 1 and values.stride(1) != 1:
+        raise OrchError(ORCH_EINVAL, "a row's values must be next to each other")
+    r = Int8Rows(values.data_ptr(), scales.data_ptr(), values.stride(0))
+    r.tensors, r.devices, r.shape = (values, scales), (values.get_device(), scales.get_device()), (rows, cols)
+    return r
+
+
+def norm(kind, eps=1e-6, weight=None, bias=None) -> Norm:
+    """A norm ("none", "layer" or "rms") of block_norms, see orch_norm.  It keeps its fp32 [hidden] tensors."""
+    import torch
+    for t in (weight, bias):
+        if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or not t.is_contiguous()):
+            raise OrchError(ORCH_EINVAL, "weight and bias must be fp32 [hidden], next to each other")
+    if kind not in NORM_CODE:
+        raise OrchError(ORCH_EINVAL, f"norm {kind!r}: one of {', '.join(NORM_CODE)} is needed")
+    n = Norm(NORM_CODE[kind], eps, _ptr(weight), _ptr(bias))
+    n.tensors = tuple(t for t in (weight, bias) if t is not None)
+    n.devices = tuple(t.get_device() for t in n.tensors)
+    return n
+
+
+_NO_NORM = Norm(0, 0.0, None, None)
+_NO_NORM.tensors, _NO_NORM.devices = (), ()
+
+
+def block_norms(h, y=None, h_out=None, out=None, *, post=None, pre=None, gate=None, shift=None, scale=None,
+                rows_per_batch=0, residual_scale=1.0, stream=None):
+    """The pass between two blocks, see orch_block_norms: h, h_out fp32 and y, out T [rows, hidden] with
+    channels next to each other (out an Int8Rows: as codes), gate, shift and scale fp32 [branches, hidden]
+    with one row stride, norms from norm()."""
+    import torch
+    f32 = torch.float32
+    rows, hidden = h.shape
+    out8 = out if isinstance(out, Int8Rows) else None
+    if out8 is not None:
+        out = None
+        if out8.shape != (rows, hidden):
+            raise OrchError(ORCH_EINVAL, f"out holds {out8.shape} codes, the call writes {(rows, hidden)}")
+    typed = y if y is not None else out
+    code = ORCH_BF16 if typed is None else _code(typed)
+    p = BlockNorms()
+    devices = (h.get_device(),) + (out8.devices if out8 is not None else ())
+    for name, t, dt in (("h", h, f32), ("y", y, typed), ("h_out", h_out, f32), ("out", out, typed)):
+        if t is None:
+            continue
+        if t.dtype != (dt if dt is f32 else dt.dtype) or t.shape != h.shape or (hidden > 1 and t.stride(1) != 1):
+            raise OrchError(ORCH_EINVAL, f"{name} must be {list(h.shape)} of the call's type with channels next to each other")
+        devices += (t.get_device(),)
+        setattr(p, name, t.data_ptr())
+        setattr(p, name + "_stride", t.stride(0))
+    mod = [(n, t) for n, t in (("gate", gate), ("shift", shift), ("scale", scale)) if t is not None]
+    if mod:
+        _check_ints(rows_per_batch, 0)
+        need = -(-rows // max(1, rows_per_batch))
+        stride = mod[0][1].stride(0)
+        for name, t in mod:
+            if t.dtype != f32 or t.dim() != 2 or t.shape[0] < need or t.shape[1] != hidden or (hidden > 1 and t.stride(1) != 1):
+                raise OrchError(ORCH_EINVAL, f"{name} must be fp32 [{need}, {hidden}] with channels next to each other")
+            if need > 1 and t.stride(0) != stride:
+                raise OrchError(ORCH_EINVAL, "gate, shift and scale must have one row stride")
+            devices += (t.get_device(),)
+            setattr(p, name, t.data_ptr())
+        p.mod_stride, p.rows_per_batch = stride, rows_per_batch
+    for n in (post, pre):
+        if n is not None:
+            devices += n.devices
+            if any(t.shape[0] != hidden for t in n.tensors):
+                raise OrchError(ORCH_EINVAL, f"a norm's weight and bias must hold {hidden} channels")
+    p.post, p.pre = post or _NO_NORM, pre or _NO_NORM
+    p.residual_scale, p.rows, p.hidden = residual_scale, rows, hidden
+    if out8 is not None:
+        p.out8 = C.pointer(out8)
+    check(lib.orch_op_block_norms(C.byref(p), code, _stream_on(stream, *devices)))
+
+
+def quantize_rows(x, out: Int8Rows, stream=None):
+    """Rows of x [rows, cols] (channels next to each other) to int8 with a scale each, see orch_op_quantize_rows."""
+    rows, cols = x.shape
+    if out.shape != (rows, cols) or (cols > 1 and x.stride(1) != 1):
+        raise OrchError(ORCH_EINVAL, f"x must be {list(out.shape)}, as out, with channels next to each other")
+    code = _code(x)
+    check(lib.orch_op_quantize_rows(x.data_ptr(), x.stride(0), rows, cols, C.byref(out), code,
+                                    _stream_on(stream, x.get_device(), *out.devices)))
+
+
+def linear_quantized_workspace_bytes(M, N, K) -> int:
+    _check_ints(M, N, K)
+    return lib.orch_linear_quantized_workspace_bytes(M, N, K)
+
+
+def _int8_operands(A, W, bias, workspace):
+    """M, K, N, the workspace's bytes and the devices of a product."""
+    import torch
+    (M, K), (N, k) = A.shape, W.shape
+    if K != k:
+        raise OrchError(ORCH_EINVAL, f"A has {K} channels, W {k}")
+    devices = A.devices + W.devices
+    if bias is not None:
+        if bias.dtype != torch.float32 or tuple(bias.shape) != (N,) or not bias.is_contiguous():
+            raise OrchError(ORCH_EINVAL, f"bias must be fp32 [{N}]")
+        devices += (bias.get_device(),)
+    ws_bytes = 0
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise OrchError(ORCH_EINVAL, "workspace must be contiguous")
+        ws_bytes = workspace.nbytes
+        devices += (workspace.get_device(),)
+    return M, K, N, ws_bytes, devices
+
+
+def linear_quantized(A: Int8Rows, W: Int8Rows, bias, epilogue, out, gate=None, rows_per_batch=0, workspace=None, stream=None):
+    """A's rows times W's into out [M, N] (contiguous), see orch_op_linear_quantized; gate fp32 [branches, N]."""
+    import torch
+    M, K, N, ws_bytes, devices = _int8_operands(A, W, bias, workspace)
+    code = _code(out)
+    if tuple(out.shape) != (M, N) or not out.is_contiguous():
+        raise OrchError(ORCH_EINVAL, f"out must be [{M}, {N}], contiguous")
+    devices += (out.get_device(),)
+    gate_stride = 0
+    if epilogue == EPI_RESIDUAL:
+        _check_ints(rows_per_batch, 0)
+        if code != ORCH_F32:
+            raise OrchError(ORCH_EINVAL, "the residual epilogue adds to fp32")
+        need = -(-M // max(1, rows_per_batch))
+        if (gate is None or gate.dtype != torch.float32 or gate.dim() != 2 or gate.shape[0] < need or gate.shape[1] != N
+                or (N > 1 and gate.stride(1) != 1)):
+            raise OrchError(ORCH_EINVAL, f"the residual epilogue needs gate, fp32 [{need}, {N}]")
+        devices += (gate.get_device(),)
+        gate_stride = gate.stride(0)
+    check(lib.orch_op_linear_quantized(C.byref(A), M, K, C.byref(W), N, _ptr(bias), epilogue, _ptr(gate), gate_stride,
+                                  rows_per_batch, out.data_ptr(), _ptr(workspace), ws_bytes, code,
+                                  _stream_on(stream, *devices)))
+
+
+def qkv_projection_quantized(A: Int8Rows, W: Int8Rows, bias, q_out, kv_out, kv_tokens, tok_offset, workspace=None, stream=None):
+    """Q [B, heads, n_tok, d] and the band's K and V of the K/V buffer kv_out [B, elements], see
+    orch_op_qkv_projection_quantized."""
+    M, K, N, ws_bytes, devices = _int8_operands(A, W, bias, workspace)
+    B, heads, n_tok, d = q_out.shape
+    code = _code(q_out)
+    if B * n_tok != M or 3 * heads * d != N or not q_out.is_contiguous():
+        raise OrchError(ORCH_EINVAL, f"q_out must be [B, heads, n_tok, d], contiguous, of {M} tokens and {N} / 3 channels")
+    if kv_out.dim() != 2 or kv_out.shape[0] != B:
+        raise OrchError(ORCH_EINVAL, f"kv_out must be [{B}, elements]")
+    _check_ints(kv_tokens, tok_offset)
+    kv_bs = kv_out.stride(0)
+    _check_kv("kv_out", kv_out, code, kv_bs, kv_tokens, B, heads, d)
+    devices += (q_out.get_device(), kv_out.get_device())
+    check(lib.orch_op_qkv_projection_quantized(C.byref(A), B, n_tok, K, C.byref(W), _ptr(bias), heads, d, q_out.data_ptr(),
+                                          kv_out.data_ptr(), kv_bs, kv_tokens, tok_offset, _ptr(workspace), ws_bytes, code,
+                                          _stream_on(stream, *devices)))
 
 
 def unet_shape(cfg, eps: float = 1e-5) -> UNetConvShape:

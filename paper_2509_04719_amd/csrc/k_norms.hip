@@ -1,0 +1,386 @@
+// The pass between two blocks (norm after a block, gate, residual scale, norm
+// before the next one, its modulation, optionally to 8-bit codes), and rows to
+// 8-bit codes with a scale each.
+//
+//   h' = a h + g post(y),   u = pre(h') (1 + s) + t
+//
+// Bytes bound both: every element is read once and written once.  A row stays in
+// the registers of the LPR lanes that share it (a part of a wave, a wave, or a
+// workgroup), so the statistics are two-pass (mean, then squares about it) at no
+// cost in memory.
+#include "common.h"
+#include "kernels.h"
+
+namespace orch {
+namespace norms {
+
+constexpr int kThreads = 256;
+
+// v of the lane that DPP control word C names
+template <int C>
+__device__ __forceinline__ unsigned dpp(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, C, 0xf, 0xf, true);
+}
+
+struct Sum {
+  __device__ __forceinline__ unsigned operator()(unsigned a, unsigned b) const {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }
+};
+struct Max {
+  __device__ __forceinline__ unsigned operator()(unsigned a, unsigned b) const { return max(a, b); }
+};
+
+// f over the LPR lanes that share a row, the same bits in each: neighbours, quads,
+// halves of 16 by DPP, rows of 16 by permlane swaps, waves by LDS
+template <int LPR>
+struct Group {
+  static constexpr int NW = LPR > 64 ? LPR / 64 : 1;
+  unsigned* lds;       // [2][NW], LPR > 64
+  int turn = 0;
+
+  template <typename F>
+  __device__ __forceinline__ unsigned all(unsigned v, F f) {
+    v = f(v, dpp<0xB1>(v));    // lane ^ 1
+    v = f(v, dpp<0x4E>(v));    // lane ^ 2
+    v = f(v, dpp<0x141>(v));   // 7 - lane of 8
+    v = f(v, dpp<0x140>(v));   // 15 - lane of 16
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(r[0], r[1]);
+    if constexpr (LPR > 32) {
+      const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+      v = f(s[0], s[1]);
+    }
+#endif
+    if constexpr (NW > 1) {
+      // (two sets of slots: one is read while the next reduction fills the other)
+      unsigned* slot = lds + turn * NW;
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = slot[0];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) v = f(v, slot[w]);
+    }
+    return v;
+  }
+  __device__ __forceinline__ float sum(float v) { return __uint_as_float(all(__float_as_uint(v), Sum{})); }
+  __device__ __forceinline__ unsigned top(unsigned v) { return all(v, Max{}); }
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void load(float* o, const T* p) {
+  typedef T W __attribute__((ext_vector_type(V)));
+  if constexpr (V == 1) {
+    o[0] = to_f<T>(*p);
+  } else {
+    const W w = *reinterpret_cast<const W*>(p);
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = to_f<T>(w[e]);
+  }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store(T* p, const float* x) {
+  typedef T W __attribute__((ext_vector_type(V)));
+  if constexpr (V == 1) {
+    *p = from_f<T>(x[0]);
+  } else {
+    W w;
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[e] = from_f<T>(x[e]);
+    *reinterpret_cast<W*>(p) = w;
+  }
+}
+
+// A row's codes: q = x * (127 / top) to nearest, ties to even, quotient and product
+// rounded to 32 bits; scale top / 127.  `bits`: the largest magnitude's.  Below 2^-64
+// the quotient is taken of 2^64 x, which is exact, so that it stays finite.
+// An infinity or NaN anywhere: codes 0 and scale NaN, so every product of the row is NaN.
+struct Codes {
+  float up, r, scale;
+  __device__ __forceinline__ explicit Codes(unsigned bits) {
+    const float top = __uint_as_float(bits);
+    up = bits < 0x1F800000u ? 0x1p64f : 1.0f;
+    r = bits == 0u || bits >= 0x7F800000u ? 0.0f : 127.0f / (top * up);
+    scale = bits >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : top / 127.0f;
+    finite = bits < 0x7F800000u;
+  }
+  bool finite;
+  __device__ __forceinline__ int code(float x) const { return finite ? (int)rintf((x * up) * r) : 0; }
+  template <int V>
+  __device__ __forceinline__ void put(signed char* p, const float* x) const {
+    if constexpr (V == 1) {
+      *p = (signed char)code(x[0]);
+    } else {
+      unsigned w[V / 4];
+#pragma unroll
+      for (int i = 0; i < V / 4; ++i)
+        w[i] = (code(x[4 * i]) & 0xff) | (code(x[4 * i + 1]) & 0xff) << 8 | (code(x[4 * i + 2]) & 0xff) << 16 |
+               (unsigned)code(x[4 * i + 3]) << 24;
+      if constexpr (V == 4) *reinterpret_cast<unsigned*>(p) = w[0];
+      else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    }
+  }
+};
+
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// x of a row -> its norm times weight plus bias (32 bits; elements past the row are 0
+// and stay out of the sums)
+template <int V, int NV, int LPR>
+__device__ __forceinline__ void norm(float (&x)[NV][V], int lane, int H, const Norm& n, Group<LPR>& g) {
+  if (n.kind != kNormNone) {
+    const float inv = 1.0f / (float)H;
+    if (n.kind == kNormLayer) {
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += x[i][e];
+      const float mean = g.sum(s) * inv;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const bool in = (lane + LPR * i) * V < H;
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] = in ? x[i][e] - mean : 0.0f;
+      }
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s = fmaf(x[i][e], x[i][e], s);
+    const float rstd = 1.0f / sqrtf(g.sum(s) * inv + n.eps);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[i][e] *= rstd;
+  }
+  if (n.weight || n.bias) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + LPR * i) * V;
+      if (c < H) {
+        float w[V], b[V];
+        if (n.weight) {
+          load<float, V>(w, n.weight + c);
+#pragma unroll
+          for (int e = 0; e < V; ++e) x[i][e] *= w[e];
+        }
+        if (n.bias) {
+          load<float, V>(b, n.bias + c);
+#pragma unroll
+          for (int e = 0; e < V; ++e) x[i][e] += b[e];
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int V, int LPR, int NV>
+__global__ __launch_bounds__(LPR > kThreads ? LPR : kThreads) void block_norms_kernel(BlockNormsParams p) {
+  constexpr int RPB = LPR > kThreads ? 1 : kThreads / LPR;    // rows of a workgroup
+  __shared__ unsigned red[LPR > 64 ? 2 * LPR / 64 : 1];
+  const int lane = threadIdx.x % LPR, H = p.hidden;
+  const int row = blockIdx.x * RPB + threadIdx.x / LPR;
+  if (row >= p.rows) return;    // (the whole group of lanes; a group of several waves is a whole workgroup)
+  Group<LPR> g{red};
+  const size_t b = row / p.rows_per_batch * p.mod_stride;
+  const float* hr = p.h + row * p.h_stride;
+  float x[NV][V];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (lane + LPR * i) * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[i][e] = 0.0f;
+    if (c < H) load<float, V>(x[i], hr + c);
+  }
+  if (p.y) {
+    const T* yr = reinterpret_cast<const T*>(p.y) + row * p.y_stride;
+    float y[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + LPR * i) * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[i][e] = 0.0f;
+      if (c < H) load<T, V>(y[i], yr + c);
+    }
+    norm<V, NV, LPR>(y, lane, H, p.post, g);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + LPR * i) * V;
+      if (c < H) {
+        float w[V];
+        if (p.gate) load<float, V>(w, p.gate + b + c);
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] = fmaf(p.residual_scale, x[i][e], p.gate ? w[e] * y[i][e] : y[i][e]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[i][e] *= p.residual_scale;
+  }
+  if (p.h_out) {
+    float* o = p.h_out + row * p.h_out_stride;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + LPR * i) * V;
+      if (c < H) store<float, V>(o + c, x[i]);
+    }
+  }
+  if (!p.out && !p.codes) return;
+  norm<V, NV, LPR>(x, lane, H, p.pre, g);
+  unsigned top = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (lane + LPR * i) * V;
+    if (c < H) {
+      float w[V];
+      if (p.scale) {
+        load<float, V>(w, p.scale + b + c);
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] *= 1.0f + w[e];
+      }
+      if (p.shift) {
+        load<float, V>(w, p.shift + b + c);
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] += w[e];
+      }
+      if (p.out) store<T, V>(reinterpret_cast<T*>(p.out) + row * p.out_stride + c, x[i]);
+#pragma unroll
+      for (int e = 0; e < V; ++e) top = max(top, magnitude(x[i][e]));
+    }
+  }
+  if (!p.codes) return;
+  const Codes q(g.top(top));
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (lane + LPR * i) * V;
+    if (c < H) q.put<V>(p.codes + row * p.codes_stride + c, x[i]);
+  }
+  if (lane == 0) p.code_scales[row] = q.scale;
+}
+
+// Rows to codes.  NV 0: rows too long for the registers, read twice.
+template <typename T, int V, int LPR, int NV>
+__global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const T* __restrict__ x, size_t x_stride, int rows, int cols,
+                                                                 signed char* __restrict__ codes, size_t codes_stride,
+                                                                 float* __restrict__ scales) {
+  __shared__ unsigned red[LPR > 64 ? 2 * LPR / 64 : 1];
+  const int lane = threadIdx.x % LPR;
+  const int row = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
+  if (row >= rows) return;
+  Group<LPR> g{red};
+  const T* xr = x + row * x_stride;
+  signed char* cr = codes + row * codes_stride;
+  unsigned top = 0;
+  if constexpr (NV > 0) {
+    float v[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + LPR * i) * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
+      if (c < cols) load<T, V>(v[i], xr + c);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) top = max(top, magnitude(v[i][e]));
+    const Codes q(g.top(top));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + LPR * i) * V;
+      if (c < cols) q.put<V>(cr + c, v[i]);
+    }
+    if (lane == 0) scales[row] = q.scale;
+  } else {
+    for (int c = lane * V; c < cols; c += LPR * V) {
+      float v[V];
+      load<T, V>(v, xr + c);
+#pragma unroll
+      for (int e = 0; e < V; ++e) top = max(top, magnitude(v[e]));
+    }
+    const Codes q(g.top(top));
+    for (int c = lane * V; c < cols; c += LPR * V) {
+      float v[V];
+      load<T, V>(v, xr + c);
+      q.put<V>(cr + c, v);
+    }
+    if (lane == 0) scales[row] = q.scale;
+  }
+}
+
+static bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
+
+template <typename T, int V, int LPR, int NV>
+static void launch_norms(const BlockNormsParams& p, hipStream_t s) {
+  constexpr int threads = LPR > kThreads ? LPR : kThreads;
+  hipLaunchKernelGGL((block_norms_kernel<T, V, LPR, NV>), dim3(ceil_div(p.rows, threads / LPR)), dim3(threads), 0, s, p);
+}
+
+// Four channels an access where every row allows it, else one.
+template <typename T>
+static void launch_norms_t(const BlockNormsParams& p, hipStream_t s) {
+  const int H = p.hidden;
+  bool four = H % 4 == 0 && p.mod_stride % 4 == 0;
+  for (const void* q : {(const void*)p.gate, (const void*)p.shift, (const void*)p.scale, (const void*)p.post.weight,
+                        (const void*)p.post.bias, (const void*)p.pre.weight, (const void*)p.pre.bias,
+                        (const void*)p.h, (const void*)p.h_out})
+    four = four && aligned(q, 16);
+  four = four && aligned(p.y, 4 * sizeof(T)) && aligned(p.out, 4 * sizeof(T)) && p.h_stride % 4 == 0 &&
+         p.h_out_stride % 4 == 0 && p.y_stride % 4 == 0 && p.out_stride % 4 == 0;
+  if (four) {
+    if (H <= 32 * 4 * 3) launch_norms<T, 4, 32, 3>(p, s);
+    else if (H <= 32 * 4 * 9) launch_norms<T, 4, 32, 9>(p, s);
+    else if (H <= 64 * 4 * 9) launch_norms<T, 4, 64, 9>(p, s);
+    else if (H <= 256 * 4 * 9) launch_norms<T, 4, 256, 9>(p, s);
+    else launch_norms<T, 4, 1024, 9>(p, s);
+  } else {
+    if (H <= 64 * 8) launch_norms<T, 1, 64, 8>(p, s);
+    else if (H <= 64 * 36) launch_norms<T, 1, 64, 36>(p, s);
+    else if (H <= 256 * 36) launch_norms<T, 1, 256, 36>(p, s);
+    else launch_norms<T, 1, 1024, 36>(p, s);
+  }
+}
+
+template <typename T, int V, int LPR, int NV>
+static void launch_quant(const QuantizeRowsParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((quantize_rows_kernel<T, V, LPR, NV>), dim3(ceil_div(p.rows, kThreads / LPR)), dim3(kThreads), 0, s,
+                     reinterpret_cast<const T*>(p.x), p.x_stride, p.rows, p.cols, p.codes, p.codes_stride, p.scales);
+}
+
+template <typename T>
+static void launch_quant_t(const QuantizeRowsParams& p, hipStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  if (p.cols % V == 0 && aligned(p.x, 16) && p.x_stride % V == 0) {
+    if (p.cols <= 32 * V * 5) launch_quant<T, V, 32, 5>(p, s);
+    else if (p.cols <= 64 * V * 9) launch_quant<T, V, 64, 9>(p, s);
+    else if (p.cols <= 256 * V * 9) launch_quant<T, V, 256, 9>(p, s);
+    else launch_quant<T, V, 256, 0>(p, s);
+  } else {
+    if (p.cols <= 64 * 16) launch_quant<T, 1, 64, 16>(p, s);
+    else launch_quant<T, 1, 256, 0>(p, s);
+  }
+}
+
+}  // namespace norms
+
+hipError_t launch_block_norms(const BlockNormsParams& p, int dtype, hipStream_t s) {
+  if (p.rows <= 0) return hipSuccess;
+  if (dtype == kBF16) norms::launch_norms_t<bf16>(p, s);
+  else norms::launch_norms_t<float>(p, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_quantize_rows(const QuantizeRowsParams& p, int dtype, hipStream_t s) {
+  if (p.rows <= 0) return hipSuccess;
+  if (dtype == kBF16) norms::launch_quant_t<bf16>(p, s);
+  else norms::launch_quant_t<float>(p, s);
+  return hipGetLastError();
+}
+
+}  // namespace orch

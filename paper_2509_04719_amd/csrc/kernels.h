@@ -225,4 +225,61 @@ bool attention_quantized_plan(int B, int heads, int n_q, int n_kv, int d, int dt
                               int* query_groups, int* key_parts);
 hipError_t launch_attention_quantized(const AttnQParams& p, int dtype, hipStream_t stream);
 
+// The pass between two blocks (k_norms.hip).
+enum NormKind { kNormNone = 0, kNormLayer = 1, kNormRms = 2 };
+struct Norm {
+  int kind;
+  float eps;
+  const float* weight;        // [hidden], or null: 1
+  const float* bias;          // [hidden], or null: 0
+};
+struct BlockNormsParams {
+  const float* h;
+  const void* y;              // T, or null: no block has ended
+  float* h_out;               // or null
+  void* out;                  // T; or null
+  signed char* codes;         // with code_scales; or null
+  float* code_scales;
+  const float *gate, *shift, *scale;   // row b of [B][mod_stride], or null: 1, 0, 0
+  size_t h_stride, y_stride, h_out_stride, out_stride, codes_stride, mod_stride;   // elements
+  Norm post, pre;
+  float residual_scale;
+  int rows, hidden, rows_per_batch;
+};
+hipError_t launch_block_norms(const BlockNormsParams& p, int dtype, hipStream_t stream);
+
+struct QuantizeRowsParams {
+  const void* x;              // T
+  size_t x_stride;            // elements
+  signed char* codes;
+  size_t codes_stride;
+  float* scales;
+  int rows, cols;
+};
+hipError_t launch_quantize_rows(const QuantizeRowsParams& p, int dtype, hipStream_t stream);
+
+// 8-bit integer products (k_gemm_int8.hip): int8 rows [M][K] of A and [N][K] of W,
+// row strides in bytes, multiples of 16.
+struct GemmI8Params {
+  const signed char *A, *W;
+  size_t lda, ldw;
+  const float *sa, *sw;       // scales of A's and W's rows
+  int M, N, K;
+  const float* bias;          // [N], or null: 0
+  void* out;                  // STORE / GELU: T [M][N]; RESIDUAL: fp32 [M][N]
+  const float* gate;          // RESIDUAL: fp32 [B][gate_stride]
+  size_t gate_stride;
+  int rows_per_batch;
+  void *q, *kv;               // QKV: as EpiParams
+  size_t kv_bs;
+  int kv_tokens, tok_offset, heads, hidden, head_dim;
+  unsigned hd_magic;          // set by the launcher: ceil(2^32 / head_dim)
+  int wide;                   // set by the launcher: rows of out take 16-byte accesses
+  int* ws;                    // optional: sums of k-splits, int32 [splits][M][N]
+  size_t ws_elems;
+  int splits;                 // set by the launcher
+};
+size_t gemm_int8_workspace_bytes(int M, int N, int K);
+hipError_t launch_gemm_int8(const GemmI8Params& p, int epi, int dtype, hipStream_t stream);
+
 }  // namespace orch
