@@ -139,7 +139,7 @@ def _load():
                                             vp, sz, i, vp]),
         "orch_attention_quantized_workspace_bytes": (sz, [i, i, i, i, i, i]),
         "orch_attention_quantized_plan": (i, [i, i, i, i, i, i, sz] + [C.POINTER(i)] * 3),
-        "orch_op_block_norms": (i, [C.POINTER(BlockNorms), i, vp]),
+        "orch_op_block_norms": (i, [vp, i, vp]),
         "orch_op_quantize_rows": (i, [vp, sz, i, i, C.POINTER(Int8Rows), i, vp]),
         "orch_op_linear_quantized": (i, [C.POINTER(Int8Rows), i, i, C.POINTER(Int8Rows), i, vp, i, vp, sz, i, vp, vp, sz, i, vp]),
         "orch_linear_quantized_workspace_bytes": (sz, [i, i, i]),
@@ -503,6 +503,7 @@ def int8_rows(values, scales) -> Int8Rows:
         raise OrchError(ORCH_EINVAL, "a row's values must be next to each other")
     r = Int8Rows(values.data_ptr(), scales.data_ptr(), values.stride(0))
     r.tensors, r.devices, r.shape = (values, scales), (values.get_device(), scales.get_device()), (rows, cols)
+    r.ref, r.address = C.byref(r), C.addressof(r)
     return r
 
 
@@ -516,12 +517,14 @@ def norm(kind, eps=1e-6, weight=None, bias=None) -> Norm:
         raise OrchError(ORCH_EINVAL, f"norm {kind!r}: one of {', '.join(NORM_CODE)} is needed")
     n = Norm(NORM_CODE[kind], eps, _ptr(weight), _ptr(bias))
     n.tensors = tuple(t for t in (weight, bias) if t is not None)
-    n.devices = tuple(t.get_device() for t in n.tensors)
+    n.devices, n.channels = tuple(t.get_device() for t in n.tensors), {t.shape[0] for t in n.tensors}
+    n.packed = bytes(n)
     return n
 
 
 _NO_NORM = Norm(0, 0.0, None, None)
-_NO_NORM.tensors, _NO_NORM.devices = (), ()
+_NO_NORM.devices, _NO_NORM.channels, _NO_NORM.packed = (), set(), bytes(_NO_NORM)
+_BLOCK_NORMS = struct.Struct("=24s24sf3i13Q")   # orch_block_norms' layout
 
 
 def block_norms(h, y=None, h_out=None, out=None, *, post=None, pre=None, gate=None, shift=None, scale=None,
@@ -529,49 +532,47 @@ def block_norms(h, y=None, h_out=None, out=None, *, post=None, pre=None, gate=No
     """The pass between two blocks, see orch_block_norms: h, h_out fp32 and y, out T [rows, hidden] with
     channels next to each other (out an Int8Rows: as codes), gate, shift and scale fp32 [branches, hidden]
     with one row stride, norms from norm()."""
-    import torch
-    f32 = torch.float32
-    rows, hidden = h.shape
-    out8 = out if isinstance(out, Int8Rows) else None
-    if out8 is not None:
-        out = None
-        if out8.shape != (rows, hidden):
-            raise OrchError(ORCH_EINVAL, f"out holds {out8.shape} codes, the call writes {(rows, hidden)}")
-    typed = y if y is not None else out
-    code = ORCH_BF16 if typed is None else _code(typed)
-    p = BlockNorms()
-    devices = (h.get_device(),) + (out8.devices if out8 is not None else ())
-    for name, t, dt in (("h", h, f32), ("y", y, typed), ("h_out", h_out, f32), ("out", out, typed)):
+    shape = h.shape
+    rows, hidden = shape
+    post, pre = post or _NO_NORM, pre or _NO_NORM
+    devices = (h.get_device(),) + post.devices + pre.devices
+    out8 = 0
+    if isinstance(out, Int8Rows):
+        if out.shape != (rows, hidden):
+            raise OrchError(ORCH_EINVAL, f"out holds {out.shape} codes, the call writes {(rows, hidden)}")
+        devices += out.devices
+        out8, out = out.address, None
+    code = ORCH_BF16 if y is None and out is None else _code(out if y is None else y)
+    ptrs, strides = [], []
+    for t, c in ((h, ORCH_F32), (y, code), (h_out, ORCH_F32), (out, code)):
         if t is None:
+            ptrs.append(0)
+            strides.append(0)
             continue
-        if t.dtype != (dt if dt is f32 else dt.dtype) or t.shape != h.shape or (hidden > 1 and t.stride(1) != 1):
-            raise OrchError(ORCH_EINVAL, f"{name} must be {list(h.shape)} of the call's type with channels next to each other")
+        s = t.stride()
+        if t.shape != shape or _code(t) != c or (s[1] != 1 and hidden > 1):
+            raise OrchError(ORCH_EINVAL, f"h, y, h_out and out must be {list(shape)} of fp32 or the call's type, channels next to each other")
         devices += (t.get_device(),)
-        setattr(p, name, t.data_ptr())
-        setattr(p, name + "_stride", t.stride(0))
-    mod = [(n, t) for n, t in (("gate", gate), ("shift", shift), ("scale", scale)) if t is not None]
-    if mod:
-        _check_ints(rows_per_batch, 0)
-        need = -(-rows // max(1, rows_per_batch))
-        stride = mod[0][1].stride(0)
-        for name, t in mod:
-            if t.dtype != f32 or t.dim() != 2 or t.shape[0] < need or t.shape[1] != hidden or (hidden > 1 and t.stride(1) != 1):
-                raise OrchError(ORCH_EINVAL, f"{name} must be fp32 [{need}, {hidden}] with channels next to each other")
-            if need > 1 and t.stride(0) != stride:
-                raise OrchError(ORCH_EINVAL, "gate, shift and scale must have one row stride")
-            devices += (t.get_device(),)
-            setattr(p, name, t.data_ptr())
-        p.mod_stride, p.rows_per_batch = stride, rows_per_batch
-    for n in (post, pre):
-        if n is not None:
-            devices += n.devices
-            if any(t.shape[0] != hidden for t in n.tensors):
-                raise OrchError(ORCH_EINVAL, f"a norm's weight and bias must hold {hidden} channels")
-    p.post, p.pre = post or _NO_NORM, pre or _NO_NORM
-    p.residual_scale, p.rows, p.hidden = residual_scale, rows, hidden
-    if out8 is not None:
-        p.out8 = C.pointer(out8)
-    check(lib.orch_op_block_norms(C.byref(p), code, _stream_on(stream, *devices)))
+        ptrs.append(t.data_ptr())
+        strides.append(s[0])
+    mods, mod_stride = [], None
+    for t in (gate, shift, scale):
+        if t is None:
+            mods.append(0)
+            continue
+        s, (branches, channels) = t.stride(), t.shape
+        if mod_stride is None:
+            mod_stride, need = s[0], -(-rows // rows_per_batch) if rows_per_batch > 0 else 0
+        if branches < need or channels != hidden or _code(t) != ORCH_F32 or (s[1] != 1 and hidden > 1) or (s[0] != mod_stride and need > 1):
+            raise OrchError(ORCH_EINVAL, f"gate, shift and scale must be fp32 [{need}, {hidden}] of one row stride, channels next to each other")
+        devices += (t.get_device(),)
+        mods.append(t.data_ptr())
+    if not (post.channels | pre.channels) <= {hidden}:
+        raise OrchError(ORCH_EINVAL, f"a norm's weight and bias must hold {hidden} channels")
+    _check_ints(rows_per_batch, 0)
+    p = _BLOCK_NORMS.pack(post.packed, pre.packed, residual_scale, rows, hidden, rows_per_batch, ptrs[0], ptrs[1], *mods,
+                          ptrs[2], ptrs[3], out8, strides[0], strides[1], mod_stride or 0, strides[2], strides[3])
+    check(lib.orch_op_block_norms(p, code, _stream_on(stream, *devices)))
 
 
 def quantize_rows(x, out: Int8Rows, stream=None):
@@ -580,7 +581,7 @@ def quantize_rows(x, out: Int8Rows, stream=None):
     if out.shape != (rows, cols) or (cols > 1 and x.stride(1) != 1):
         raise OrchError(ORCH_EINVAL, f"x must be {list(out.shape)}, as out, with channels next to each other")
     code = _code(x)
-    check(lib.orch_op_quantize_rows(x.data_ptr(), x.stride(0), rows, cols, C.byref(out), code,
+    check(lib.orch_op_quantize_rows(x.data_ptr(), x.stride(0), rows, cols, out.ref, code,
                                     _stream_on(stream, x.get_device(), *out.devices)))
 
 
@@ -591,13 +592,12 @@ def linear_quantized_workspace_bytes(M, N, K) -> int:
 
 def _int8_operands(A, W, bias, workspace):
     """M, K, N, the workspace's bytes and the devices of a product."""
-    import torch
     (M, K), (N, k) = A.shape, W.shape
     if K != k:
         raise OrchError(ORCH_EINVAL, f"A has {K} channels, W {k}")
     devices = A.devices + W.devices
     if bias is not None:
-        if bias.dtype != torch.float32 or tuple(bias.shape) != (N,) or not bias.is_contiguous():
+        if _code(bias) != ORCH_F32 or bias.shape != (N,) or not bias.is_contiguous():
             raise OrchError(ORCH_EINVAL, f"bias must be fp32 [{N}]")
         devices += (bias.get_device(),)
     ws_bytes = 0
@@ -611,10 +611,9 @@ def _int8_operands(A, W, bias, workspace):
 
 def linear_quantized(A: Int8Rows, W: Int8Rows, bias, epilogue, out, gate=None, rows_per_batch=0, workspace=None, stream=None):
     """A's rows times W's into out [M, N] (contiguous), see orch_op_linear_quantized; gate fp32 [branches, N]."""
-    import torch
     M, K, N, ws_bytes, devices = _int8_operands(A, W, bias, workspace)
     code = _code(out)
-    if tuple(out.shape) != (M, N) or not out.is_contiguous():
+    if out.shape != (M, N) or not out.is_contiguous():
         raise OrchError(ORCH_EINVAL, f"out must be [{M}, {N}], contiguous")
     devices += (out.get_device(),)
     gate_stride = 0
@@ -623,12 +622,12 @@ def linear_quantized(A: Int8Rows, W: Int8Rows, bias, epilogue, out, gate=None, r
         if code != ORCH_F32:
             raise OrchError(ORCH_EINVAL, "the residual epilogue adds to fp32")
         need = -(-M // max(1, rows_per_batch))
-        if (gate is None or gate.dtype != torch.float32 or gate.dim() != 2 or gate.shape[0] < need or gate.shape[1] != N
+        if (gate is None or _code(gate) != ORCH_F32 or gate.dim() != 2 or gate.shape[0] < need or gate.shape[1] != N
                 or (N > 1 and gate.stride(1) != 1)):
             raise OrchError(ORCH_EINVAL, f"the residual epilogue needs gate, fp32 [{need}, {N}]")
         devices += (gate.get_device(),)
         gate_stride = gate.stride(0)
-    check(lib.orch_op_linear_quantized(C.byref(A), M, K, C.byref(W), N, _ptr(bias), epilogue, _ptr(gate), gate_stride,
+    check(lib.orch_op_linear_quantized(A.ref, M, K, W.ref, N, _ptr(bias), epilogue, _ptr(gate), gate_stride,
                                   rows_per_batch, out.data_ptr(), _ptr(workspace), ws_bytes, code,
                                   _stream_on(stream, *devices)))
 
@@ -647,7 +646,7 @@ def qkv_projection_quantized(A: Int8Rows, W: Int8Rows, bias, q_out, kv_out, kv_t
     kv_bs = kv_out.stride(0)
     _check_kv("kv_out", kv_out, code, kv_bs, kv_tokens, B, heads, d)
     devices += (q_out.get_device(), kv_out.get_device())
-    check(lib.orch_op_qkv_projection_quantized(C.byref(A), B, n_tok, K, C.byref(W), _ptr(bias), heads, d, q_out.data_ptr(),
+    check(lib.orch_op_qkv_projection_quantized(A.ref, B, n_tok, K, W.ref, _ptr(bias), heads, d, q_out.data_ptr(),
                                           kv_out.data_ptr(), kv_bs, kv_tokens, tok_offset, _ptr(workspace), ws_bytes, code,
                                           _stream_on(stream, *devices)))
 

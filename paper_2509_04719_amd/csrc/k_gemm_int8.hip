@@ -266,25 +266,33 @@ struct Strip {
   }
 };
 
+// Columns of a strip of a wave that holds FN blocks of 32
+constexpr int strip_cols(int FN) { return FN % 2 ? 32 : 64; }
+constexpr int strip_bytes(int FN) { return 32 * (strip_cols(FN) + 4) * 4; }
+
 // A wave's sums, FM x FN blocks of 32 x 32 from (m0 + mw, n0 + nw) of the tile at (m0,
 // n0); the MFMAs make transposed blocks: a lane holds row lane % 32, columns 8 g + 4
 // (lane / 32) + 0 .. 3.
 template <typename T, int EPI, int FM, int FN, int BM, int BN>
 __device__ __forceinline__ void epilogue(const GemmI8Params& p, const i32x16 (&acc)[FM][FN], char* lds, const Side<BM, BN>& side,
                                          int lane, int m0, int n0, int mw, int nw, int split) {
-  using S = Strip<T, 32 * FN, EPI>;
+  constexpr int SN = strip_cols(FN), SB = SN / 32;
+  using S = Strip<T, SN, EPI>;
   int* strip = reinterpret_cast<int*>(lds);
   const int lr = lane & 31, h = lane >> 5;
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
+    for (int jb = 0; jb < FN; jb += SB) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<i32x4*>(strip + lr * S::LS + j * 32 + 8 * g + 4 * h) =
-            i32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-    S{p, strip, side.sa + mw + 32 * i, side.sw + nw, side.bias + nw, lane, m0 + mw + 32 * i, n0 + nw, split}.rows();
-  }
+      for (int j = 0; j < SB; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<i32x4*>(strip + lr * S::LS + j * 32 + 8 * g + 4 * h) =
+              i32x4{acc[i][jb + j][4 * g], acc[i][jb + j][4 * g + 1], acc[i][jb + j][4 * g + 2], acc[i][jb + j][4 * g + 3]};
+      const int mr = mw + 32 * i, nc = nw + 32 * jb;
+      S{p, strip, side.sa + mr, side.sw + nc, side.bias + nc, lane, m0 + mr, n0 + nc, split}.rows();
+    }
 }
 
 // Which tile a workgroup takes: workgroup b is in split b / T of T = tiles_m x
@@ -343,7 +351,7 @@ struct Geo {
   static constexpr int STAGE = (BM + BN) * BK;
   static constexpr int KK = BK / 32;                // MFMA k-steps per k-tile
   static constexpr int LPK = S == 2 ? LPT : (LPT + KK - 1) / KK;
-  static constexpr int STRIPS = NW * 32 * (TN + 4) * 4;
+  static constexpr int STRIPS = NW * strip_bytes(FN);
   static constexpr int RING = S * STAGE > STRIPS ? S * STAGE : STRIPS;   // the strips take the ring's place
   static constexpr int LDS = RING + (int)sizeof(Side<BM, BN>);
   static_assert(BK == 64 || BK == 128, "k-tile");
@@ -470,7 +478,7 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
   compute(kt % S, No{}, Yes{}, 0, 0);
 
   __syncthreads();
-  epilogue<T, EPI>(p, acc, smem + wave * (32 * (G::TN + 4) * 4), side, lane, m0, n0, wm * G::TM, wn * G::TN, at.split);
+  epilogue<T, EPI>(p, acc, smem + wave * strip_bytes(FN), side, lane, m0, n0, wm * G::TM, wn * G::TN, at.split);
 #endif
 }
 
@@ -486,7 +494,7 @@ struct SmallGeo {
   static constexpr int RING = KG * S * STAGE;
   static constexpr int LDS = RING + (int)sizeof(Side<BM, BN>);
   static constexpr int SUMS = (KG - 1) * NWG * 4096;
-  static constexpr int STRIP = 32 * 36 * 4;
+  static constexpr int STRIP = strip_bytes(1);
   static_assert((BM / 32) * (BN / 32) == NWG, "a 32 x 32 block per wave");
   static_assert((BM + BN) / 8 % NWG == 0 && (S - 1) * LPT < 60, "whole loads");
   static_assert(SUMS + NWG * STRIP <= RING && LDS <= 160 * 1024, "LDS");

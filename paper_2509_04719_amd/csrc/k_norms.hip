@@ -69,17 +69,43 @@ struct Group {
   __device__ __forceinline__ unsigned top(unsigned v) { return all(v, Max{}); }
 };
 
+// V elements as they are held, and as fp32
 template <typename T, int V>
-__device__ __forceinline__ void load(float* o, const T* p) {
+struct Raw {
   typedef T W __attribute__((ext_vector_type(V)));
-  if constexpr (V == 1) {
-    o[0] = to_f<T>(*p);
-  } else {
-    const W w = *reinterpret_cast<const W*>(p);
+  W w;
+  __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const W*>(p); }
+  __device__ __forceinline__ float operator[](int e) const { return to_f<T>(w[e]); }
+};
+template <typename T>
+struct Raw<T, 1> {
+  T w;
+  __device__ __forceinline__ void load(const T* p) { w = *p; }
+  __device__ __forceinline__ float operator[](int) const { return to_f<T>(w); }
+};
+
+// A lane's share of a row of n channels: V of them from (lane + LPR i) V on, i < NV.  Loads
+// past the row read its first channels instead (a branch each would wait for each).
+template <int V, int NV, int LPR>
+struct Share {
+  int lane, n;
+  __device__ __forceinline__ int at(int i) const { return (lane + LPR * i) * V; }
+  __device__ __forceinline__ bool in(int i) const { return at(i) < n; }
+  template <typename T>
+  __device__ __forceinline__ void load(Raw<T, V> (&r)[NV], const T* row) const {
 #pragma unroll
-    for (int e = 0; e < V; ++e) o[e] = to_f<T>(w[e]);
+    for (int i = 0; i < NV; ++i) r[i].load(row + (in(i) ? at(i) : 0));
   }
-}
+  // f(i, e, in the row) of every element
+  template <typename F>
+  __device__ __forceinline__ static void each(F f) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) f(i, e);
+  }
+};
+
 template <typename T, int V>
 __device__ __forceinline__ void store(T* p, const float* x) {
   typedef T W __attribute__((ext_vector_type(V)));
@@ -126,142 +152,95 @@ struct Codes {
 
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-// x of a row -> its norm times weight plus bias (32 bits; elements past the row are 0
-// and stay out of the sums)
+// x of a row -> its norm times weight plus bias (32 bits); what lies past the row comes
+// in as 0 and stays out of the sums
 template <int V, int NV, int LPR>
-__device__ __forceinline__ void norm(float (&x)[NV][V], int lane, int H, const Norm& n, Group<LPR>& g) {
+__device__ __forceinline__ void norm(float (&x)[NV][V], const Share<V, NV, LPR>& sh, const Norm& n, Group<LPR>& g) {
+  using S = Share<V, NV, LPR>;
   if (n.kind != kNormNone) {
-    const float inv = 1.0f / (float)H;
+    const float inv = 1.0f / (float)sh.n;
     if (n.kind == kNormLayer) {
       float s = 0.0f;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) s += x[i][e];
+      S::each([&](int i, int e) __attribute__((always_inline)) { s += x[i][e]; });
       const float mean = g.sum(s) * inv;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const bool in = (lane + LPR * i) * V < H;
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[i][e] = in ? x[i][e] - mean : 0.0f;
-      }
+      S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] = sh.in(i) ? x[i][e] - mean : 0.0f; });
     }
     float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) s = fmaf(x[i][e], x[i][e], s);
+    S::each([&](int i, int e) __attribute__((always_inline)) { s = fmaf(x[i][e], x[i][e], s); });
     const float rstd = 1.0f / sqrtf(g.sum(s) * inv + n.eps);
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[i][e] *= rstd;
+    S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] *= rstd; });
   }
-  if (n.weight || n.bias) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + LPR * i) * V;
-      if (c < H) {
-        float w[V], b[V];
-        if (n.weight) {
-          load<float, V>(w, n.weight + c);
-#pragma unroll
-          for (int e = 0; e < V; ++e) x[i][e] *= w[e];
-        }
-        if (n.bias) {
-          load<float, V>(b, n.bias + c);
-#pragma unroll
-          for (int e = 0; e < V; ++e) x[i][e] += b[e];
-        }
-      }
-    }
+  if (n.weight) {
+    Raw<float, V> w[NV];
+    sh.load(w, n.weight);
+    S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] *= w[i][e]; });
+  }
+  if (n.bias) {
+    Raw<float, V> w[NV];
+    sh.load(w, n.bias);
+    S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] += w[i][e]; });
   }
 }
 
 template <typename T, int V, int LPR, int NV>
 __global__ __launch_bounds__(LPR > kThreads ? LPR : kThreads) void block_norms_kernel(BlockNormsParams p) {
   constexpr int RPB = LPR > kThreads ? 1 : kThreads / LPR;    // rows of a workgroup
+  using S = Share<V, NV, LPR>;
   __shared__ unsigned red[LPR > 64 ? 2 * LPR / 64 : 1];
-  const int lane = threadIdx.x % LPR, H = p.hidden;
   const int row = blockIdx.x * RPB + threadIdx.x / LPR;
   if (row >= p.rows) return;    // (the whole group of lanes; a group of several waves is a whole workgroup)
+  const S sh{(int)(threadIdx.x % LPR), p.hidden};
   Group<LPR> g{red};
   const size_t b = row / p.rows_per_batch * p.mod_stride;
-  const float* hr = p.h + row * p.h_stride;
+  // every load first, as far as the registers hold them
+  constexpr bool EARLY = NV * V <= 24;
+  Raw<float, V> h[NV], gate[NV], shift[NV], scale[NV];
+  Raw<T, V> y[NV];
+  if (EARLY || !p.y) sh.load(h, p.h + row * p.h_stride);
+  if (p.y) sh.load(y, reinterpret_cast<const T*>(p.y) + row * p.y_stride);
+  if (EARLY && p.gate) sh.load(gate, p.gate + b);
+  if (EARLY && p.scale) sh.load(scale, p.scale + b);
+  if (EARLY && p.shift) sh.load(shift, p.shift + b);
   float x[NV][V];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (lane + LPR * i) * V;
-#pragma unroll
-    for (int e = 0; e < V; ++e) x[i][e] = 0.0f;
-    if (c < H) load<float, V>(x[i], hr + c);
-  }
   if (p.y) {
-    const T* yr = reinterpret_cast<const T*>(p.y) + row * p.y_stride;
-    float y[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + LPR * i) * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) y[i][e] = 0.0f;
-      if (c < H) load<T, V>(y[i], yr + c);
-    }
-    norm<V, NV, LPR>(y, lane, H, p.post, g);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + LPR * i) * V;
-      if (c < H) {
-        float w[V];
-        if (p.gate) load<float, V>(w, p.gate + b + c);
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[i][e] = fmaf(p.residual_scale, x[i][e], p.gate ? w[e] * y[i][e] : y[i][e]);
-      }
-    }
+    float z[NV][V];
+    S::each([&](int i, int e) __attribute__((always_inline)) { z[i][e] = sh.in(i) ? y[i][e] : 0.0f; });
+    norm<V, NV, LPR>(z, sh, p.post, g);
+    if (!EARLY && p.gate) sh.load(gate, p.gate + b);
+    if (p.gate) S::each([&](int i, int e) __attribute__((always_inline)) { z[i][e] *= gate[i][e]; });
+    if (!EARLY) sh.load(h, p.h + row * p.h_stride);
+    S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] = fmaf(p.residual_scale, h[i][e], z[i][e]); });
   } else {
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[i][e] *= p.residual_scale;
+    S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] = p.residual_scale * h[i][e]; });
   }
   if (p.h_out) {
     float* o = p.h_out + row * p.h_out_stride;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + LPR * i) * V;
-      if (c < H) store<float, V>(o + c, x[i]);
-    }
+    for (int i = 0; i < NV; ++i)
+      if (sh.in(i)) store<float, V>(o + sh.at(i), x[i]);
   }
   if (!p.out && !p.codes) return;
-  norm<V, NV, LPR>(x, lane, H, p.pre, g);
-  unsigned top = 0;
+  S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] = sh.in(i) ? x[i][e] : 0.0f; });
+  norm<V, NV, LPR>(x, sh, p.pre, g);
+  if (!EARLY && p.scale) sh.load(scale, p.scale + b);
+  if (p.scale) S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] *= 1.0f + scale[i][e]; });
+  if (!EARLY && p.shift) sh.load(shift, p.shift + b);
+  if (p.shift) S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] += shift[i][e]; });
+  if (p.out) {
+    T* o = reinterpret_cast<T*>(p.out) + row * p.out_stride;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (lane + LPR * i) * V;
-    if (c < H) {
-      float w[V];
-      if (p.scale) {
-        load<float, V>(w, p.scale + b + c);
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[i][e] *= 1.0f + w[e];
-      }
-      if (p.shift) {
-        load<float, V>(w, p.shift + b + c);
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[i][e] += w[e];
-      }
-      if (p.out) store<T, V>(reinterpret_cast<T*>(p.out) + row * p.out_stride + c, x[i]);
-#pragma unroll
-      for (int e = 0; e < V; ++e) top = max(top, magnitude(x[i][e]));
-    }
+    for (int i = 0; i < NV; ++i)
+      if (sh.in(i)) store<T, V>(o + sh.at(i), x[i]);
   }
   if (!p.codes) return;
+  unsigned top = 0;
+  S::each([&](int i, int e) __attribute__((always_inline)) { top = max(top, sh.in(i) ? magnitude(x[i][e]) : 0u); });
   const Codes q(g.top(top));
+  signed char* o = p.codes + row * p.codes_stride;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (lane + LPR * i) * V;
-    if (c < H) q.put<V>(p.codes + row * p.codes_stride + c, x[i]);
-  }
-  if (lane == 0) p.code_scales[row] = q.scale;
+  for (int i = 0; i < NV; ++i)
+    if (sh.in(i)) q.put<V>(o + sh.at(i), x[i]);
+  if (sh.lane == 0) p.code_scales[row] = q.scale;
 }
 
 // Rows to codes.  NV 0: rows too long for the registers, read twice.
@@ -278,37 +257,36 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const T* __rest
   signed char* cr = codes + row * codes_stride;
   unsigned top = 0;
   if constexpr (NV > 0) {
-    float v[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + LPR * i) * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
-      if (c < cols) load<T, V>(v[i], xr + c);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) top = max(top, magnitude(v[i][e]));
+    const Share<V, NV, LPR> sh{lane, cols};
+    Raw<T, V> v[NV];
+    sh.load(v, xr);
+    // (what repeats the row's first elements does not change its largest)
+    sh.each([&](int i, int e) __attribute__((always_inline)) { top = max(top, magnitude(v[i][e])); });
     const Codes q(g.top(top));
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (lane + LPR * i) * V;
-      if (c < cols) q.put<V>(cr + c, v[i]);
+      float f[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) f[e] = v[i][e];
+      if (sh.in(i)) q.put<V>(cr + sh.at(i), f);
     }
     if (lane == 0) scales[row] = q.scale;
   } else {
+    Raw<T, V> v;
+#pragma unroll 4
     for (int c = lane * V; c < cols; c += LPR * V) {
-      float v[V];
-      load<T, V>(v, xr + c);
+      v.load(xr + c);
 #pragma unroll
       for (int e = 0; e < V; ++e) top = max(top, magnitude(v[e]));
     }
     const Codes q(g.top(top));
+#pragma unroll 4
     for (int c = lane * V; c < cols; c += LPR * V) {
-      float v[V];
-      load<T, V>(v, xr + c);
-      q.put<V>(cr + c, v);
+      v.load(xr + c);
+      float f[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) f[e] = v[e];
+      q.put<V>(cr + c, f);
     }
     if (lane == 0) scales[row] = q.scale;
   }
@@ -335,15 +313,14 @@ static void launch_norms_t(const BlockNormsParams& p, hipStream_t s) {
          p.h_out_stride % 4 == 0 && p.y_stride % 4 == 0 && p.out_stride % 4 == 0;
   if (four) {
     if (H <= 32 * 4 * 3) launch_norms<T, 4, 32, 3>(p, s);
-    else if (H <= 32 * 4 * 9) launch_norms<T, 4, 32, 9>(p, s);
-    else if (H <= 64 * 4 * 9) launch_norms<T, 4, 64, 9>(p, s);
-    else if (H <= 256 * 4 * 9) launch_norms<T, 4, 256, 9>(p, s);
-    else launch_norms<T, 4, 1024, 9>(p, s);
+    else if (H <= 64 * 4 * 5) launch_norms<T, 4, 64, 5>(p, s);
+    else if (H <= 256 * 4 * 5) launch_norms<T, 4, 256, 5>(p, s);
+    else launch_norms<T, 4, 1024, 8>(p, s);
   } else {
     if (H <= 64 * 8) launch_norms<T, 1, 64, 8>(p, s);
-    else if (H <= 64 * 36) launch_norms<T, 1, 64, 36>(p, s);
-    else if (H <= 256 * 36) launch_norms<T, 1, 256, 36>(p, s);
-    else launch_norms<T, 1, 1024, 36>(p, s);
+    else if (H <= 256 * 5) launch_norms<T, 1, 256, 5>(p, s);
+    else if (H <= 256 * 20) launch_norms<T, 1, 256, 20>(p, s);
+    else launch_norms<T, 1, 1024, 32>(p, s);
   }
 }
 
