@@ -10,6 +10,7 @@
 // Any M, N and K: rows past M and N re-read the last one and are not stored; the
 // bytes past K of the last k-tile are cleared in A's fragments (what W's hold
 // there does not matter then: integers have no NaN).
+#include <cmath>
 #include <cstdlib>
 
 #include "common.h"
@@ -30,281 +31,303 @@ __device__ __forceinline__ float gelu(float y) {
   return sizeof(T) == 2 ? y * __builtin_amdgcn_rcpf(1.0f + e) : y / (1.0f + e);
 }
 
+// m / rows_per_batch: a product with the rounded-up inverse, exact below 2^31
+__device__ __forceinline__ int branch(const GemmI8Params& p, int m) {
+  return (int)(((unsigned long long)(unsigned)m * p.rpb_inverse) >> p.rpb_shift);
+}
+
 // What a tile's epilogue reads beside its sums, in LDS: scales of its rows, scales
 // and biases of its columns.
 template <int BM, int BN>
 struct Side {
   float sa[BM], sw[BN], bias[BN];
-  struct Regs { float a[(BM + 255) / 256], w[(BN + 255) / 256], b[(BN + 255) / 256]; };
+  struct Regs { float a, w, b; };
   // (loads first, LDS writes behind the prologue's other loads; at least 256 threads)
   __device__ __forceinline__ static void fetch(Regs& r, const GemmI8Params& p, int m0, int n0) {
     const int t = threadIdx.x;
-    r.a[0] = t < BM && m0 + t < p.M ? p.sa[m0 + t] : 0.0f;
-    r.w[0] = t < BN && n0 + t < p.N ? p.sw[n0 + t] : 0.0f;
-    r.b[0] = t < BN && n0 + t < p.N && p.bias ? p.bias[n0 + t] : 0.0f;
+    r.a = t < BM && m0 + t < p.M ? p.sa[m0 + t] : 0.0f;
+    r.w = t < BN && n0 + t < p.N ? p.sw[n0 + t] : 0.0f;
+    r.b = t < BN && n0 + t < p.N && p.bias ? p.bias[n0 + t] : 0.0f;
   }
   __device__ __forceinline__ void keep(const Regs& r) {
     const int t = threadIdx.x;
-    if (t < BM) sa[t] = r.a[0];
-    if (t < BN) sw[t] = r.w[0], bias[t] = r.b[0];
+    if (t < BM) sa[t] = r.a;
+    if (t < BN) sw[t] = r.w, bias[t] = r.b;
   }
   static_assert(BM <= 256 && BN <= 256, "one value a thread");
 };
 
-// 32 rows x TN columns of sums, staged in LDS (rows of TN + 4 ints, so that the
-// 16-byte writes of 16 rows land in distinct banks), then walked in 16-byte chunks of
-// the output's rows, or along V^T's tokens.
-template <typename T, int TN, int EPI>
-struct Strip {
-  static constexpr int LS = TN + 4;
-  static constexpr int BYTES = 32 * LS * 4;
+// The epilogue of a 32 x 32 block of sums from (m, n) on, straight from the registers.
+// The MFMAs make transposed blocks: lane (lr, h) = (lane % 32, lane / 32) holds row lr,
+// columns 8 g + 4 h + r.  In bf16 the halves h swap registers, so that a lane holds columns 16 h
+// .. 16 h + 15 and every store is 16 bytes.  V^T wants tokens next to each other: its
+// blocks (`Vt`) are made the other way round, so that a lane holds column lr and tokens 8 g + 4 h
+// + r.
+template <typename T, int EPI, bool Vt>
+struct Block {
   const GemmI8Params& p;
-  const int* strip;
-  const float *sa, *sw, *bias;   // of the strip's rows, of its columns
-  int lane, m0, n0, split;       // its first row and column
+  int lr, h;
 
-  __device__ __forceinline__ float value(int s, float a, float w, float b) const { return fmaf((float)s * a, w, b); }
-
-  __device__ __forceinline__ void rows_store() const {
-    constexpr int CE = 16 / sizeof(T), CH = TN / CE, RQ = 64 / CH;
-    static_assert(64 % CH == 0, "a lane's columns stay the same");
-    const int c = lane % CH * CE, n = n0 + c;
-    if (n >= p.N) return;
-    float w[CE], b[CE];
-#pragma unroll
-    for (int e = 0; e < CE; ++e) w[e] = sw[c + e], b[e] = bias[c + e];
-    T* out = reinterpret_cast<T*>(p.out);
-#pragma unroll
-    for (int q = 0; q < 32 / RQ; ++q) {
-      const int r = q * RQ + lane / CH, m = m0 + r;
-      if (m >= p.M) continue;
-      T o[CE];
-#pragma unroll
-      for (int e = 0; e < CE; e += 4) {
-        const i32x4 s = *reinterpret_cast<const i32x4*>(strip + r * LS + c + e);
-#pragma unroll
-        for (int f = 0; f < 4; ++f) {
-          const float y = value(s[f], sa[r], w[e + f], b[e + f]);
-          o[e + f] = from_f<T>(EPI == kEpiGelu ? gelu<T>(y) : y);
-        }
-      }
-      put<CE>(out + (size_t)m * p.N + n, o, p.N - n);
-    }
-  }
-
-  // CE values to p, `left` of them within the row
-  template <int CE, typename U>
-  __device__ __forceinline__ void put(U* d, const U* o, int left) const {
-    typedef U W __attribute__((ext_vector_type(CE)));
-    if (p.wide) {
-      W v;
-#pragma unroll
-      for (int e = 0; e < CE; ++e) v[e] = o[e];
-      *reinterpret_cast<W*>(d) = v;
+  // columns' (Vt: the column's) scales and biases, and rows' scales, of the lane
+  struct Cols { f32x4 w[Vt ? 1 : 4], b[Vt ? 1 : 4]; };
+  __device__ __forceinline__ void cols(Cols& c, const float* sw, const float* bias) const {
+    if constexpr (Vt) {
+      c.w[0][0] = sw[lr];
+      c.b[0][0] = bias[lr];
     } else {
 #pragma unroll
-      for (int e = 0; e < CE; ++e)
-        if (e < left) d[e] = o[e];
+      for (int g = 0; g < 4; ++g) {
+        c.w[g] = *reinterpret_cast<const f32x4*>(sw + 8 * g + 4 * h);
+        c.b[g] = *reinterpret_cast<const f32x4*>(bias + 8 * g + 4 * h);
+      }
     }
   }
 
-  __device__ __forceinline__ void rows_residual() const {
-    constexpr int CH = TN / 4, RQ = 64 / CH, IT = 32 / RQ;
-    const int c = lane % CH * 4, n = n0 + c;
-    if (n >= p.N) return;
-    float* out = reinterpret_cast<float*>(p.out);
-    const f32x4 w = *reinterpret_cast<const f32x4*>(sw + c), b = *reinterpret_cast<const f32x4*>(bias + c);
-    const int left = p.N - n;
-    int br = m0 / p.rows_per_batch;
-    f32x4 h[IT], g[IT];
-    // (all loads first: the stores may alias them as far as the compiler knows)
+  // four bf16 as two words
+  __device__ __forceinline__ static uint2 pack(const float* y) {
+    const bf16x4 v = {(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+    return __builtin_bit_cast(uint2, v);
+  }
+  // 16 bytes with what the other half holds of groups g (kept by h = 0) and g + 2 (by h = 1)
+  __device__ __forceinline__ static uint4 join(uint2 x, uint2 y) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto a = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+    return make_uint4(a[0], b[0], a[1], b[1]);
+#else
+    return make_uint4(x.x, x.y, y.x, y.y);
+#endif
+  }
+
+  // where (row m, column n) of Q, K or V^T lies
+  __device__ __forceinline__ T* at(int b, int tok, int n) const {
+    const int hidden = p.hidden, which = n >= 2 * hidden ? 2 : n >= hidden ? 1 : 0, nn = n - which * hidden;
+    const int head = (int)__umulhi((unsigned)nn, p.hd_magic), dd = nn - head * p.head_dim;
+    T* kv = reinterpret_cast<T*>(p.kv) + b * p.kv_bs;
+    const size_t ntot = (size_t)p.kv_tokens, t = (size_t)(p.tok_offset + tok);
+    if (which == 0) return reinterpret_cast<T*>(p.q) + (((size_t)b * p.heads + head) * p.rows_per_batch + tok) * p.head_dim + dd;
+    if (which == 1) return kv + ((size_t)head * ntot + t) * p.head_dim + dd;
+    return kv + ntot * hidden + ((size_t)head * p.head_dim + dd) * ntot + t;
+  }
+
+  // outputs of a block, before a gated residual
+  __device__ __forceinline__ void values(float (&y)[4][4], const i32x16& acc, const Cols& c, const float* sa) const {
+    const float own = Vt ? 0.0f : sa[lr];
 #pragma unroll
-    for (int q = 0; q < IT; ++q) {
-      const int m = min(m0 + q * RQ + lane / CH, p.M - 1);
-      while (m >= (long long)(br + 1) * p.rows_per_batch) ++br;
-      const float *hr = out + (size_t)m * p.N + n, *gr = p.gate + br * p.gate_stride + n;
-      if (p.wide) {
-        h[q] = *reinterpret_cast<const f32x4*>(hr);
-        g[q] = *reinterpret_cast<const f32x4*>(gr);
+    for (int g = 0; g < 4; ++g) {
+      f32x4 a;
+      if constexpr (Vt) a = *reinterpret_cast<const f32x4*>(sa + 8 * g + 4 * h);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        y[g][r] = Vt ? fmaf((float)acc[4 * g + r] * a[r], c.w[0][0], c.b[0][0])
+                     : fmaf((float)acc[4 * g + r] * own, c.w[Vt ? 0 : g][r], c.b[Vt ? 0 : g][r]);
+        if (EPI == kEpiGelu) y[g][r] = gelu<T>(y[g][r]);
+      }
+    }
+  }
+
+  // 16 bytes of outputs from (m, n) on: channels (Vt: tokens) next to each other.  Rows of
+  // `out` take 16-byte accesses (p.wide).  held: the same in LDS, where they are.
+  __device__ __forceinline__ void sink(const uint4& v, const T* held, int m, int n) const {
+    constexpr int CE = 16 / sizeof(T);
+    if (m >= p.M || n >= p.N) return;
+    if constexpr (EPI == kEpiResidual) {
+      float* out = reinterpret_cast<float*>(p.out) + (size_t)m * p.N + n;
+      const f32x4 y = __builtin_bit_cast(f32x4, v), hv = *reinterpret_cast<const f32x4*>(out),
+                  g = *reinterpret_cast<const f32x4*>(p.gate + branch(p, m) * p.gate_stride + n);
+      f32x4 o;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[r] = fmaf(g[r], y[r], hv[r]);
+      *reinterpret_cast<f32x4*>(out) = o;
+    } else if constexpr (EPI == kEpiQkv) {
+      const int b = branch(p, m), tok = m - b * p.rows_per_batch;
+      T* d = at(b, tok, n);
+      // whole: the 16 bytes lie next to each other (not so at a branch's end, or for V^T's columns
+      // beside K's in one wave's blocks)
+      if (Vt ? m + CE <= p.M && tok + CE <= p.rows_per_batch && ((uintptr_t)d & 15) == 0 : n < 2 * p.hidden) {
+        *reinterpret_cast<uint4*>(d) = v;
+      } else if (held) {
+#pragma unroll 1
+        for (int f = 0; f < CE; ++f) one(held[f], Vt ? m + f : m, Vt ? n : n + f);
       } else {
+        typedef T W __attribute__((ext_vector_type(CE)));
+        const W w = __builtin_bit_cast(W, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[q][e] = e < left ? hr[e] : 0.0f, g[q][e] = e < left ? gr[e] : 0.0f;
+        for (int f = 0; f < CE; ++f) one(w[f], Vt ? m + f : m, Vt ? n : n + f);
       }
-    }
-#pragma unroll
-    for (int q = 0; q < IT; ++q) {
-      const int r = q * RQ + lane / CH, m = m0 + r;
-      if (m >= p.M) continue;
-      const i32x4 s = *reinterpret_cast<const i32x4*>(strip + r * LS + c);
-      float o[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(g[q][e], value(s[e], sa[r], w[e], b[e]), h[q][e]);
-      put<4>(out + (size_t)m * p.N + n, o, left);
+    } else {
+      *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + (size_t)m * p.N + n) = v;
     }
   }
+  __device__ __forceinline__ void one(T x, int m, int n) const {
+    const int b = branch(p, m);
+    if (m < p.M && n < p.N) *at(b, m - b * p.rows_per_batch, n) = x;
+  }
 
-  __device__ __forceinline__ void rows_qkv() const {
-    const int hd = p.head_dim, hidden = p.hidden, rpb = p.rows_per_batch;
-    const size_t ntot = (size_t)p.kv_tokens;
-    T* qb = reinterpret_cast<T*>(p.q);
-    T* kvb = reinterpret_cast<T*>(p.kv);
-    const int b0 = m0 / rpb;
-    // Q and K: 16 bytes of one head's row a lane
-    if (n0 < 2 * hidden) {
-      constexpr int CE = 16 / sizeof(T), CH = TN / CE, RQ = 64 / CH;
-      const int c = lane % CH * CE, n = n0 + c;
-      if (n < 2 * hidden) {
-        const int which = n >= hidden, nn = n - which * hidden;
-        const int head = (int)__umulhi((unsigned)nn, p.hd_magic), dd = nn - head * hd;
-        float w[CE], bi[CE];
+  // a block straight from the registers
+  __device__ __forceinline__ void run(const i32x16& acc, const Cols& c, const float* sa, int m0, int n0, int split) const {
+    if constexpr (EPI == kEpiPartial) {
+      const int m = m0 + lr;
+      int* d = p.ws + ((size_t)split * p.M + m) * p.N + n0;
+      if (m < p.M) {
 #pragma unroll
-        for (int e = 0; e < CE; ++e) w[e] = sw[c + e], bi[e] = bias[c + e];
-        int b = b0;
+        for (int g = 0; g < 4; ++g) {
+          const int n = 8 * g + 4 * h;
+          if (p.N % 4 == 0) {
+            if (n0 + n < p.N)
+              *reinterpret_cast<i32x4*>(d + n) = i32x4{acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]};
+          } else {
 #pragma unroll
-        for (int q = 0; q < 32 / RQ; ++q) {
-          const int r = q * RQ + lane / CH, m = m0 + r;
-          if (m >= p.M) continue;
-          while (m >= (long long)(b + 1) * rpb) ++b;
-          const int tok = m - b * rpb;
-          T* dst = which == 0 ? qb + (((size_t)b * p.heads + head) * rpb + tok) * hd + dd
-                              : kvb + b * p.kv_bs + ((size_t)head * ntot + p.tok_offset + tok) * hd + dd;
-          typedef T W __attribute__((ext_vector_type(CE)));
-          W o;
-#pragma unroll
-          for (int e = 0; e < CE; e += 4) {
-            const i32x4 s = *reinterpret_cast<const i32x4*>(strip + r * LS + c + e);
-#pragma unroll
-            for (int f = 0; f < 4; ++f) o[e + f] = from_f<T>(value(s[f], sa[r], w[e + f], bi[e + f]));
+            for (int r = 0; r < 4; ++r)
+              if (n0 + n + r < p.N) d[n + r] = acc[4 * g + r];
           }
-          *reinterpret_cast<W*>(dst) = o;
         }
       }
-    }
-    // V^T [head][d][token]: 8 consecutive tokens of one channel a lane, four lanes the
-    // strip's 32.  Groups 2 and 3 read their tokens rotated by four (8 LS = 32 mod 64
-    // banks would put them on the banks of groups 0 and 1; 4 LS = 16 mod 64 moves them
-    // to the free ones), then swap the halves back.
-    static_assert((4 * LS) % 64 == 16, "conflict-free V^T reads");
-    if (n0 + TN > 2 * hidden) {
+    } else {
+      float y[4][4];
+      values(y, acc, c, sa);
+      if (EPI != kEpiQkv && !p.wide) {
 #pragma unroll
-      for (int q = 0; q < TN / 16; ++q) {
-        const int col = q * 16 + (lane >> 2), grp = lane & 3, n = n0 + col;
-        if (n < 2 * hidden || n >= p.N) continue;
-        const int rot = (grp >> 1) * 4;
-        int s[8];
+        for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int t = 0; t < 8; ++t) s[t] = strip[(grp * 8 + ((t + rot) & 7)) * LS + col];   // token t ^ rot
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int x = s[t], y = s[t + 4];
-          s[t] = rot ? y : x;
-          s[t + 4] = rot ? x : y;
-        }
-        T o[8];
-#pragma unroll
-        for (int t = 0; t < 8; ++t) o[t] = from_f<T>(value(s[t], sa[grp * 8 + t], sw[col], bias[col]));
-        const int nn = n - 2 * hidden, head = (int)__umulhi((unsigned)nn, p.hd_magic), dd = nn - head * hd;
-        T* vt = kvb + ntot * hidden + ((size_t)head * hd + dd) * ntot + p.tok_offset;
-        const int m = m0 + grp * 8;
-        int b = b0;
-        if (m >= p.M) continue;
-        while (m >= (long long)(b + 1) * rpb) ++b;
-        const int tok = m - b * rpb;
-        T* dst = vt + b * p.kv_bs + tok;
-        if (m + 7 < p.M && tok + 7 < rpb && ((uintptr_t)dst & 15) == 0) {
-          constexpr int CE = 16 / sizeof(T);
-          typedef T W __attribute__((ext_vector_type(CE)));
-#pragma unroll
-          for (int e = 0; e < 8; e += CE) {
-            W v;
-#pragma unroll
-            for (int f = 0; f < CE; ++f) v[f] = o[e + f];
-            *reinterpret_cast<W*>(dst + e) = v;
-          }
-        } else {
-#pragma unroll
-          for (int t = 0; t < 8; ++t) {
-            const int mm = m + t;
-            if (mm < p.M) {
-              while (mm >= (long long)(b + 1) * rpb) ++b;
-              vt[b * p.kv_bs + (mm - b * rpb)] = o[t];
+          for (int r = 0; r < 4; ++r) {
+            const int m = m0 + lr, n = n0 + 8 * g + 4 * h + r;
+            if (m < p.M && n < p.N) {
+              T* d = reinterpret_cast<T*>(p.out) + (size_t)m * p.N + n;
+              if constexpr (EPI == kEpiResidual) *d = fmaf(p.gate[branch(p, m) * p.gate_stride + n], y[g][r], *d);
+              else *d = from_f<T>(y[g][r]);
             }
           }
+      } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint4 v = join(pack(y[e]), pack(y[e + 2]));
+          const int x = 16 * h + 8 * e;
+          if constexpr (Vt) sink(v, nullptr, m0 + x, n0 + lr);
+          else sink(v, nullptr, m0 + lr, n0 + x);
+        }
+      } else {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const uint4 v = __builtin_bit_cast(uint4, f32x4{y[g][0], y[g][1], y[g][2], y[g][3]});
+          const int x = 8 * g + 4 * h;
+          if constexpr (Vt) sink(v, nullptr, m0 + x, n0 + lr);
+          else sink(v, nullptr, m0 + lr, n0 + x);
         }
       }
     }
-  }
-
-  // a k-split's sums, rows of ws[split]
-  __device__ __forceinline__ void rows_partial() const {
-    constexpr int CH = TN / 4, RQ = 64 / CH;
-    const int c = lane % CH * 4, n = n0 + c;
-    if (n >= p.N) return;
-    int* ws = p.ws + (size_t)split * p.M * p.N;
-#pragma unroll
-    for (int q = 0; q < 32 / RQ; ++q) {
-      const int r = q * RQ + lane / CH, m = m0 + r;
-      if (m >= p.M) continue;
-      const i32x4 s = *reinterpret_cast<const i32x4*>(strip + r * LS + c);
-      int* d = ws + (size_t)m * p.N + n;
-      if (p.N % 4 == 0) {
-        *reinterpret_cast<i32x4*>(d) = s;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < p.N) d[e] = s[e];
-      }
-    }
-  }
-
-  __device__ __forceinline__ void rows() const {
-    if (m0 >= p.M) return;
-    if constexpr (EPI == kEpiStore || EPI == kEpiGelu) rows_store();
-    else if constexpr (EPI == kEpiResidual) rows_residual();
-    else if constexpr (EPI == kEpiPartial) rows_partial();
-    else rows_qkv();
   }
 };
 
-// Columns of a strip of a wave that holds FN blocks of 32
-constexpr int strip_cols(int FN) { return FN % 2 ? 32 : 64; }
-constexpr int strip_bytes(int FN) { return 32 * (strip_cols(FN) + 4) * 4; }
-
-// A wave's sums, FM x FN blocks of 32 x 32 from (m0 + mw, n0 + nw) of the tile at (m0,
-// n0); the MFMAs make transposed blocks: a lane holds row lane % 32, columns 8 g + 4
-// (lane / 32) + 0 .. 3.
-template <typename T, int EPI, int FM, int FN, int BM, int BN>
-__device__ __forceinline__ void epilogue(const GemmI8Params& p, const i32x16 (&acc)[FM][FN], char* lds, const Side<BM, BN>& side,
-                                         int lane, int m0, int n0, int mw, int nw, int split) {
-  constexpr int SN = strip_cols(FN), SB = SN / 32;
-  using S = Strip<T, SN, EPI>;
-  int* strip = reinterpret_cast<int*>(lds);
-  const int lr = lane & 31, h = lane >> 5;
+// A wave's sums, FM x FN blocks from (m, n) on, whose rows' scales are at sa, columns'
+// at sw and bias.
+template <typename T, int EPI, bool Vt, int FM, int FN>
+__device__ __forceinline__ void direct(const GemmI8Params& p, const i32x16 (&acc)[FM][FN], const float* sa, const float* sw,
+                                       const float* bias, int lane, int m, int n, int split) {
+  using B = Block<T, EPI, Vt>;
+  const B blk{p, lane & 31, lane >> 5};
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+  for (int j = 0; j < FN; ++j) {
+    if (n + 32 * j >= p.N) break;
+    typename B::Cols c;
+    if constexpr (EPI != kEpiPartial) blk.cols(c, sw + 32 * j, bias + 32 * j);
 #pragma unroll
-    for (int jb = 0; jb < FN; jb += SB) {
-#pragma unroll
-      for (int j = 0; j < SB; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<i32x4*>(strip + lr * S::LS + j * 32 + 8 * g + 4 * h) =
-              i32x4{acc[i][jb + j][4 * g], acc[i][jb + j][4 * g + 1], acc[i][jb + j][4 * g + 2], acc[i][jb + j][4 * g + 3]};
-      const int mr = mw + 32 * i, nc = nw + 32 * jb;
-      S{p, strip, side.sa + mr, side.sw + nc, side.bias + nc, lane, m0 + mr, n0 + nc, split}.rows();
-    }
+    for (int i = 0; i < FM; ++i)
+      if (m + 32 * i < p.M) blk.run(acc[i][j], c, sa + 32 * i, m + 32 * i, n + 32 * j, split);
+  }
 }
 
-// Which tile a workgroup takes: workgroup b is in split b / T of T = tiles_m x
-// tiles_n tiles; inside a split XCD-major, then groups of 8 tile rows, column-major
+// The same by way of LDS, so that a store instruction writes whole 128-byte lines (eight
+// rows of 64 bf16 or 32 fp32; stores straight from the registers write 32 bytes of 32 rows:
+// 32768 x 1152 -> 4608 took 231 us, by way of LDS 213).  16 rows at a time in an area of the
+// wave's own; rows 144 bytes apart spread over the banks.
+constexpr int kLine = 144, kArea = 16 * kLine;
+
+template <typename T, int EPI, bool Vt, int FM, int FN>
+__device__ __forceinline__ void staged(const GemmI8Params& p, const i32x16 (&acc)[FM][FN], char* area, const float* sa,
+                                       const float* sw, const float* bias, int lane, int m, int n) {
+  using B = Block<T, EPI, Vt>;
+  const B blk{p, lane & 31, lane >> 5};
+  const int lr = blk.lr, h = blk.h;
+  // blocks side by side along the stored rows: two in bf16, one in fp32
+  constexpr int SB = sizeof(T) == 2 ? 2 : 1, CE = 16 / sizeof(T);
+  constexpr int O = Vt ? FN : FM, I = Vt ? FM : FN;       // blocks across and along the stored rows
+  typename B::Cols c[Vt ? 1 : FN];
+  if constexpr (!Vt) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) blk.cols(c[j], sw + 32 * j, bias + 32 * j);
+  }
+#pragma unroll
+  for (int o = 0; o < O; ++o) {
+    if ((Vt ? n : m) + 32 * o >= (Vt ? p.N : p.M)) break;
+    if constexpr (Vt) blk.cols(c[0], sw + 32 * o, bias + 32 * o);
+#pragma unroll
+    for (int i0 = 0; i0 < I; i0 += SB) {
+      const int along = (Vt ? m : n) + 32 * i0;
+      if (along >= (Vt ? p.M : p.N)) break;
+      // (this turn's addresses from this turn's copy: hoisted ones would not fit the registers)
+      int at = lane;
+      if constexpr (EPI == kEpiQkv) asm volatile("" : "+v"(at));
+      const int nb = i0 + SB <= I ? SB : 1, ch8 = sizeof(T) == 2 ? 4 * nb : 8;    // (a last block of its own: half lines)
+      uint4 v[4];     // chunk 4 k + 2 h + e of block k in bf16, 2 g + h in fp32
+#pragma unroll
+      for (int k = 0; k < nb; ++k) {
+        float y[4][4];
+        if constexpr (Vt) blk.values(y, acc[i0 + k][o], c[0], sa + 32 * (i0 + k));
+        else blk.values(y, acc[o][i0 + k], c[i0 + k], sa + 32 * o);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) v[2 * k + e] = B::join(B::pack(y[e]), B::pack(y[e + 2]));
+        } else {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) v[g] = __builtin_bit_cast(uint4, f32x4{y[g][0], y[g][1], y[g][2], y[g][3]});
+        }
+      }
+#pragma unroll
+      for (int pass = 0; pass < 2; ++pass) {
+        if ((lr >> 4) == pass) {
+#pragma unroll
+          for (int x = 0; x < ch8 / 2; ++x)
+            *reinterpret_cast<uint4*>(area + (lr & 15) * kLine +
+                                      (sizeof(T) == 2 ? 4 * (x >> 1) + 2 * h + (x & 1) : 2 * x + h) * 16) = v[x];
+        }
+#pragma unroll
+        for (int q = 0; q < ch8 / 4; ++q) {
+          const int row = q * 8 + at / ch8, ch = at % ch8;
+          const char* held = area + row * kLine + ch * 16;
+          const uint4 w = *reinterpret_cast<const uint4*>(held);
+          const T* el = reinterpret_cast<const T*>(held);
+          const int across = (Vt ? n : m) + 32 * o + 16 * pass + row;
+          if constexpr (Vt) blk.sink(w, el, along + CE * ch, across);
+          else blk.sink(w, el, across, along + CE * ch);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+}
+
+// Whether a wave's blocks from column n on are V^T's alone, and so made the other way round
+template <int EPI>
+__device__ __forceinline__ bool all_vt(const GemmI8Params& p, int n) {
+  return EPI == kEpiQkv && n >= 2 * p.hidden;
+}
+template <bool Vt>
+__device__ __forceinline__ i32x16 mfma(const i32x4& a, const i32x4& w, const i32x16& c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (Vt) return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, w, c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_i32_32x32x32_i8(w, a, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+// Which tile workgroup `pid` takes: XCD-major, then groups of 8 tile rows, column-major
 // inside.
 struct TileAt {
-  int split, m, n;
-  __device__ __forceinline__ TileAt(int tiles_m, int tiles_n) {
-    const int T = tiles_m * tiles_n;
-    split = __builtin_amdgcn_readfirstlane(blockIdx.x / T);
-    int pid = blockIdx.x - split * T;
-    const int per = T / 8;
+  int m, n;
+  __device__ __forceinline__ TileAt(int tiles_m, int tiles_n, int pid) {
+    const int per = tiles_m * tiles_n / 8;
     if (pid < per * 8) pid = (pid & 7) * per + (pid >> 3);
     constexpr int GROUP = 8;
     const int gid = pid / (GROUP * tiles_n);
@@ -336,53 +359,48 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const signed char* b
 #endif
 
 // ---------------------------------------------------------------------------
-// BM x BN tile over WM x WN waves, k-tiles of BK bytes in a ring of S stages: one
-// barrier a k-tile; the loads of tile kt + S - 1 lie between the MFMAs of tile kt.
-template <int BM, int BN, int BK, int WM, int WN, int S>
+// BM x BN tile over WM x WN waves, k-tiles of 128 bytes in a ring of S stages: one barrier a
+// k-tile; the loads of tile kt + S - 1 lie between the MFMAs of tile kt.
+template <int BM, int BN, int WM, int WN, int S>
 struct Geo {
-  static constexpr int NW = WM * WN;
+  static constexpr int BK = 128, NW = WM * WN;
   static constexpr int TM = BM / WM, TN = BN / WN;  // wave tile
   static constexpr int FM = TM / 32, FN = TN / 32;  // 32x32 blocks per wave
-  static constexpr int CPR = BK / 16;               // 16-byte chunks per row
-  static constexpr int RPL = 1024 / BK;             // rows per wave-level load
-  static constexpr int Q = 256 / BK;                // rows per 256-byte bank sweep
-  static constexpr int IA = BM / (NW * RPL), IB = BN / (NW * RPL);
-  static constexpr int LPT = IA + IB;               // loads per lane per k-tile
+  static constexpr int IA = BM / (8 * NW), LPT = IA + BN / (8 * NW);  // loads of A's rows, of all, per lane and k-tile
   static constexpr int STAGE = (BM + BN) * BK;
   static constexpr int KK = BK / 32;                // MFMA k-steps per k-tile
   static constexpr int LPK = S == 2 ? LPT : (LPT + KK - 1) / KK;
-  static constexpr int STRIPS = NW * strip_bytes(FN);
-  static constexpr int RING = S * STAGE > STRIPS ? S * STAGE : STRIPS;   // the strips take the ring's place
+  static constexpr int RING = S * STAGE;
   static constexpr int LDS = RING + (int)sizeof(Side<BM, BN>);
-  static_assert(BK == 64 || BK == 128, "k-tile");
   static_assert(NW >= 4 && TM % 32 == 0 && TN % 32 == 0, "wave tile");
-  static_assert(BM % (NW * RPL) == 0 && BN % (NW * RPL) == 0, "rows per wave");
-  static_assert(S >= 2 && LPT * (S - 1) < 60 && LDS <= 160 * 1024, "pipeline depth");
+  static_assert(BM % (NW * 8) == 0 && BN % (NW * 8) == 0, "rows per wave");
+  static_assert(S >= 2 && LPT * (S - 1) < 60 && NW * kArea <= RING && LDS <= 160 * 1024, "LDS");
 };
 
-template <int BM, int BN, int BK, int WM, int WN, int S, int WPE, typename T, int EPI>
+template <int BM, int BN, int WM, int WN, int S, int WPE, typename T, int EPI>
 __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p, int tiles_m, int tiles_n) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  using G = Geo<BM, BN, BK, WM, WN, S>;
-  constexpr int FM = G::FM, FN = G::FN, KK = G::KK, IA = G::IA, LPT = G::LPT, LPK = G::LPK;
+  using G = Geo<BM, BN, WM, WN, S>;
+  constexpr int BK = G::BK, FM = G::FM, FN = G::FN, KK = G::KK, IA = G::IA, LPT = G::LPT, LPK = G::LPK;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
-  const TileAt at(tiles_m, tiles_n);
+  const TileAt at(tiles_m, tiles_n, blockIdx.x);
   const int m0 = at.m * BM, n0 = at.n * BN;
   auto& side = *reinterpret_cast<Side<BM, BN>*>(smem + G::RING);
   typename Side<BM, BN>::Regs sr;
-  if constexpr (EPI != kEpiPartial) side.fetch(sr, p, m0, n0);
+  side.fetch(sr, p, m0, n0);
 
-  // load j covers tile rows (j NW + wave) RPL .. + RPL - 1 (A's first, then W's)
+  // load j covers tile rows (j NW + wave) 8 .. + 8 (A's first, then W's); chunk c of row r lies at
+  // c ^ (r / 2 % 8)
   unsigned off[LPT];
 #pragma unroll
   for (int j = 0; j < LPT; ++j) {
-    const int r = ((j < IA ? j : j - IA) * G::NW + wave) * G::RPL + lane / G::CPR;
-    const int ch = (lane % G::CPR) ^ ((r / G::Q) % G::CPR);
-    off[j] = j < IA ? (unsigned)min(r, p.M - 1 - m0) * (unsigned)p.lda + ch * 16u
-                    : (unsigned)min(r, p.N - 1 - n0) * (unsigned)p.ldw + ch * 16u;
+    const int r = ((j < IA ? j : j - IA) * G::NW + wave) * 8 + (lane >> 3);
+    const unsigned ch = (unsigned)((lane & 7) ^ ((r >> 1) & 7)) * 16u;
+    off[j] = j < IA ? (unsigned)min(r, p.M - 1 - m0) * (unsigned)p.lda + ch
+                    : (unsigned)min(r, p.N - 1 - n0) * (unsigned)p.ldw + ch;
   }
   const __amdgpu_buffer_rsrc_t rA = rows_rsrc(p.A, p.lda, m0, p.M, BM, p.K);
   const __amdgpu_buffer_rsrc_t rW = rows_rsrc(p.W, p.ldw, n0, p.N, BN, p.K);
@@ -398,30 +416,26 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
   const int lrow = lane & 31, h = lane >> 5;
   int koff[KK];
 #pragma unroll
-  for (int kk = 0; kk < KK; ++kk) koff[kk] = ((2 * kk + h) ^ ((lrow / G::Q) % G::CPR)) * 16;
+  for (int kk = 0; kk < KK; ++kk) koff[kk] = ((2 * kk + h) ^ ((lrow >> 1) & 7)) * 16;
   const int arow = (wm * G::TM + lrow) * BK, brow = BM * BK + (wn * G::TN + lrow) * BK;
 
-  // this split's k-tiles
-  const int all = (p.K + BK - 1) / BK;
-  const int kt0 = EPI == kEpiPartial ? (int)((long long)all * at.split / p.splits) : 0;
-  const int KT = EPI == kEpiPartial ? (int)((long long)all * (at.split + 1) / p.splits) - kt0 : all;
-  const int left = p.K - (kt0 + KT - 1) * BK;     // bytes of k in its last one
+  const int KT = (p.K + BK - 1) / BK;
+  const int left = p.K - (KT - 1) * BK;           // bytes of k in the last k-tile
 
-  // load j of its k-tile kt into stage st
-  auto dma = [&](auto jc, int kt, int st) __attribute__((always_inline)) {
+  // load j of k-tile t into its stage
+  auto dma = [&](auto jc, int t) __attribute__((always_inline)) {
     constexpr int j = decltype(jc)::value;
     constexpr int i = j < IA ? j : j - IA;
-    char* dst = smem + st * G::STAGE + (j < IA ? 0 : BM * BK) + (i * G::NW + wave) * 1024;
+    char* dst = smem + t % S * G::STAGE + (j < IA ? 0 : BM * BK) + (i * G::NW + wave) * 1024;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(j < IA ? rA : rW, (ORCH_LDS void*)dst, 16, off[j],
-                                             (unsigned)(kt0 + kt) * BK, 0, 0);
+                                             (unsigned)t * BK, 0, 0);
   };
-  // the MFMAs of stage st, with ISSUE the loads of k-tile ikt into stage ist between
-  // them: MFMA e of k-step kk, then its share of the next k-step's fragments, then its
-  // share of the loads
-  auto compute = [&](int st, auto issue_c, auto last_c, int ikt, int ist) __attribute__((always_inline)) {
+  // the MFMAs of k-tile t, with ISSUE the loads of k-tile t + S - 1 between them: MFMA e of k-step
+  // kk, then its share of the next k-step's fragments, then its share of the loads
+  auto compute = [&](auto vt_c, auto issue_c, auto last_c, int t) __attribute__((always_inline)) {
     constexpr bool ISSUE = decltype(issue_c)::value;
     constexpr int NM = FM * FN, ND = FM + FN;
-    const char* base = smem + st * G::STAGE;
+    const char* base = smem + t % S * G::STAGE;
     i32x4 a[2][FM], b[2][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i) a[0][i] = *reinterpret_cast<const i32x4*>(base + arow + i * 32 * BK + koff[0]);
@@ -441,13 +455,13 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
       }
       static_for<0, NM>([&](auto ec) __attribute__((always_inline)) {
         constexpr int e = decltype(ec)::value, i = e / FN, j = e % FN;
-        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[cur][j], a[cur][i], acc[i][j], 0, 0, 0);
+        acc[i][j] = mfma<decltype(vt_c)::value>(a[cur][i], b[cur][j], acc[i][j]);
         static_for<e * nd / NM, (e + 1) * nd / NM>([&](auto dc) __attribute__((always_inline)) {
           constexpr int d = decltype(dc)::value;
           if constexpr (d < FM) a[cur ^ 1][d] = *reinterpret_cast<const i32x4*>(base + arow + d * 32 * BK + koff[kk + 1]);
           else b[cur ^ 1][d - FM] = *reinterpret_cast<const i32x4*>(base + brow + (d - FM) * 32 * BK + koff[kk + 1]);
         });
-        static_for<l0 + e * nl / NM, l0 + (e + 1) * nl / NM>([&](auto jc) __attribute__((always_inline)) { dma(jc, ikt, ist); });
+        static_for<l0 + e * nl / NM, l0 + (e + 1) * nl / NM>([&](auto jc) __attribute__((always_inline)) { dma(jc, t + S - 1); });
         __builtin_amdgcn_sched_barrier(0);
       });
     });
@@ -457,28 +471,181 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
 
 #pragma unroll
   for (int s = 0; s < S - 1; ++s)
-    if (s < KT) static_for<0, LPT>([&](auto jc) __attribute__((always_inline)) { dma(jc, s, s); });
-  if constexpr (EPI != kEpiPartial) side.keep(sr);
-  int kt = 0;
-  for (; kt + S - 1 < KT; ++kt) {
-    wait_vmcnt<(S - 2) * LPT>();
+    if (s < KT) static_for<0, LPT>([&](auto jc) __attribute__((always_inline)) { dma(jc, s); });
+  side.keep(sr);
+  auto loop = [&](auto vt) __attribute__((always_inline)) {
+    int t = 0;
+    for (; t + S - 1 < KT; ++t) {
+      wait_vmcnt<(S - 2) * LPT>();
+      lds_barrier();
+      compute(vt, Yes{}, No{}, t);
+    }
+    // the last S - 1 (or fewer): all loads are on their way
+    for (; t + 1 < KT; ++t) {
+      if (S > 3 && t + 3 == KT) wait_vmcnt<(S > 3 ? 2 : 0) * LPT>();
+      else if (S > 2 && t + 2 == KT) wait_vmcnt<LPT>();
+      else wait_vmcnt<0>();
+      lds_barrier();
+      compute(vt, No{}, No{}, t);
+    }
+    wait_vmcnt<0>();
     lds_barrier();
-    compute(kt % S, Yes{}, No{}, kt + S - 1, (kt + S - 1) % S);
-  }
-  // the last S - 1 (or fewer): all loads are on their way
-  for (; kt + 1 < KT; ++kt) {
-    if (S > 3 && kt + 3 == KT) wait_vmcnt<(S > 3 ? 2 : 0) * LPT>();
-    else if (S > 2 && kt + 2 == KT) wait_vmcnt<LPT>();
-    else wait_vmcnt<0>();
-    lds_barrier();
-    compute(kt % S, No{}, No{}, 0, 0);
-  }
-  wait_vmcnt<0>();
-  lds_barrier();
-  compute(kt % S, No{}, Yes{}, 0, 0);
+    compute(vt, No{}, Yes{}, t);
+    __syncthreads();    // (the areas take the ring's place; the side's values are there)
+    const int mw = wm * G::TM, nw = wn * G::TN;
+    const float *sa = side.sa + mw, *sw = side.sw + nw, *bias = side.bias + nw;
+    if (EPI == kEpiQkv || p.wide)
+      staged<T, EPI, decltype(vt)::value>(p, acc, smem + wave * kArea, sa, sw, bias, lane, m0 + mw, n0 + nw);
+    else
+      direct<T, EPI, decltype(vt)::value>(p, acc, sa, sw, bias, lane, m0 + mw, n0 + nw, 0);
+  };
+  // (a wave's own choice: both loops meet the same barriers)
+  if (all_vt<EPI>(p, n0 + wn * G::TN)) loop(Yes{});
+  else loop(No{});
+#endif
+}
 
-  __syncthreads();
-  epilogue<T, EPI>(p, acc, smem + wave * strip_bytes(FN), side, lane, m0, n0, wm * G::TM, wn * G::TN, at.split);
+// ---------------------------------------------------------------------------
+// BM x 256 tiles, BM 256 or 192, eight waves (2 x 4, BM / 2 x 64 outputs each), k-tiles of 128 bytes in two
+// LDS stages, one workgroup a CU that takes tiles until none is left.  The k-tiles of its
+// tiles are one sequence: one barrier a k-tile, the next one's loads between the MFMAs, and
+// behind a tile's last come the next one's first, whose loads are in flight while the
+// outputs are written.  Behind the last tile the buffers of the loads are empty, so that they
+// fetch nothing.  Needs K % 16 == 0 and rows of out that take 16-byte accesses.
+template <int BM>
+struct BigGeo {
+  static constexpr int BN = 256, BK = 128, KK = 4, STAGE = (BM + BN) * BK;
+  static constexpr int FM = BM / 64, IA = BM / 64, LPT = IA + 4;    // blocks of a wave, loads of A's rows, of all
+  static constexpr int SIDES = 2 * STAGE, AREAS = SIDES + 2 * (int)sizeof(Side<BM, BN>), LDS = AREAS + 8 * kArea;
+  static_assert(BM % 64 == 0 && LDS <= 160 * 1024, "LDS");
+};
+
+template <int BM, typename T, int EPI>
+__global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m, int tiles_n) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  using G = BigGeo<BM>;
+  constexpr int BN = G::BN, BK = G::BK, KK = G::KK, STAGE = G::STAGE, FM = G::FM, IA = G::IA, LPT = G::LPT;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, lr = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const int tiles = tiles_m * tiles_n, KT = (p.K + BK - 1) / BK;
+  Side<BM, BN>* sides = reinterpret_cast<Side<BM, BN>*>(smem + G::SIDES);
+
+  // The loads' place in the sequence: k-tile lk of tile lt.  Load j fills tile rows (8 j + wave)
+  // 8 .. + 8, A's first, then W's; chunk c of row r lies at c ^ (r / 2 % 8).  A's chunks past
+  // K, in a tile's last k-tile, are loaded from past the buffer, which gives 0.
+  int lt = blockIdx.x, lk = 0, lside = 0;
+  const int lrow = wave * 8 + (lane >> 3), chunk = (lane & 7) ^ ((lrow >> 1) & 7);
+  const unsigned past = ((KT - 1) * 8 + chunk) * 16 < p.K ? 0u : 0x80000000u;
+  unsigned off[LPT];
+  __amdgpu_buffer_rsrc_t rA, rW;
+  auto place = [&]() __attribute__((always_inline)) {
+    if (lt >= tiles) {
+      rA = buffer_rsrc(p.A, 0);
+      rW = buffer_rsrc(p.W, 0);
+      return;
+    }
+    const TileAt ta(tiles_m, tiles_n, lt);
+    const int m0 = ta.m * BM, n0 = ta.n * BN;
+#pragma unroll
+    for (int j = 0; j < LPT; ++j)
+      off[j] = (j < IA ? (unsigned)min(64 * j + lrow, p.M - 1 - m0) * (unsigned)p.lda
+                       : (unsigned)min(64 * (j - IA) + lrow, p.N - 1 - n0) * (unsigned)p.ldw) + chunk * 16u;
+    rA = rows_rsrc(p.A, p.lda, m0, p.M, BM, p.K);
+    rW = rows_rsrc(p.W, p.ldw, n0, p.N, BN, p.K);
+    // the tile's scales and biases: 64 values a load, twelve loads over the waves
+    Side<BM, BN>& sd = sides[lside];
+    const int part = (wave & 3) * 64;
+    const unsigned o = (unsigned)(part + lane) * 4u;
+    if (wave < 4) {
+      const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(p.sa + m0, (size_t)min(p.M - m0, BM) * 4);
+      const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(p.sw + n0, (size_t)min(p.N - n0, BN) * 4);
+      if (part < BM) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (ORCH_LDS void*)(sd.sa + part), 4, o, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (ORCH_LDS void*)(sd.sw + part), 4, o, 0, 0, 0);
+    } else if (p.bias) {
+      const __amdgpu_buffer_rsrc_t rb = buffer_rsrc(p.bias + n0, (size_t)min(p.N - n0, BN) * 4);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (ORCH_LDS void*)(sd.bias + part), 4, o, 0, 0, 0);
+    } else {
+      sd.bias[part + lane] = 0.0f;
+    }
+  };
+  auto load = [&](auto jc, int st) __attribute__((always_inline)) {
+    constexpr int j = decltype(jc)::value;
+    char* dst = smem + st * STAGE + (j * 8 + wave) * 1024;     // (W's rows follow A's)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(j < IA ? rA : rW, (ORCH_LDS void*)dst, 16,
+                                             j < IA ? off[j] | (lk == KT - 1 ? past : 0u) : off[j], (unsigned)lk * BK, 0, 0);
+  };
+  auto next = [&]() __attribute__((always_inline)) {
+    if (++lk == KT) {
+      lk = 0;
+      lt += gridDim.x;
+      lside ^= 1;
+      place();
+    }
+  };
+
+  i32x16 acc[FM][2];
+  int koff[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) koff[kk] = ((2 * kk + h) ^ ((lr >> 1) & 7)) * 16;
+  const int arow = (wm * (BM / 2) + lr) * BK, brow = BM * BK + (wn * 64 + lr) * BK;
+  // the MFMAs of stage st: MFMA e of k-step kk, then its share of the next k-step's fragments
+  // and, in the first k-step, of the loads into the other stage
+  auto compute = [&](auto vt, int st) __attribute__((always_inline)) {
+    const char* base = smem + st * STAGE;
+    i32x4 a[2][FM], b[2][2];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) a[0][i] = *reinterpret_cast<const i32x4*>(base + arow + i * 32 * BK + koff[0]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) b[0][j] = *reinterpret_cast<const i32x4*>(base + brow + j * 32 * BK + koff[0]);
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<0, KK>([&](auto kkc) __attribute__((always_inline)) {
+      constexpr int kk = decltype(kkc)::value, cur = kk & 1, NM = 2 * FM, nd = kk + 1 < KK ? FM + 2 : 0;
+      static_for<0, NM>([&](auto ec) __attribute__((always_inline)) {
+        constexpr int e = decltype(ec)::value, i = e / 2, j = e % 2;
+        acc[i][j] = mfma<decltype(vt)::value>(a[cur][i], b[cur][j], acc[i][j]);
+        static_for<e * nd / NM, (e + 1) * nd / NM>([&](auto dc) __attribute__((always_inline)) {
+          constexpr int d = decltype(dc)::value;
+          if constexpr (d < FM) a[cur ^ 1][d] = *reinterpret_cast<const i32x4*>(base + arow + d * 32 * BK + koff[kk + 1]);
+          else b[cur ^ 1][d - FM] = *reinterpret_cast<const i32x4*>(base + brow + (d - FM) * 32 * BK + koff[kk + 1]);
+        });
+        if constexpr (kk == 0)
+          static_for<e * LPT / NM, (e + 1) * LPT / NM>([&](auto jc) __attribute__((always_inline)) { load(jc, st ^ 1); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+  };
+
+  place();
+  static_for<0, LPT>([&](auto jc) __attribute__((always_inline)) { load(jc, 0); });
+  int st = 0, side = 0;
+  for (int ct = blockIdx.x; ct < tiles; ct += gridDim.x) {
+    const TileAt ta(tiles_m, tiles_n, ct);
+    const int m0 = ta.m * BM + wm * (BM / 2), n0 = ta.n * BN + wn * 64;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+    auto tile = [&](auto vt) __attribute__((always_inline)) {
+      for (int kt = 0; kt < KT; ++kt) {
+        wait_vmcnt<0>();
+        lds_barrier();
+        next();
+        compute(vt, st);
+        st ^= 1;
+      }
+      const Side<BM, BN>& sd = sides[side];
+      staged<T, EPI, decltype(vt)::value>(p, acc, smem + G::AREAS + wave * kArea, sd.sa + wm * (BM / 2), sd.sw + wn * 64,
+                                          sd.bias + wn * 64, lane, m0, n0);
+    };
+    if (all_vt<EPI>(p, n0)) tile(std::true_type{});
+    else tile(std::false_type{});
+    side ^= 1;
+  }
+  wait_vmcnt<0>();    // (loads into LDS that is about to be another workgroup's)
 #endif
 }
 
@@ -494,10 +661,9 @@ struct SmallGeo {
   static constexpr int RING = KG * S * STAGE;
   static constexpr int LDS = RING + (int)sizeof(Side<BM, BN>);
   static constexpr int SUMS = (KG - 1) * NWG * 4096;
-  static constexpr int STRIP = strip_bytes(1);
   static_assert((BM / 32) * (BN / 32) == NWG, "a 32 x 32 block per wave");
   static_assert((BM + BN) / 8 % NWG == 0 && (S - 1) * LPT < 60, "whole loads");
-  static_assert(SUMS + NWG * STRIP <= RING && LDS <= 160 * 1024, "LDS");
+  static_assert(SUMS <= RING && LDS <= 160 * 1024, "LDS");
 };
 
 template <int BM, int BN, int KG, int S, typename T, int EPI>
@@ -561,6 +727,7 @@ __global__ __launch_bounds__(256) void small_kernel(GemmI8Params p, int tiles_n)
   for (int t = 0; t < S - 1; ++t)
     if (t < mine) issue(t);
   if constexpr (EPI != kEpiPartial) side.keep(sr);
+  const bool vt = all_vt<EPI>(p, n0 + nw);
   for (int t = 0; t < NIT; ++t) {
     if (t + S - 2 < mine) wait_vmcnt<(S - 2) * LPT>();
     else wait_vmcnt<0>();
@@ -579,7 +746,11 @@ __global__ __launch_bounds__(256) void small_kernel(GemmI8Params p, int tiles_n)
       for (int c = 0; c < 4; ++c) a[c] &= within(left, 2 * c + h);
     }
 #pragma unroll
-    for (int c = 0; c < 4; ++c) acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[c], a[c], acc[0][0], 0, 0, 0);
+    for (int c = 0; c < 4; ++c) {
+      // (the block of V^T the other way round: the operands change places)
+      const i32x4 x = vt ? a[c] : b[c], y = vt ? b[c] : a[c];
+      acc[0][0] = mfma<false>(y, x, acc[0][0]);
+    }
   }
   __syncthreads();
   if constexpr (KG > 1) {
@@ -597,35 +768,48 @@ __global__ __launch_bounds__(256) void small_kernel(GemmI8Params p, int tiles_n)
       for (int r = 0; r < 16; ++r) acc[0][0][r] += part[r * 64];
     }
   }
-  // (the strips lie past the groups' sums)
-  epilogue<T, EPI>(p, acc, smem + G::SUMS + wg * G::STRIP, side, lane, m0, n0, mw, nw, split);
+  if (vt) direct<T, EPI, true>(p, acc, side.sa + mw, side.sw + nw, side.bias + nw, lane, m0 + mw, n0 + nw, split);
+  else direct<T, EPI, false>(p, acc, side.sa + mw, side.sw + nw, side.bias + nw, lane, m0 + mw, n0 + nw, split);
 #endif
 }
 
-// The k-splits' sums, then the caller's epilogue: a strip of 32 x 64 a wave.
+// The k-splits' sums, then the caller's epilogue: a workgroup a block of 32 x 32, whose four
+// waves share the splits (at most kMaxSplits, so that a wave's loads are in flight at once).
+constexpr int kMaxSplits = 16;
+
 template <typename T, int EPI>
-__global__ __launch_bounds__(256) void split_sum_kernel(GemmI8Params p, int strips_n, int strips) {
-  using S = Strip<T, 64, EPI>;
-  __shared__ __attribute__((aligned(16))) int lds[4][S::BYTES / 4];
-  __shared__ __attribute__((aligned(16))) float sides[4][32 + 64 + 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int id = blockIdx.x * 4 + wave;
-  if (id >= strips) return;
-  const int m0 = id / strips_n * 32, n0 = id % strips_n * 64;
-  int* strip = lds[wave];
-  float* sd = sides[wave];
-  if (lane < 32) sd[lane] = m0 + lane < p.M ? p.sa[m0 + lane] : 0.0f;
-  sd[32 + lane] = n0 + lane < p.N ? p.sw[n0 + lane] : 0.0f;
-  sd[96 + lane] = n0 + lane < p.N && p.bias ? p.bias[n0 + lane] : 0.0f;
+__global__ __launch_bounds__(256) void split_sum_kernel(GemmI8Params p, int blocks_n) {
+  __shared__ __attribute__((aligned(16))) Side<32, 32> sd;
+  __shared__ int part[3][16][64];
+  const int lane = threadIdx.x & 63, lr = lane & 31, h = lane >> 5, wave = threadIdx.x >> 6;
+  const int m0 = blockIdx.x / blocks_n * 32, n0 = blockIdx.x % blocks_n * 32;
+  typename Side<32, 32>::Regs sr;
+  sd.fetch(sr, p, m0, n0);
+  sd.keep(sr);
   const size_t MN = (size_t)p.M * p.N;
-  const int n = n0 + lane;
-  for (int r = 0; r < 32; ++r) {
-    int s = 0;
-    if (m0 + r < p.M && n < p.N)
-      for (int k = 0; k < p.splits; ++k) s += p.ws[k * MN + (size_t)(m0 + r) * p.N + n];
-    strip[r * S::LS + lane] = s;
+  const bool vt = all_vt<EPI>(p, n0);
+  i32x16 acc[1][1];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[0][0][r] = 0;
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / 4; ++i) {
+    const int k = wave + 4 * i;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int x = 8 * (r >> 2) + 4 * h + (r & 3), m = m0 + (vt ? x : lr), n = n0 + (vt ? lr : x);
+      if (k < p.splits && m < p.M && n < p.N) acc[0][0][r] += p.ws[k * MN + (size_t)m * p.N + n];
+    }
   }
-  S{p, strip, sd, sd + 32, sd + 96, lane, m0, n0, 0}.rows();
+  if (wave > 0) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) part[wave - 1][r][lane] = acc[0][0][r];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[0][0][r] += part[0][r][lane] + part[1][r][lane] + part[2][r][lane];
+  if (vt) direct<T, EPI, true>(p, acc, sd.sa, sd.sw, sd.bias, lane, m0, n0, 0);
+  else direct<T, EPI, false>(p, acc, sd.sa, sd.sw, sd.bias, lane, m0, n0, 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -640,14 +824,14 @@ static void allow_lds(K kern, int lds) {
   (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
 }
 
-template <int BM, int BN, int BK, int WM, int WN, int S, int WPE, typename T, int EPI>
+template <int BM, int BN, int WM, int WN, int S, int WPE, typename T, int EPI>
 static void launch_ring(const GemmI8Params& p, hipStream_t s) {
-  using G = Geo<BM, BN, BK, WM, WN, S>;
-  auto kern = ring_kernel<BM, BN, BK, WM, WN, S, WPE, T, EPI>;
+  using G = Geo<BM, BN, WM, WN, S>;
+  auto kern = ring_kernel<BM, BN, WM, WN, S, WPE, T, EPI>;
   static const bool once = (allow_lds(kern, G::LDS), true);
   (void)once;
   const int tm = ceil_div(p.M, BM), tn = ceil_div(p.N, BN);
-  hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn * p.splits)), dim3(64 * WM * WN), G::LDS, s, p, tm, tn);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn)), dim3(64 * WM * WN), G::LDS, s, p, tm, tn);
 }
 
 template <int BM, int BN, int KG, int S, typename T, int EPI>
@@ -660,29 +844,72 @@ static void launch_small(const GemmI8Params& p, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(p.M, BM) * tn * p.splits)), dim3(256), G::LDS, s, p, tn);
 }
 
-enum Form { k256x128, k128x128, k64x64, k32x64, k32x32, kForms };
+// Tiles go round 256 workgroups, one a CU.
+template <int BM, typename T, int EPI>
+static void launch_big(const GemmI8Params& p, hipStream_t s) {
+  using G = BigGeo<BM>;
+  auto kern = big_kernel<BM, T, EPI>;
+  static const bool once = (allow_lds(kern, G::LDS), true);
+  (void)once;
+  const int tm = ceil_div(p.M, BM), tn = ceil_div(p.N, G::BN);
+  hipLaunchKernelGGL(kern, dim3((unsigned)cmin(tm * tn, 256)), dim3(512), G::LDS, s, p, tm, tn);
+}
+
+enum Form { k256x256, k192x256, k128x128, k128x128Alone, k64x64, k32x64, k32x32, kForms };
 
 template <typename T, int EPI>
 static void launch_form(int f, const GemmI8Params& p, hipStream_t s) {
   switch (f) {
-    case k256x128: launch_ring<256, 128, 64, 2, 2, 3, 2, T, EPI>(p, s); break;
-    case k128x128: launch_ring<128, 128, 128, 2, 2, 2, 2, T, EPI>(p, s); break;
-    case k64x64: launch_small<64, 64, 1, 3, T, EPI>(p, s); break;
+    case k256x256: launch_big<256, T, EPI>(p, s); break;
+    case k192x256: launch_big<192, T, EPI>(p, s); break;
+    case k128x128: launch_ring<128, 128, 2, 2, 2, 2, T, EPI>(p, s); break;
+    case k128x128Alone: launch_ring<128, 128, 4, 2, 4, 2, T, EPI>(p, s); break;
+    case k64x64: launch_ring<64, 64, 2, 2, 4, 2, T, EPI>(p, s); break;
     case k32x64: launch_small<32, 64, 2, 3, T, EPI>(p, s); break;
     default: launch_small<32, 32, 4, 3, T, EPI>(p, s); break;
   }
 }
 
+// The form with the least estimated time in us, T its tiles and KT the k-tiles of 128: fitted to M
+// from 1 to 32768 at the DiT projections of hidden 384 and 1152 and K up to 4608 (one run each,
+// stores of bf16).  Measured, us, 256 x 256 / 192 x 256 / 128 x 128 / alone / 64 x 64 / 32 x 64 / 32 x 32:
+//   32768 x 1152 -> 4608      198 / 210 / 229 / 324 / 383 / 800 / 1900
+//   3328 x 1152 -> 3456        23 /  20 /  22 /  26 /  31 /  58 /  131
+//   3328 x 4608 -> 1152        59 /  50 /  35 /  25 /  36 /  54 /  107
+//   768 x 4608 -> 1152         46 /  38 /  26 /  18 /  11 /  15 /   27
+//   96 x 4608 -> 1152           - /   - /   - /   - / 9.4 / 11.4 / 7.1
+// A CU holds one workgroup of the large tiles, of `alone` and of 32 x 32, two of the others, where
+// one's outputs are written beside another's products.
 struct Plan { int form, splits; };
 
-static Plan pick(int M, int N, int K, size_t ws_elems) {
-  const int f = forced();
-  if (f >= 0 && f < kForms) return {f, 1};
-  const long long blocks = (long long)ceil_div(M, 32) * ceil_div(N, 32);
-  if (blocks <= 512) return {k32x32, 1};
-  if (blocks <= 2048) return {k32x64, 1};
-  if (blocks <= 4096) return {k64x64, 1};
-  return {(long long)ceil_div(M, 256) * ceil_div(N, 128) >= 256 ? k256x128 : k128x128, 1};
+static Plan pick(int M, int N, int K, bool wide, size_t ws_elems) {
+  const bool big_ok = wide && K % 16 == 0;
+  const int f = forced(), kt = ceil_div(K, 128);
+  if (f >= 0 && f < kForms && (f > k192x256 || big_ok)) return {f, 1};
+  float best = 0.0f;
+  int form = -1;
+  auto tiles = [&](int bm, int bn) { return (float)ceil_div(M, bm) * ceil_div(N, bn); };
+  auto rounds = [&](float t) { return ceilf(t / 256.0f); };
+  auto take = [&](int c, float us) {
+    if (form < 0 || us < best) form = c, best = us;
+  };
+  const float k = (float)kt, t128 = tiles(128, 128), t64 = tiles(64, 64), t3264 = tiles(32, 64), t32 = tiles(32, 32);
+  if (big_ok) {
+    take(k256x256, 2.5f + rounds(tiles(256, 256)) * (8.0f + 1.4f * k));
+    take(k192x256, 2.5f + rounds(tiles(192, 256)) * (6.5f + 1.1f * k));
+  }
+  take(k128x128, t128 <= 256 ? 5.5f + 0.65f * k : 3.0f + t128 / 512 * (4.0f + k));
+  take(k128x128Alone, 4.0f + rounds(t128) * (2.5f + 0.3f * k) + t128 / 256 * (2.5f + 0.22f * k));
+  take(k64x64, t64 <= 256 ? 3.5f + 0.2f * k : 3.0f + t64 / 512 * (1.0f + 0.45f * k));
+  take(k32x64, t3264 <= 256 ? 3.2f + 0.22f * k : 3.0f + t3264 / 512 * (1.3f + 0.45f * k));
+  take(k32x32, 2.9f + 0.105f * k + (rounds(t32) - 1) * (1.6f + 0.155f * k));
+  // Few blocks of a long K: its k-tiles over more workgroups, 16 at least each, and a second launch
+  // that adds their sums (32 x 18432 -> 128: 18.3 -> 12.9 us; 131056 111 -> 22)
+  if (form == k32x32 && kt >= 96) {
+    const int wgs = ceil_div(M, 32) * ceil_div(N, 32), sp = cmin(cmin(256 / cmin(wgs, 256), kMaxSplits), kt / 16);
+    if (sp > 1 && (size_t)sp * M * N <= ws_elems) return {form, sp};
+  }
+  return {form, 1};
 }
 
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -693,12 +920,18 @@ static hipError_t launch_t(const GemmI8Params& p0, hipStream_t s) {
   constexpr int ce = EPI == kEpiResidual ? 4 : 16 / (int)sizeof(T);
   p.wide = p.N % ce == 0 && aligned16(p.out) && (EPI != kEpiResidual || (aligned16(p.gate) && p.gate_stride % 4 == 0));
   if (EPI == kEpiQkv) p.hd_magic = (unsigned)((0x100000000ull + p.head_dim - 1) / p.head_dim);
-  const Plan pl = pick(p.M, p.N, p.K, p.ws ? p.ws_elems : 0);
+  if (EPI == kEpiQkv || EPI == kEpiResidual) {
+    int l = 0;
+    while ((1ll << l) < p.rows_per_batch) ++l;
+    p.rpb_shift = 31 + l;
+    p.rpb_inverse = (unsigned)(((1ull << p.rpb_shift) + p.rows_per_batch - 1) / p.rows_per_batch);
+  }
+  const Plan pl = pick(p.M, p.N, p.K, EPI == kEpiQkv || p.wide, p.ws ? p.ws_elems : 0);
   p.splits = pl.splits;
   if (pl.splits > 1) {
-    launch_form<T, kEpiPartial>(pl.form, p, s);
-    const int sn = ceil_div(p.N, 64), strips = ceil_div(p.M, 32) * sn;
-    hipLaunchKernelGGL((split_sum_kernel<T, EPI>), dim3(ceil_div(strips, 4)), dim3(256), 0, s, p, sn, strips);
+    launch_small<32, 32, 4, 3, T, kEpiPartial>(p, s);
+    const int bn = ceil_div(p.N, 32), blocks = ceil_div(p.M, 32) * bn;
+    hipLaunchKernelGGL((split_sum_kernel<T, EPI>), dim3(blocks), dim3(256), 0, s, p, bn);
   } else {
     launch_form<T, EPI>(pl.form, p, s);
   }
@@ -719,7 +952,7 @@ static hipError_t launch_epi(const GemmI8Params& p, int epi, hipStream_t s) {
 }  // namespace i8
 
 size_t gemm_int8_workspace_bytes(int M, int N, int K) {
-  const i8::Plan pl = i8::pick(M, N, K, (size_t)-1);
+  const i8::Plan pl = i8::pick(M, N, K, true, (size_t)-1);
   return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0;
 }
 

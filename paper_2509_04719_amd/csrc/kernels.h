@@ -274,6 +274,8 @@ struct GemmI8Params {
   size_t kv_bs;
   int kv_tokens, tok_offset, heads, hidden, head_dim;
   unsigned hd_magic;          // set by the launcher: ceil(2^32 / head_dim)
+  unsigned rpb_inverse;       // set by the launcher: ceil(2^rpb_shift / rows_per_batch)
+  int rpb_shift;
   int wide;                   // set by the launcher: rows of out take 16-byte accesses
   int* ws;                    // optional: sums of k-splits, int32 [splits][M][N]
   size_t ws_elems;

@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
 HALF = {"f32": U, "bf16": 2.0 ** -8}
-FORMS = range(5)
+FORMS = range(7)
 
 
 @pytest.fixture(params=FORMS)
@@ -219,3 +219,34 @@ def test_no_rows(orch_lib, shape):
     W = lib.int8_rows(torch.zeros((N, 64), dtype=torch.int8, device=DEV)[:, :K], torch.ones(N, device=DEV))
     lib.linear_quantized(A, W, None, lib.EPI_STORE, torch.empty((0, N), device=DEV))
     lib.quantize_rows(torch.empty((0, K), device=DEV), A)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 12161, 24), (33, 13000, 72), (70, 16385, 96), (32, 131071, 40)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_split_k(orch_lib, dtype, M, K, N):
+    """A long K over more workgroups: the same bits as without workspace, for every epilogue."""
+    lib = orch_lib
+    rng = np.random.default_rng(K)
+    need = lib.linear_quantized_workspace_bytes(M, N, K)
+    assert need > 0
+    ws = torch.full((need // 4 + 4,), -7, dtype=torch.int32, device=DEV)
+    A, W, bias, s, *_ = _operands(lib, rng, M, K, N, gap=16)
+    bd, gate, dt = to_dev(bias), to_dev(rng.standard_normal((M, N))), torch.float32 if dtype == "f32" else torch.bfloat16
+    h = to_dev(rng.standard_normal((M, N)))
+    for epi in (lib.EPI_STORE, lib.EPI_GELU, lib.EPI_RESIDUAL):
+        outs = []
+        for w in (None, ws[:need // 4 - 1], ws[:need // 4]):
+            outs.append(h.clone() if epi == lib.EPI_RESIDUAL else torch.empty((M, N), dtype=dt, device=DEV))
+            lib.linear_quantized(A, W, bd, epi, outs[-1], gate=gate, rows_per_batch=1, workspace=w)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+        if epi == lib.EPI_STORE:
+            _check(to_host(outs[2]), s + bias, 3 * U * np.abs(s) + U * np.abs(s + bias), dtype)
+    assert torch.all(ws[need // 4:] == -7)
+    B, H = 1 if M % 2 else 2, 32 * 3
+    if N == H:
+        qk = []
+        for w in (None, ws):
+            q, kv = torch.empty((B, 1, M // B, 32), dtype=dt, device=DEV), torch.zeros((B, 2 * (M // B + 3) * 32), dtype=dt, device=DEV)
+            lib.qkv_projection_quantized(A, W, bd, q, kv, M // B + 3, 2, workspace=w)
+            qk.append((q, kv))
+        assert torch.equal(qk[0][0], qk[1][0]) and torch.equal(qk[0][1], qk[1][1])
