@@ -202,6 +202,18 @@ def _check_ints(*values):
         raise OrchError(ORCH_EINVAL, f"{values}: past an int's range")
 
 
+_F32 = None
+
+
+def _f32():
+    """torch.float32 (torch is not imported before the first use)."""
+    global _F32
+    if _F32 is None:
+        import torch
+        _F32 = torch.float32
+    return _F32
+
+
 _CODES = {}             # by torch type, filled at the first use (torch is not imported before)
 
 
@@ -517,14 +529,26 @@ def norm(kind, eps=1e-6, weight=None, bias=None) -> Norm:
         raise OrchError(ORCH_EINVAL, f"norm {kind!r}: one of {', '.join(NORM_CODE)} is needed")
     n = Norm(NORM_CODE[kind], eps, _ptr(weight), _ptr(bias))
     n.tensors = tuple(t for t in (weight, bias) if t is not None)
-    n.devices, n.channels = tuple(t.get_device() for t in n.tensors), {t.shape[0] for t in n.tensors}
+    n.devices, n.channels = tuple(t.get_device() for t in n.tensors), n.tensors[0].shape[0] if n.tensors else None
+    if len(n.tensors) == 2 and bias.shape != weight.shape:
+        raise OrchError(ORCH_EINVAL, "weight and bias must hold as many channels")
     n.packed = bytes(n)
     return n
 
 
 _NO_NORM = Norm(0, 0.0, None, None)
-_NO_NORM.devices, _NO_NORM.channels, _NO_NORM.packed = (), set(), bytes(_NO_NORM)
+_NO_NORM.devices, _NO_NORM.channels, _NO_NORM.packed = (), None, bytes(_NO_NORM)
 _BLOCK_NORMS = struct.Struct("=24s24sf3i13Q")   # orch_block_norms' layout
+
+
+def _stream_here(stream, device, *others):
+    """_stream_on for tensors of one device: a current GPU that is theirs needs no second look."""
+    if device < 0 or stream is not None or others.count(device) != len(others):
+        return _stream_on(stream, device, *others)
+    from torch import _C
+    if _C._cuda_getDevice() != device:
+        return _stream_on(stream, device)
+    return _C._cuda_getCurrentRawStream(device)
 
 
 def block_norms(h, y=None, h_out=None, out=None, *, post=None, pre=None, gate=None, shift=None, scale=None,
@@ -535,54 +559,78 @@ def block_norms(h, y=None, h_out=None, out=None, *, post=None, pre=None, gate=No
     shape = h.shape
     rows, hidden = shape
     post, pre = post or _NO_NORM, pre or _NO_NORM
-    devices = (h.get_device(),) + post.devices + pre.devices
-    out8 = 0
-    if isinstance(out, Int8Rows):
-        if out.shape != (rows, hidden):
-            raise OrchError(ORCH_EINVAL, f"out holds {out.shape} codes, the call writes {(rows, hidden)}")
-        devices += out.devices
-        out8, out = out.address, None
-    code = ORCH_BF16 if y is None and out is None else _code(out if y is None else y)
-    ptrs, strides = [], []
-    for t, c in ((h, ORCH_F32), (y, code), (h_out, ORCH_F32), (out, code)):
-        if t is None:
-            ptrs.append(0)
-            strides.append(0)
-            continue
-        s = t.stride()
-        if t.shape != shape or _code(t) != c or (s[1] != 1 and hidden > 1):
-            raise OrchError(ORCH_EINVAL, f"h, y, h_out and out must be {list(shape)} of fp32 or the call's type, channels next to each other")
-        devices += (t.get_device(),)
-        ptrs.append(t.data_ptr())
-        strides.append(s[0])
+    others = post.devices + pre.devices
+    f32, one = _f32(), hidden == 1
+    typed = y
+    out8 = ptr_y = ptr_ho = ptr_o = st_y = st_ho = st_o = 0
+    if out is not None:
+        if type(out) is Int8Rows:
+            if out.shape != (rows, hidden):
+                raise OrchError(ORCH_EINVAL, f"out holds {out.shape} codes, the call writes {(rows, hidden)}")
+            others += out.devices
+            out8 = out.address
+        else:
+            st_o, c = out.stride()
+            ptr_o = out.data_ptr()
+            others += (out.get_device(),)
+            if y is None:
+                typed = out
+            if out.shape != shape or out.dtype is not typed.dtype or not (c == 1 or one):
+                _bad_rows(shape)
+    st_h, c = h.stride()
+    if h.dtype is not f32 or not (c == 1 or one):
+        _bad_rows(shape)
+    if y is not None:
+        st_y, c = y.stride()
+        ptr_y = y.data_ptr()
+        others += (y.get_device(),)
+        if y.shape != shape or not (c == 1 or one):
+            _bad_rows(shape)
+    if h_out is not None:
+        st_ho, c = h_out.stride()
+        ptr_ho = h_out.data_ptr()
+        others += (h_out.get_device(),)
+        if h_out.dtype is not f32 or h_out.shape != shape or not (c == 1 or one):
+            _bad_rows(shape)
+    code = ORCH_BF16 if typed is None else _code(typed)
     mods, mod_stride = [], None
     for t in (gate, shift, scale):
         if t is None:
             mods.append(0)
             continue
-        s, (branches, channels) = t.stride(), t.shape
+        (s, c), (branches, channels) = t.stride(), t.shape
         if mod_stride is None:
-            mod_stride, need = s[0], -(-rows // rows_per_batch) if rows_per_batch > 0 else 0
-        if branches < need or channels != hidden or _code(t) != ORCH_F32 or (s[1] != 1 and hidden > 1) or (s[0] != mod_stride and need > 1):
+            mod_stride, need = s, -(-rows // rows_per_batch) if rows_per_batch > 0 else 0
+        if branches < need or channels != hidden or t.dtype is not f32 or not (c == 1 or one) or (s != mod_stride and need > 1):
             raise OrchError(ORCH_EINVAL, f"gate, shift and scale must be fp32 [{need}, {hidden}] of one row stride, channels next to each other")
-        devices += (t.get_device(),)
+        others += (t.get_device(),)
         mods.append(t.data_ptr())
-    if not (post.channels | pre.channels) <= {hidden}:
+    if post.channels not in (None, hidden) or pre.channels not in (None, hidden):
         raise OrchError(ORCH_EINVAL, f"a norm's weight and bias must hold {hidden} channels")
-    _check_ints(rows_per_batch, 0)
-    p = _BLOCK_NORMS.pack(post.packed, pre.packed, residual_scale, rows, hidden, rows_per_batch, ptrs[0], ptrs[1], *mods,
-                          ptrs[2], ptrs[3], out8, strides[0], strides[1], mod_stride or 0, strides[2], strides[3])
-    check(lib.orch_op_block_norms(p, code, _stream_on(stream, *devices)))
+    if not -0x80000000 <= rows_per_batch <= 0x7fffffff:
+        _check_ints(rows_per_batch, 0)
+    p = _BLOCK_NORMS.pack(post.packed, pre.packed, residual_scale, rows, hidden, rows_per_batch, h.data_ptr(), ptr_y, *mods,
+                          ptr_ho, ptr_o, out8, st_h, st_y, mod_stride or 0, st_ho, st_o)
+    rc = lib.orch_op_block_norms(p, code, _stream_here(stream, h.get_device(), *others))
+    if rc:
+        check(rc)
+
+
+def _bad_rows(shape):
+    raise OrchError(ORCH_EINVAL, f"h, y, h_out and out must be {list(shape)}, h and h_out fp32, y and out of one type, channels next to each other")
 
 
 def quantize_rows(x, out: Int8Rows, stream=None):
     """Rows of x [rows, cols] (channels next to each other) to int8 with a scale each, see orch_op_quantize_rows."""
     rows, cols = x.shape
-    if out.shape != (rows, cols) or (cols > 1 and x.stride(1) != 1):
+    st, c = x.stride()
+    if out.shape != (rows, cols) or not (c == 1 or cols == 1):
         raise OrchError(ORCH_EINVAL, f"x must be {list(out.shape)}, as out, with channels next to each other")
     code = _code(x)
-    check(lib.orch_op_quantize_rows(x.data_ptr(), x.stride(0), rows, cols, out.ref, code,
-                                    _stream_on(stream, x.get_device(), *out.devices)))
+    rc = lib.orch_op_quantize_rows(x.data_ptr(), st, rows, cols, out.ref, code,
+                                   _stream_here(stream, x.get_device(), *out.devices))
+    if rc:
+        check(rc)
 
 
 def linear_quantized_workspace_bytes(M, N, K) -> int:
@@ -597,7 +645,7 @@ def _int8_operands(A, W, bias, workspace):
         raise OrchError(ORCH_EINVAL, f"A has {K} channels, W {k}")
     devices = A.devices + W.devices
     if bias is not None:
-        if _code(bias) != ORCH_F32 or bias.shape != (N,) or not bias.is_contiguous():
+        if bias.dtype is not _f32() or bias.shape != (N,) or not bias.is_contiguous():
             raise OrchError(ORCH_EINVAL, f"bias must be fp32 [{N}]")
         devices += (bias.get_device(),)
     ws_bytes = 0
@@ -622,14 +670,15 @@ def linear_quantized(A: Int8Rows, W: Int8Rows, bias, epilogue, out, gate=None, r
         if code != ORCH_F32:
             raise OrchError(ORCH_EINVAL, "the residual epilogue adds to fp32")
         need = -(-M // max(1, rows_per_batch))
-        if (gate is None or _code(gate) != ORCH_F32 or gate.dim() != 2 or gate.shape[0] < need or gate.shape[1] != N
+        if (gate is None or gate.dtype is not _f32() or gate.dim() != 2 or gate.shape[0] < need or gate.shape[1] != N
                 or (N > 1 and gate.stride(1) != 1)):
             raise OrchError(ORCH_EINVAL, f"the residual epilogue needs gate, fp32 [{need}, {N}]")
         devices += (gate.get_device(),)
         gate_stride = gate.stride(0)
-    check(lib.orch_op_linear_quantized(A.ref, M, K, W.ref, N, _ptr(bias), epilogue, _ptr(gate), gate_stride,
-                                  rows_per_batch, out.data_ptr(), _ptr(workspace), ws_bytes, code,
-                                  _stream_on(stream, *devices)))
+    rc = lib.orch_op_linear_quantized(A.ref, M, K, W.ref, N, _ptr(bias), epilogue, _ptr(gate), gate_stride, rows_per_batch,
+                                      out.data_ptr(), _ptr(workspace), ws_bytes, code, _stream_here(stream, *devices))
+    if rc:
+        check(rc)
 
 
 def qkv_projection_quantized(A: Int8Rows, W: Int8Rows, bias, q_out, kv_out, kv_tokens, tok_offset, workspace=None, stream=None):
@@ -646,9 +695,11 @@ def qkv_projection_quantized(A: Int8Rows, W: Int8Rows, bias, q_out, kv_out, kv_t
     kv_bs = kv_out.stride(0)
     _check_kv("kv_out", kv_out, code, kv_bs, kv_tokens, B, heads, d)
     devices += (q_out.get_device(), kv_out.get_device())
-    check(lib.orch_op_qkv_projection_quantized(A.ref, B, n_tok, K, W.ref, _ptr(bias), heads, d, q_out.data_ptr(),
-                                          kv_out.data_ptr(), kv_bs, kv_tokens, tok_offset, _ptr(workspace), ws_bytes, code,
-                                          _stream_on(stream, *devices)))
+    rc = lib.orch_op_qkv_projection_quantized(A.ref, B, n_tok, K, W.ref, _ptr(bias), heads, d, q_out.data_ptr(),
+                                              kv_out.data_ptr(), kv_bs, kv_tokens, tok_offset, _ptr(workspace), ws_bytes,
+                                              code, _stream_here(stream, *devices))
+    if rc:
+        check(rc)
 
 
 def unet_shape(cfg, eps: float = 1e-5) -> UNetConvShape:
