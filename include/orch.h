@@ -536,7 +536,8 @@ typedef struct {
 } orch_block_norms;
 
 /* One pass over memory, everything in fp32 (statistics of two passes over the row in
- * registers), one rounding to T.  out8: as orch_op_quantize_rows of u, which is not
+ * registers; squares of 1e19 and more are past its range, and such rows come out as 0 or NaN), one
+ * rounding to T.  out8: as orch_op_quantize_rows of u, which is not
  * rounded to T before.  h_out may be h and out may be y, with the same strides.  Any
  * element-aligned address and stride is taken; four channels an access where all
  * rows are aligned to it.  No rows are no error.  Errors: ORCH_EINVAL (kinds, eps, hidden
@@ -561,7 +562,7 @@ int orch_op_quantize_rows(const void* x, size_t x_stride, int rows, int cols,
  * workspace (16-byte aligned, one call's at a time): orch_linear_quantized_workspace_bytes()
  * bytes let products of few outputs split K over more workgroups; NULL or fewer bytes run
  * without.  Errors: ORCH_EINVAL (as orch_op_linear; K above 131071, where sums could pass 32 bits; 2^24
- * tiles of 256 x 128 outputs or more; alignment; out or workspace overlapping an input), ORCH_EHIP. */
+ * tiles of 64 x 64 outputs or more; alignment; out or workspace overlapping an input), ORCH_EHIP. */
 int orch_op_linear_quantized(const orch_int8_rows* A, int M, int K, const orch_int8_rows* W, int N,
                         const float* bias, int epilogue, const float* gate, size_t gate_stride,
                         int rows_per_batch, void* out, void* workspace, size_t workspace_bytes,

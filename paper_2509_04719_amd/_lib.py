@@ -689,11 +689,12 @@ def qkv_projection_quantized(A: Int8Rows, W: Int8Rows, bias, q_out, kv_out, kv_t
     code = _code(q_out)
     if B * n_tok != M or 3 * heads * d != N or not q_out.is_contiguous():
         raise OrchError(ORCH_EINVAL, f"q_out must be [B, heads, n_tok, d], contiguous, of {M} tokens and {N} / 3 channels")
-    if kv_out.dim() != 2 or kv_out.shape[0] != B:
-        raise OrchError(ORCH_EINVAL, f"kv_out must be [{B}, elements]")
+    if kv_out.dim() != 2 or kv_out.shape[0] != B or kv_out.dtype is not q_out.dtype:
+        raise OrchError(ORCH_EINVAL, f"kv_out must be [{B}, elements] of q_out's type")
     _check_ints(kv_tokens, tok_offset)
-    kv_bs = kv_out.stride(0)
-    _check_kv("kv_out", kv_out, code, kv_bs, kv_tokens, B, heads, d)
+    kv_bs, c = kv_out.stride()
+    if kv_out.shape[1] < 2 * kv_tokens * heads * d or c != 1:
+        raise OrchError(ORCH_EINVAL, f"kv_out must hold {2 * kv_tokens * heads * d} elements a branch, next to each other")
     devices += (q_out.get_device(), kv_out.get_device())
     rc = lib.orch_op_qkv_projection_quantized(A.ref, B, n_tok, K, W.ref, _ptr(bias), heads, d, q_out.data_ptr(),
                                               kv_out.data_ptr(), kv_bs, kv_tokens, tok_offset, _ptr(workspace), ws_bytes,

@@ -590,9 +590,10 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) koff[kk] = ((2 * kk + h) ^ ((lr >> 1) & 7)) * 16;
   const int arow = (wm * (BM / 2) + lr) * BK, brow = BM * BK + (wn * 64 + lr) * BK;
-  // the MFMAs of stage st: MFMA e of k-step kk, then its share of the next k-step's fragments
+  // the MFMAs of stage st (FIRST: of a tile's first k-tile, on sums of 0): MFMA e of k-step kk, then its share of the next k-step's fragments
   // and, in the first k-step, of the loads into the other stage
-  auto compute = [&](auto vt, int st) __attribute__((always_inline)) {
+  auto compute = [&](auto vt, auto first_c, int st) __attribute__((always_inline)) {
+    const i32x16 zero = {};
     const char* base = smem + st * STAGE;
     i32x4 a[2][FM], b[2][2];
 #pragma unroll
@@ -604,7 +605,7 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
       constexpr int kk = decltype(kkc)::value, cur = kk & 1, NM = 2 * FM, nd = kk + 1 < KK ? FM + 2 : 0;
       static_for<0, NM>([&](auto ec) __attribute__((always_inline)) {
         constexpr int e = decltype(ec)::value, i = e / 2, j = e % 2;
-        acc[i][j] = mfma<decltype(vt)::value>(a[cur][i], b[cur][j], acc[i][j]);
+        acc[i][j] = mfma<decltype(vt)::value>(a[cur][i], b[cur][j], decltype(first_c)::value && kk == 0 ? zero : acc[i][j]);
         static_for<e * nd / NM, (e + 1) * nd / NM>([&](auto dc) __attribute__((always_inline)) {
           constexpr int d = decltype(dc)::value;
           if constexpr (d < FM) a[cur ^ 1][d] = *reinterpret_cast<const i32x4*>(base + arow + d * 32 * BK + koff[kk + 1]);
@@ -623,20 +624,17 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
   for (int ct = blockIdx.x; ct < tiles; ct += gridDim.x) {
     const TileAt ta(tiles_m, tiles_n, ct);
     const int m0 = ta.m * BM + wm * (BM / 2), n0 = ta.n * BN + wn * 64;
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
     auto tile = [&](auto vt) __attribute__((always_inline)) {
-      for (int kt = 0; kt < KT; ++kt) {
+      auto step = [&](auto first) __attribute__((always_inline)) {
         wait_vmcnt<0>();
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): a missing bias' zeros too
         lds_barrier();
         next();
-        compute(vt, st);
+        compute(vt, first, st);
         st ^= 1;
-      }
+      };
+      step(std::true_type{});
+      for (int kt = 1; kt < KT; ++kt) step(std::false_type{});
       const Side<BM, BN>& sd = sides[side];
       staged<T, EPI, decltype(vt)::value>(p, acc, smem + G::AREAS + wave * kArea, sd.sa + wm * (BM / 2), sd.sw + wn * 64,
                                           sd.bias + wn * 64, lane, m0, n0);

@@ -90,7 +90,7 @@ int check_product(const orch_int8_rows* A, int M, int K, const orch_int8_rows* W
                   size_t workspace_bytes, int dtype, GemmI8Params* p, Rows (&in)[6], Rows* ws) {
   if (int rc = check_type(dtype)) return rc;
   if (M < 0 || N < 1 || K < 1 || K > kMaxCols) return fail("bad shape: M >= 0, N >= 1, K of 1 .. %d", kMaxCols);
-  if (((long long)M / 256 + 1) * ((long long)N / 128 + 1) >= 1ll << 24) return fail("bad shape: M * N too large");
+  if (((long long)M / 64 + 1) * ((long long)N / 64 + 1) >= 1ll << 24) return fail("bad shape: M * N too large");
   if (M == 0) return ORCH_OK;
   if (int rc = check_int8(A, "A", M, K, &in[0], &in[1], &p->lda)) return rc;
   if (int rc = check_int8(W, "W", N, K, &in[2], &in[3], &p->ldw)) return rc;
@@ -212,7 +212,7 @@ int orch_op_quantize_rows(const void* x, size_t x_stride, int rows, int cols, co
 }
 
 size_t orch_linear_quantized_workspace_bytes(int M, int N, int K) {
-  if (M < 1 || N < 1 || K < 1 || K > kMaxCols || ((long long)M / 256 + 1) * ((long long)N / 128 + 1) >= 1ll << 24) return 0;
+  if (M < 1 || N < 1 || K < 1 || K > kMaxCols || ((long long)M / 64 + 1) * ((long long)N / 64 + 1) >= 1ll << 24) return 0;
   return gemm_int8_workspace_bytes(M, N, K);
 }
 

@@ -163,7 +163,7 @@ def _linear(lib, A=(P[0], P[1], 48), M=5, K=40, W=(P[2], P[3], 64), N=24, bias=P
 
 @pytest.mark.parametrize("kw,word", [
     (dict(dtype=-1), "dtype"), (dict(epi=3), "epilogue"), (dict(M=-1), "shape"), (dict(N=0), "shape"), (dict(K=0), "shape"),
-    (dict(K=131072), "shape"), (dict(M=1 << 30, N=1 << 20), "too large"), (dict(A=None), "NULL"), (dict(W=None), "NULL"),
+    (dict(K=131072), "shape"), (dict(M=1 << 30, N=1 << 20), "too large"), (dict(M=(1 << 30) - 64, N=1), "too large"), (dict(A=None), "NULL"), (dict(W=None), "NULL"),
     (dict(A=(None, P[1], 48)), "NULL"), (dict(W=(P[2], None, 64)), "NULL"), (dict(A=(P[0] + 8, P[1], 48)), "16-byte"),
     (dict(A=(P[0], P[1], 32)), "multiple of 16"), (dict(W=(P[2], P[3], 56)), "multiple of 16"),
     (dict(W=(P[2], P[3], 1 << 23)), "2^23"), (dict(bias=P[4] + 2), "bias"), (dict(out=None), "NULL"),
