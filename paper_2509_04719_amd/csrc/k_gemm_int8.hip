@@ -128,7 +128,7 @@ struct Block {
 
   // 16 bytes of outputs from (m, n) on: channels (Vt: tokens) next to each other.  Rows of
   // `out` take 16-byte accesses (p.wide).  held: the same in LDS, where they are.
-  __device__ __forceinline__ void sink(const uint4& v, const T* held, int m, int n) const {
+  __device__ __forceinline__ void sink(const uint4& v, const char* held, int m, int n) const {
     constexpr int CE = 16 / sizeof(T);
     if (m >= p.M || n >= p.N) return;
     if constexpr (EPI == kEpiResidual) {
@@ -148,7 +148,7 @@ struct Block {
         *reinterpret_cast<uint4*>(d) = v;
       } else if (held) {
 #pragma unroll 1
-        for (int f = 0; f < CE; ++f) one(held[f], Vt ? m + f : m, Vt ? n : n + f);
+        for (int f = 0; f < CE; ++f) one(held_one(held, f), Vt ? m + f : m, Vt ? n : n + f);
       } else {
         typedef T W __attribute__((ext_vector_type(CE)));
         const W w = __builtin_bit_cast(W, v);
@@ -158,6 +158,19 @@ struct Block {
     } else {
       *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + (size_t)m * p.N + n) = v;
     }
+  }
+  // element i of what is held in LDS (written there as 16-byte words)
+  __device__ __forceinline__ static T held_one(const char* p, int i) {
+    T x;
+    __builtin_memcpy(&x, p + i * (int)sizeof(T), sizeof(T));
+    return x;
+  }
+  // one output where rows of out take no 16-byte accesses
+  __device__ __forceinline__ void element(T x, int m, int n) const {
+    if (m >= p.M || n >= p.N) return;
+    T* d = reinterpret_cast<T*>(p.out) + (size_t)m * p.N + n;
+    if constexpr (EPI == kEpiResidual) *d = fmaf(p.gate[branch(p, m) * p.gate_stride + n], x, *d);
+    else *d = x;
   }
   __device__ __forceinline__ void one(T x, int m, int n) const {
     const int b = branch(p, m);
@@ -190,14 +203,7 @@ struct Block {
 #pragma unroll
         for (int g = 0; g < 4; ++g)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int m = m0 + lr, n = n0 + 8 * g + 4 * h + r;
-            if (m < p.M && n < p.N) {
-              T* d = reinterpret_cast<T*>(p.out) + (size_t)m * p.N + n;
-              if constexpr (EPI == kEpiResidual) *d = fmaf(p.gate[branch(p, m) * p.gate_stride + n], y[g][r], *d);
-              else *d = from_f<T>(y[g][r]);
-            }
-          }
+          for (int r = 0; r < 4; ++r) element(from_f<T>(y[g][r]), m0 + lr, n0 + 8 * g + 4 * h + r);
       } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -252,29 +258,30 @@ __device__ __forceinline__ void staged(const GemmI8Params& p, const i32x16 (&acc
   // blocks side by side along the stored rows: two in bf16, one in fp32
   constexpr int SB = sizeof(T) == 2 ? 2 : 1, CE = 16 / sizeof(T);
   constexpr int O = Vt ? FN : FM, I = Vt ? FM : FN;       // blocks across and along the stored rows
-  typename B::Cols c[Vt ? 1 : FN];
-  if constexpr (!Vt) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) blk.cols(c[j], sw + 32 * j, bias + 32 * j);
-  }
+  for (int i0 = 0; i0 < I; i0 += SB) {
+    const int along = (Vt ? m : n) + 32 * i0;
+    if (along >= (Vt ? p.M : p.N)) break;
+    typename B::Cols c[Vt ? 1 : SB];
+    if constexpr (!Vt) {
 #pragma unroll
-  for (int o = 0; o < O; ++o) {
-    if ((Vt ? n : m) + 32 * o >= (Vt ? p.N : p.M)) break;
-    if constexpr (Vt) blk.cols(c[0], sw + 32 * o, bias + 32 * o);
+      for (int k = 0; k < SB; ++k)
+        if (i0 + k < I) blk.cols(c[k], sw + 32 * (i0 + k), bias + 32 * (i0 + k));
+    }
 #pragma unroll
-    for (int i0 = 0; i0 < I; i0 += SB) {
-      const int along = (Vt ? m : n) + 32 * i0;
-      if (along >= (Vt ? p.M : p.N)) break;
+    for (int o = 0; o < O; ++o) {
+      if ((Vt ? n : m) + 32 * o >= (Vt ? p.N : p.M)) break;
+      if constexpr (Vt) blk.cols(c[0], sw + 32 * o, bias + 32 * o);
       // (this turn's addresses from this turn's copy: hoisted ones would not fit the registers)
       int at = lane;
-      if constexpr (EPI == kEpiQkv) asm volatile("" : "+v"(at));
+      asm volatile("" : "+v"(at));
       const int nb = i0 + SB <= I ? SB : 1, ch8 = sizeof(T) == 2 ? 4 * nb : 8;    // (a last block of its own: half lines)
       uint4 v[4];     // chunk 4 k + 2 h + e of block k in bf16, 2 g + h in fp32
 #pragma unroll
       for (int k = 0; k < nb; ++k) {
         float y[4][4];
         if constexpr (Vt) blk.values(y, acc[i0 + k][o], c[0], sa + 32 * (i0 + k));
-        else blk.values(y, acc[o][i0 + k], c[i0 + k], sa + 32 * o);
+        else blk.values(y, acc[o][i0 + k], c[Vt ? 0 : k], sa + 32 * o);
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) v[2 * k + e] = B::join(B::pack(y[e]), B::pack(y[e + 2]));
@@ -291,15 +298,23 @@ __device__ __forceinline__ void staged(const GemmI8Params& p, const i32x16 (&acc
             *reinterpret_cast<uint4*>(area + (lr & 15) * kLine +
                                       (sizeof(T) == 2 ? 4 * (x >> 1) + 2 * h + (x & 1) : 2 * x + h) * 16) = v[x];
         }
+        const int across = (Vt ? n : m) + 32 * o + 16 * pass;
+        if (EPI == kEpiQkv || p.wide) {
 #pragma unroll
-        for (int q = 0; q < ch8 / 4; ++q) {
-          const int row = q * 8 + at / ch8, ch = at % ch8;
-          const char* held = area + row * kLine + ch * 16;
-          const uint4 w = *reinterpret_cast<const uint4*>(held);
-          const T* el = reinterpret_cast<const T*>(held);
-          const int across = (Vt ? n : m) + 32 * o + 16 * pass + row;
-          if constexpr (Vt) blk.sink(w, el, along + CE * ch, across);
-          else blk.sink(w, el, across, along + CE * ch);
+          for (int q = 0; q < ch8 / 4; ++q) {
+            const int row = q * 8 + at / ch8, ch = at % ch8;
+            const char* held = area + row * kLine + ch * 16;
+            const uint4 w = *reinterpret_cast<const uint4*>(held);
+            if constexpr (Vt) blk.sink(w, held, along + CE * ch, across + row);
+            else blk.sink(w, held, across + row, along + CE * ch);
+          }
+        } else {        // (rows of out that 16 bytes do not fit: an element a lane)
+          const int per = ch8 * CE;
+#pragma unroll 2
+          for (int q = 0; q < per / 4; ++q) {
+            const int row = q * (64 / per) + at / per, c = at % per;
+            blk.element(B::held_one(area + row * kLine, c), across + row, along + c);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -494,10 +509,7 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
     __syncthreads();    // (the areas take the ring's place; the side's values are there)
     const int mw = wm * G::TM, nw = wn * G::TN;
     const float *sa = side.sa + mw, *sw = side.sw + nw, *bias = side.bias + nw;
-    if (EPI == kEpiQkv || p.wide)
-      staged<T, EPI, decltype(vt)::value>(p, acc, smem + wave * kArea, sa, sw, bias, lane, m0 + mw, n0 + nw);
-    else
-      direct<T, EPI, decltype(vt)::value>(p, acc, sa, sw, bias, lane, m0 + mw, n0 + nw, 0);
+    staged<T, EPI, decltype(vt)::value>(p, acc, smem + wave * kArea, sa, sw, bias, lane, m0 + mw, n0 + nw);
   };
   // (a wave's own choice: both loops meet the same barriers)
   if (all_vt<EPI>(p, n0 + wn * G::TN)) loop(Yes{});
@@ -511,7 +523,7 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
 // tiles are one sequence: one barrier a k-tile, the next one's loads between the MFMAs, and
 // behind a tile's last come the next one's first, whose loads are in flight while the
 // outputs are written.  Behind the last tile the buffers of the loads are empty, so that they
-// fetch nothing.  Needs K % 16 == 0 and rows of out that take 16-byte accesses.
+// fetch nothing.
 template <int BM>
 struct BigGeo {
   static constexpr int BN = 256, BK = 128, KK = 4, STAGE = (BM + BN) * BK;
@@ -533,11 +545,9 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
   Side<BM, BN>* sides = reinterpret_cast<Side<BM, BN>*>(smem + G::SIDES);
 
   // The loads' place in the sequence: k-tile lk of tile lt.  Load j fills tile rows (8 j + wave)
-  // 8 .. + 8, A's first, then W's; chunk c of row r lies at c ^ (r / 2 % 8).  A's chunks past
-  // K, in a tile's last k-tile, are loaded from past the buffer, which gives 0.
+  // 8 .. + 8, A's first, then W's; chunk c of row r lies at c ^ (r / 2 % 8).
   int lt = blockIdx.x, lk = 0, lside = 0;
   const int lrow = wave * 8 + (lane >> 3), chunk = (lane & 7) ^ ((lrow >> 1) & 7);
-  const unsigned past = ((KT - 1) * 8 + chunk) * 16 < p.K ? 0u : 0x80000000u;
   unsigned off[LPT];
   __amdgpu_buffer_rsrc_t rA, rW;
   auto place = [&]() __attribute__((always_inline)) {
@@ -573,8 +583,8 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
   auto load = [&](auto jc, int st) __attribute__((always_inline)) {
     constexpr int j = decltype(jc)::value;
     char* dst = smem + st * STAGE + (j * 8 + wave) * 1024;     // (W's rows follow A's)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(j < IA ? rA : rW, (ORCH_LDS void*)dst, 16,
-                                             j < IA ? off[j] | (lk == KT - 1 ? past : 0u) : off[j], (unsigned)lk * BK, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(j < IA ? rA : rW, (ORCH_LDS void*)dst, 16, off[j],
+                                             (unsigned)lk * BK, 0, 0);
   };
   auto next = [&]() __attribute__((always_inline)) {
     if (++lk == KT) {
@@ -590,9 +600,10 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) koff[kk] = ((2 * kk + h) ^ ((lr >> 1) & 7)) * 16;
   const int arow = (wm * (BM / 2) + lr) * BK, brow = BM * BK + (wn * 64 + lr) * BK;
-  // the MFMAs of stage st (FIRST: of a tile's first k-tile, on sums of 0): MFMA e of k-step kk, then its share of the next k-step's fragments
+  const int left = p.K - (KT - 1) * BK;     // bytes of k in a tile's last k-tile
+  // the MFMAs of stage st (first: a tile's first k-tile, on sums of 0; last: what lies past K cleared): MFMA e of k-step kk, then its share of the next k-step's fragments
   // and, in the first k-step, of the loads into the other stage
-  auto compute = [&](auto vt, auto first_c, int st) __attribute__((always_inline)) {
+  auto compute = [&](auto vt, auto first_c, auto last_c, int st) __attribute__((always_inline)) {
     const i32x16 zero = {};
     const char* base = smem + st * STAGE;
     i32x4 a[2][FM], b[2][2];
@@ -603,6 +614,13 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
     __builtin_amdgcn_sched_barrier(0);
     static_for<0, KK>([&](auto kkc) __attribute__((always_inline)) {
       constexpr int kk = decltype(kkc)::value, cur = kk & 1, NM = 2 * FM, nd = kk + 1 < KK ? FM + 2 : 0;
+      if constexpr (decltype(last_c)::value) {
+        if (left < BK) {
+          const i32x4 m = within(left, 2 * kk + h);
+#pragma unroll
+          for (int i = 0; i < FM; ++i) a[cur][i] &= m;
+        }
+      }
       static_for<0, NM>([&](auto ec) __attribute__((always_inline)) {
         constexpr int e = decltype(ec)::value, i = e / 2, j = e % 2;
         acc[i][j] = mfma<decltype(vt)::value>(a[cur][i], b[cur][j], decltype(first_c)::value && kk == 0 ? zero : acc[i][j]);
@@ -625,16 +643,23 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
     const TileAt ta(tiles_m, tiles_n, ct);
     const int m0 = ta.m * BM + wm * (BM / 2), n0 = ta.n * BN + wn * 64;
     auto tile = [&](auto vt) __attribute__((always_inline)) {
-      auto step = [&](auto first) __attribute__((always_inline)) {
+      auto step = [&](auto first, auto last) __attribute__((always_inline)) {
         wait_vmcnt<0>();
         __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): a missing bias' zeros too
         lds_barrier();
         next();
-        compute(vt, first, st);
+        compute(vt, first, last, st);
         st ^= 1;
       };
-      step(std::true_type{});
-      for (int kt = 1; kt < KT; ++kt) step(std::false_type{});
+      using Yes = std::true_type;
+      using No = std::false_type;
+      if (KT == 1) {
+        step(Yes{}, Yes{});
+      } else {
+        step(Yes{}, No{});
+        for (int kt = 2; kt < KT; ++kt) step(No{}, No{});
+        step(No{}, Yes{});
+      }
       const Side<BM, BN>& sd = sides[side];
       staged<T, EPI, decltype(vt)::value>(p, acc, smem + G::AREAS + wave * kArea, sd.sa + wm * (BM / 2), sd.sw + wn * 64,
                                           sd.bias + wn * 64, lane, m0, n0);
@@ -880,10 +905,9 @@ static void launch_form(int f, const GemmI8Params& p, hipStream_t s) {
 // one's outputs are written beside another's products.
 struct Plan { int form, splits; };
 
-static Plan pick(int M, int N, int K, bool wide, size_t ws_elems) {
-  const bool big_ok = wide && K % 16 == 0;
+static Plan pick(int M, int N, int K, size_t ws_elems) {
   const int f = forced(), kt = ceil_div(K, 128);
-  if (f >= 0 && f < kForms && (f > k192x256 || big_ok)) return {f, 1};
+  if (f >= 0 && f < kForms) return {f, 1};
   float best = 0.0f;
   int form = -1;
   auto tiles = [&](int bm, int bn) { return (float)ceil_div(M, bm) * ceil_div(N, bn); };
@@ -892,10 +916,8 @@ static Plan pick(int M, int N, int K, bool wide, size_t ws_elems) {
     if (form < 0 || us < best) form = c, best = us;
   };
   const float k = (float)kt, t128 = tiles(128, 128), t64 = tiles(64, 64), t3264 = tiles(32, 64), t32 = tiles(32, 32);
-  if (big_ok) {
-    take(k256x256, 2.5f + rounds(tiles(256, 256)) * (8.0f + 1.4f * k));
-    take(k192x256, 2.5f + rounds(tiles(192, 256)) * (6.5f + 1.1f * k));
-  }
+  take(k256x256, 2.5f + rounds(tiles(256, 256)) * (8.0f + 1.4f * k));
+  take(k192x256, 2.5f + rounds(tiles(192, 256)) * (6.5f + 1.1f * k));
   take(k128x128, t128 <= 256 ? 5.5f + 0.65f * k : 3.0f + t128 / 512 * (4.0f + k));
   take(k128x128Alone, 4.0f + rounds(t128) * (2.5f + 0.3f * k) + t128 / 256 * (2.5f + 0.22f * k));
   take(k64x64, t64 <= 256 ? 3.5f + 0.2f * k : 3.0f + t64 / 512 * (1.0f + 0.45f * k));
@@ -924,7 +946,7 @@ static hipError_t launch_t(const GemmI8Params& p0, hipStream_t s) {
     p.rpb_shift = 31 + l;
     p.rpb_inverse = (unsigned)(((1ull << p.rpb_shift) + p.rows_per_batch - 1) / p.rows_per_batch);
   }
-  const Plan pl = pick(p.M, p.N, p.K, EPI == kEpiQkv || p.wide, p.ws ? p.ws_elems : 0);
+  const Plan pl = pick(p.M, p.N, p.K, p.ws ? p.ws_elems : 0);
   p.splits = pl.splits;
   if (pl.splits > 1) {
     launch_small<32, 32, 4, 3, T, kEpiPartial>(p, s);
@@ -950,7 +972,7 @@ static hipError_t launch_epi(const GemmI8Params& p, int epi, hipStream_t s) {
 }  // namespace i8
 
 size_t gemm_int8_workspace_bytes(int M, int N, int K) {
-  const i8::Plan pl = i8::pick(M, N, K, true, (size_t)-1);
+  const i8::Plan pl = i8::pick(M, N, K, (size_t)-1);
   return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0;
 }
 

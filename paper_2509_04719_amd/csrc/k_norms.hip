@@ -46,8 +46,10 @@ struct Group {
     v = f(v, dpp<0x141>(v));   // 7 - lane of 8
     v = f(v, dpp<0x140>(v));   // 15 - lane of 16
 #if defined(__HIP_DEVICE_COMPILE__)
-    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    v = f(r[0], r[1]);
+    if constexpr (LPR > 16) {
+      const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+      v = f(r[0], r[1]);
+    }
     if constexpr (LPR > 32) {
       const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
       v = f(s[0], s[1]);
@@ -69,34 +71,39 @@ struct Group {
   __device__ __forceinline__ unsigned top(unsigned v) { return all(v, Max{}); }
 };
 
-// V elements as they are held, and as fp32
-template <typename T, int V>
+// V elements as they are held (anywhere that suits one of them), and as fp32
+template <typename T, int V, bool Ragged>
 struct Raw {
-  typedef T W __attribute__((ext_vector_type(V)));
+  typedef T W __attribute__((ext_vector_type(V), aligned(Ragged ? sizeof(T) : V * sizeof(T))));
   W w;
   __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const W*>(p); }
   __device__ __forceinline__ float operator[](int e) const { return to_f<T>(w[e]); }
 };
-template <typename T>
-struct Raw<T, 1> {
+template <typename T, bool Ragged>
+struct Raw<T, 1, Ragged> {
   T w;
   __device__ __forceinline__ void load(const T* p) { w = *p; }
   __device__ __forceinline__ float operator[](int) const { return to_f<T>(w); }
 };
 
-// A lane's share of a row of n channels: V of them from (lane + LPR i) V on, i < NV.  Loads
-// past the row read its first channels instead (a branch each would wait for each).
-template <int V, int NV, int LPR>
+// A lane's share of a row of n >= V channels: V of them from (lane + LPR i) V on, i < NV.  Ragged
+// rows end anywhere and lie anywhere: the chunk that would pass the end begins at n - V, and its
+// first elements, which are the chunk's before, stay out of everything (a branch for each load
+// would wait for each).  Chunks past the row read its first channels.
+template <int V, int NV, int LPR, bool Ragged>
 struct Share {
   int lane, n;
-  __device__ __forceinline__ int at(int i) const { return (lane + LPR * i) * V; }
-  __device__ __forceinline__ bool in(int i) const { return at(i) < n; }
-  template <typename T>
-  __device__ __forceinline__ void load(Raw<T, V> (&r)[NV], const T* row) const {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) r[i].load(row + (in(i) ? at(i) : 0));
+  __device__ __forceinline__ int nominal(int i) const { return (lane + LPR * i) * V; }
+  __device__ __forceinline__ int at(int i) const { return Ragged ? min(nominal(i), n - V) : nominal(i) < n ? nominal(i) : 0; }
+  __device__ __forceinline__ bool in(int i, int e) const {
+    return nominal(i) < n && (!Ragged || e >= nominal(i) + V - n);
   }
-  // f(i, e, in the row) of every element
+  template <typename T>
+  __device__ __forceinline__ void load(Raw<T, V, Ragged> (&r)[NV], const T* row) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) r[i].load(row + at(i));
+  }
+  // f(i, e) of every element
   template <typename F>
   __device__ __forceinline__ static void each(F f) {
 #pragma unroll
@@ -104,11 +111,25 @@ struct Share {
 #pragma unroll
       for (int e = 0; e < V; ++e) f(i, e);
   }
+  // whole(i) for chunks within the row, one(i, e) for what a last shorter one holds
+  template <typename F, typename G>
+  __device__ __forceinline__ void put(F whole, G one) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (Ragged ? nominal(i) + V <= n : nominal(i) < n) {
+        whole(i);
+      } else if (Ragged && nominal(i) < n) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (in(i, e)) one(i, e);
+      }
+    }
+  }
 };
 
-template <typename T, int V>
+template <typename T, int V, bool Ragged>
 __device__ __forceinline__ void store(T* p, const float* x) {
-  typedef T W __attribute__((ext_vector_type(V)));
+  typedef T W __attribute__((ext_vector_type(V), aligned(Ragged ? sizeof(T) : V * sizeof(T))));
   if constexpr (V == 1) {
     *p = from_f<T>(x[0]);
   } else {
@@ -152,18 +173,18 @@ struct Codes {
 
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-// x of a row -> its norm times weight plus bias (32 bits); what lies past the row comes
-// in as 0 and stays out of the sums
-template <int V, int NV, int LPR>
-__device__ __forceinline__ void norm(float (&x)[NV][V], const Share<V, NV, LPR>& sh, const Norm& n, Group<LPR>& g) {
-  using S = Share<V, NV, LPR>;
+// x of a row -> its norm times weight plus bias (32 bits); what is not in the share
+// comes in as 0 and stays out of the sums
+template <int V, int NV, int LPR, bool Ragged>
+__device__ __forceinline__ void norm(float (&x)[NV][V], const Share<V, NV, LPR, Ragged>& sh, const Norm& n, Group<LPR>& g) {
+  using S = Share<V, NV, LPR, Ragged>;
   if (n.kind != kNormNone) {
     const float inv = 1.0f / (float)sh.n;
     if (n.kind == kNormLayer) {
       float s = 0.0f;
       S::each([&](int i, int e) __attribute__((always_inline)) { s += x[i][e]; });
       const float mean = g.sum(s) * inv;
-      S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] = sh.in(i) ? x[i][e] - mean : 0.0f; });
+      S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] = sh.in(i, e) ? x[i][e] - mean : 0.0f; });
     }
     float s = 0.0f;
     S::each([&](int i, int e) __attribute__((always_inline)) { s = fmaf(x[i][e], x[i][e], s); });
@@ -171,21 +192,21 @@ __device__ __forceinline__ void norm(float (&x)[NV][V], const Share<V, NV, LPR>&
     S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] *= rstd; });
   }
   if (n.weight) {
-    Raw<float, V> w[NV];
+    Raw<float, V, Ragged> w[NV];
     sh.load(w, n.weight);
     S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] *= w[i][e]; });
   }
   if (n.bias) {
-    Raw<float, V> w[NV];
+    Raw<float, V, Ragged> w[NV];
     sh.load(w, n.bias);
     S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] += w[i][e]; });
   }
 }
 
-template <typename T, int V, int LPR, int NV>
+template <typename T, int V, int LPR, int NV, bool Ragged>
 __global__ __launch_bounds__(LPR > kThreads ? LPR : kThreads) void block_norms_kernel(BlockNormsParams p) {
   constexpr int RPB = LPR > kThreads ? 1 : kThreads / LPR;    // rows of a workgroup
-  using S = Share<V, NV, LPR>;
+  using S = Share<V, NV, LPR, Ragged>;
   __shared__ unsigned red[LPR > 64 ? 2 * LPR / 64 : 1];
   const int row = blockIdx.x * RPB + threadIdx.x / LPR;
   if (row >= p.rows) return;    // (the whole group of lanes; a group of several waves is a whole workgroup)
@@ -194,8 +215,8 @@ __global__ __launch_bounds__(LPR > kThreads ? LPR : kThreads) void block_norms_k
   const size_t b = row / p.rows_per_batch * p.mod_stride;
   // every load first, as far as the registers hold them
   constexpr bool EARLY = NV * V <= 24;
-  Raw<float, V> h[NV], gate[NV], shift[NV], scale[NV];
-  Raw<T, V> y[NV];
+  Raw<float, V, Ragged> h[NV], gate[NV], shift[NV], scale[NV];
+  Raw<T, V, Ragged> y[NV];
   if (EARLY || !p.y) sh.load(h, p.h + row * p.h_stride);
   if (p.y) sh.load(y, reinterpret_cast<const T*>(p.y) + row * p.y_stride);
   if (EARLY && p.gate) sh.load(gate, p.gate + b);
@@ -204,8 +225,8 @@ __global__ __launch_bounds__(LPR > kThreads ? LPR : kThreads) void block_norms_k
   float x[NV][V];
   if (p.y) {
     float z[NV][V];
-    S::each([&](int i, int e) __attribute__((always_inline)) { z[i][e] = sh.in(i) ? y[i][e] : 0.0f; });
-    norm<V, NV, LPR>(z, sh, p.post, g);
+    S::each([&](int i, int e) __attribute__((always_inline)) { z[i][e] = sh.in(i, e) ? y[i][e] : 0.0f; });
+    norm<V, NV, LPR, Ragged>(z, sh, p.post, g);
     if (!EARLY && p.gate) sh.load(gate, p.gate + b);
     if (p.gate) S::each([&](int i, int e) __attribute__((always_inline)) { z[i][e] *= gate[i][e]; });
     if (!EARLY) sh.load(h, p.h + row * p.h_stride);
@@ -215,36 +236,33 @@ __global__ __launch_bounds__(LPR > kThreads ? LPR : kThreads) void block_norms_k
   }
   if (p.h_out) {
     float* o = p.h_out + row * p.h_out_stride;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (sh.in(i)) store<float, V>(o + sh.at(i), x[i]);
+    sh.put([&](int i) __attribute__((always_inline)) { store<float, V, Ragged>(o + sh.at(i), x[i]); },
+           [&](int i, int e) __attribute__((always_inline)) { o[sh.at(i) + e] = x[i][e]; });
   }
   if (!p.out && !p.codes) return;
-  S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] = sh.in(i) ? x[i][e] : 0.0f; });
-  norm<V, NV, LPR>(x, sh, p.pre, g);
+  S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] = sh.in(i, e) ? x[i][e] : 0.0f; });
+  norm<V, NV, LPR, Ragged>(x, sh, p.pre, g);
   if (!EARLY && p.scale) sh.load(scale, p.scale + b);
   if (p.scale) S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] *= 1.0f + scale[i][e]; });
   if (!EARLY && p.shift) sh.load(shift, p.shift + b);
   if (p.shift) S::each([&](int i, int e) __attribute__((always_inline)) { x[i][e] += shift[i][e]; });
   if (p.out) {
     T* o = reinterpret_cast<T*>(p.out) + row * p.out_stride;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (sh.in(i)) store<T, V>(o + sh.at(i), x[i]);
+    sh.put([&](int i) __attribute__((always_inline)) { store<T, V, Ragged>(o + sh.at(i), x[i]); },
+           [&](int i, int e) __attribute__((always_inline)) { o[sh.at(i) + e] = from_f<T>(x[i][e]); });
   }
   if (!p.codes) return;
   unsigned top = 0;
-  S::each([&](int i, int e) __attribute__((always_inline)) { top = max(top, sh.in(i) ? magnitude(x[i][e]) : 0u); });
+  S::each([&](int i, int e) __attribute__((always_inline)) { top = max(top, sh.in(i, e) ? magnitude(x[i][e]) : 0u); });
   const Codes q(g.top(top));
   signed char* o = p.codes + row * p.codes_stride;
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (sh.in(i)) q.put<V>(o + sh.at(i), x[i]);
+  sh.put([&](int i) __attribute__((always_inline)) { q.put<V>(o + sh.at(i), x[i]); },
+         [&](int i, int e) __attribute__((always_inline)) { o[sh.at(i) + e] = (signed char)q.code(x[i][e]); });
   if (sh.lane == 0) p.code_scales[row] = q.scale;
 }
 
 // Rows to codes.  NV 0: rows too long for the registers, read twice.
-template <typename T, int V, int LPR, int NV>
+template <typename T, int V, int LPR, int NV, bool Ragged>
 __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const T* __restrict__ x, size_t x_stride, int rows, int cols,
                                                                  signed char* __restrict__ codes, size_t codes_stride,
                                                                  float* __restrict__ scales) {
@@ -255,38 +273,38 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const T* __rest
   Group<LPR> g{red};
   const T* xr = x + row * x_stride;
   signed char* cr = codes + row * codes_stride;
+  // (repeated elements do not change the largest)
+  constexpr int C = NV > 0 ? NV : 4;
+  using S = Share<V, C, LPR, Ragged>;
   unsigned top = 0;
-  if constexpr (NV > 0) {
-    const Share<V, NV, LPR> sh{lane, cols};
-    Raw<T, V> v[NV];
+  auto largest = [&](Raw<T, V, Ragged> (&v)[C], const S& sh) __attribute__((always_inline)) {
     sh.load(v, xr);
-    // (what repeats the row's first elements does not change its largest)
-    sh.each([&](int i, int e) __attribute__((always_inline)) { top = max(top, magnitude(v[i][e])); });
+    S::each([&](int i, int e) __attribute__((always_inline)) { top = max(top, magnitude(v[i][e])); });
+  };
+  auto write = [&](Raw<T, V, Ragged> (&v)[C], const S& sh, const Codes& q) __attribute__((always_inline)) {
+    sh.put(
+        [&](int i) __attribute__((always_inline)) {
+          float f[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) f[e] = v[i][e];
+          q.put<V>(cr + sh.at(i), f);
+        },
+        [&](int i, int e) __attribute__((always_inline)) { cr[sh.at(i) + e] = (signed char)q.code(v[i][e]); });
+  };
+  Raw<T, V, Ragged> v[C];
+  if constexpr (NV > 0) {
+    const S sh{lane, cols};
+    largest(v, sh);
     const Codes q(g.top(top));
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float f[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) f[e] = v[i][e];
-      if (sh.in(i)) q.put<V>(cr + sh.at(i), f);
-    }
+    write(v, sh, q);
     if (lane == 0) scales[row] = q.scale;
   } else {
-    Raw<T, V> v;
-#pragma unroll 4
-    for (int c = lane * V; c < cols; c += LPR * V) {
-      v.load(xr + c);
-#pragma unroll
-      for (int e = 0; e < V; ++e) top = max(top, magnitude(v[e]));
-    }
+    for (int l = lane; l * V < cols; l += LPR * C) largest(v, S{l, cols});
     const Codes q(g.top(top));
-#pragma unroll 4
-    for (int c = lane * V; c < cols; c += LPR * V) {
-      v.load(xr + c);
-      float f[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) f[e] = v[e];
-      q.put<V>(cr + c, f);
+    for (int l = lane; l * V < cols; l += LPR * C) {
+      const S sh{l, cols};
+      sh.load(v, xr);
+      write(v, sh, q);
     }
     if (lane == 0) scales[row] = q.scale;
   }
@@ -294,54 +312,61 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const T* __rest
 
 static bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
-template <typename T, int V, int LPR, int NV>
+template <typename T, int V, int LPR, int NV, bool Ragged>
 static void launch_norms(const BlockNormsParams& p, hipStream_t s) {
   constexpr int threads = LPR > kThreads ? LPR : kThreads;
-  hipLaunchKernelGGL((block_norms_kernel<T, V, LPR, NV>), dim3(ceil_div(p.rows, threads / LPR)), dim3(threads), 0, s, p);
+  hipLaunchKernelGGL((block_norms_kernel<T, V, LPR, NV, Ragged>), dim3(ceil_div(p.rows, threads / LPR)), dim3(threads), 0, s, p);
 }
 
-// Four channels an access where every row allows it, else one.
+// As few lanes a row as keep to 20 channels each (more cost registers, and with them rows in
+// flight).
+template <typename T, bool Ragged>
+static void launch_norms_width(const BlockNormsParams& p, hipStream_t s) {
+  const int H = p.hidden;
+  if (H <= 16 * 4 * 2) launch_norms<T, 4, 16, 2, Ragged>(p, s);
+  else if (H <= 32 * 4 * 3) launch_norms<T, 4, 32, 3, Ragged>(p, s);
+  else if (H <= 64 * 4 * 5) launch_norms<T, 4, 64, 5, Ragged>(p, s);
+  else if (H <= 256 * 4 * 2) launch_norms<T, 4, 256, 2, Ragged>(p, s);
+  else if (H <= 256 * 4 * 5) launch_norms<T, 4, 256, 5, Ragged>(p, s);
+  else launch_norms<T, 4, 1024, 8, Ragged>(p, s);
+}
+
 template <typename T>
 static void launch_norms_t(const BlockNormsParams& p, hipStream_t s) {
-  const int H = p.hidden;
-  bool four = H % 4 == 0 && p.mod_stride % 4 == 0;
+  bool even = p.hidden % 4 == 0 && p.mod_stride % 4 == 0;
   for (const void* q : {(const void*)p.gate, (const void*)p.shift, (const void*)p.scale, (const void*)p.post.weight,
                         (const void*)p.post.bias, (const void*)p.pre.weight, (const void*)p.pre.bias,
                         (const void*)p.h, (const void*)p.h_out})
-    four = four && aligned(q, 16);
-  four = four && aligned(p.y, 4 * sizeof(T)) && aligned(p.out, 4 * sizeof(T)) && p.h_stride % 4 == 0 &&
+    even = even && aligned(q, 16);
+  even = even && aligned(p.y, 4 * sizeof(T)) && aligned(p.out, 4 * sizeof(T)) && p.h_stride % 4 == 0 &&
          p.h_out_stride % 4 == 0 && p.y_stride % 4 == 0 && p.out_stride % 4 == 0;
-  if (four) {
-    if (H <= 32 * 4 * 3) launch_norms<T, 4, 32, 3>(p, s);
-    else if (H <= 64 * 4 * 5) launch_norms<T, 4, 64, 5>(p, s);
-    else if (H <= 256 * 4 * 5) launch_norms<T, 4, 256, 5>(p, s);
-    else launch_norms<T, 4, 1024, 8>(p, s);
-  } else {
-    if (H <= 64 * 8) launch_norms<T, 1, 64, 8>(p, s);
-    else if (H <= 256 * 5) launch_norms<T, 1, 256, 5>(p, s);
-    else if (H <= 256 * 20) launch_norms<T, 1, 256, 20>(p, s);
-    else launch_norms<T, 1, 1024, 32>(p, s);
-  }
+  if (p.hidden < 4) launch_norms<T, 1, 16, 1, false>(p, s);
+  else if (even) launch_norms_width<T, false>(p, s);
+  else launch_norms_width<T, true>(p, s);
 }
 
-template <typename T, int V, int LPR, int NV>
+template <typename T, int V, int LPR, int NV, bool Ragged>
 static void launch_quant(const QuantizeRowsParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((quantize_rows_kernel<T, V, LPR, NV>), dim3(ceil_div(p.rows, kThreads / LPR)), dim3(kThreads), 0, s,
+  hipLaunchKernelGGL((quantize_rows_kernel<T, V, LPR, NV, Ragged>), dim3(ceil_div(p.rows, kThreads / LPR)), dim3(kThreads), 0, s,
                      reinterpret_cast<const T*>(p.x), p.x_stride, p.rows, p.cols, p.codes, p.codes_stride, p.scales);
+}
+
+template <typename T, bool Ragged>
+static void launch_quant_width(const QuantizeRowsParams& p, hipStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  if (p.cols <= 16 * V * 2) launch_quant<T, V, 16, 2, Ragged>(p, s);
+  else if (p.cols <= 32 * V * 5) launch_quant<T, V, 32, 5, Ragged>(p, s);
+  else if (p.cols <= 64 * V * 9) launch_quant<T, V, 64, 9, Ragged>(p, s);
+  else if (p.cols <= 256 * V * 9) launch_quant<T, V, 256, 9, Ragged>(p, s);
+  else launch_quant<T, V, 256, 0, Ragged>(p, s);
 }
 
 template <typename T>
 static void launch_quant_t(const QuantizeRowsParams& p, hipStream_t s) {
   constexpr int V = 16 / sizeof(T);
-  if (p.cols % V == 0 && aligned(p.x, 16) && p.x_stride % V == 0) {
-    if (p.cols <= 32 * V * 5) launch_quant<T, V, 32, 5>(p, s);
-    else if (p.cols <= 64 * V * 9) launch_quant<T, V, 64, 9>(p, s);
-    else if (p.cols <= 256 * V * 9) launch_quant<T, V, 256, 9>(p, s);
-    else launch_quant<T, V, 256, 0>(p, s);
-  } else {
-    if (p.cols <= 64 * 16) launch_quant<T, 1, 64, 16>(p, s);
-    else launch_quant<T, 1, 256, 0>(p, s);
-  }
+  if (p.cols < V) launch_quant<T, 1, 16, 1, false>(p, s);
+  else if (p.cols % V == 0 && aligned(p.x, 16) && p.x_stride % V == 0) launch_quant_width<T, false>(p, s);
+  else launch_quant_width<T, true>(p, s);
 }
 
 }  // namespace norms
