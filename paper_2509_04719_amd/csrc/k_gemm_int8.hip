@@ -126,26 +126,35 @@ struct Block {
     }
   }
 
+  // what the residual stream and the gate hold at (m, n)
+  struct Stream { f32x4 h, g; };
+  __device__ __forceinline__ void fetch(Stream& s, int m, int n) const {
+    if (EPI == kEpiResidual && m < p.M && n < p.N) {
+      s.h = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(p.out) + (size_t)m * p.N + n);
+      s.g = *reinterpret_cast<const f32x4*>(p.gate + branch(p, m) * p.gate_stride + n);
+    }
+  }
+
   // 16 bytes of outputs from (m, n) on: channels (Vt: tokens) next to each other.  Rows of
   // `out` take 16-byte accesses (p.wide).  held: the same in LDS, where they are.
-  __device__ __forceinline__ void sink(const uint4& v, const char* held, int m, int n) const {
+  __device__ __forceinline__ void sink(const uint4& v, const char* held, int m, int n, const Stream& was) const {
     constexpr int CE = 16 / sizeof(T);
     if (m >= p.M || n >= p.N) return;
     if constexpr (EPI == kEpiResidual) {
-      float* out = reinterpret_cast<float*>(p.out) + (size_t)m * p.N + n;
-      const f32x4 y = __builtin_bit_cast(f32x4, v), hv = *reinterpret_cast<const f32x4*>(out),
-                  g = *reinterpret_cast<const f32x4*>(p.gate + branch(p, m) * p.gate_stride + n);
+      const f32x4 y = __builtin_bit_cast(f32x4, v);
       f32x4 o;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) o[r] = fmaf(g[r], y[r], hv[r]);
-      *reinterpret_cast<f32x4*>(out) = o;
+      for (int r = 0; r < 4; ++r) o[r] = fmaf(was.g[r], y[r], was.h[r]);
+      *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.out) + (size_t)m * p.N + n) = o;
     } else if constexpr (EPI == kEpiQkv) {
       const int b = branch(p, m), tok = m - b * p.rows_per_batch;
       T* d = at(b, tok, n);
       // whole: the 16 bytes lie next to each other (not so at a branch's end, or for V^T's columns
-      // beside K's in one wave's blocks)
-      if (Vt ? m + CE <= p.M && tok + CE <= p.rows_per_batch && ((uintptr_t)d & 15) == 0 : n < 2 * p.hidden) {
-        *reinterpret_cast<uint4*>(d) = v;
+      // beside K's in one wave's blocks); V^T's at any token
+      if (Vt ? m + CE <= p.M && tok + CE <= p.rows_per_batch : n < 2 * p.hidden) {
+        typedef T Any __attribute__((ext_vector_type(CE), aligned(sizeof(T))));
+        if constexpr (Vt) *reinterpret_cast<Any*>(d) = __builtin_bit_cast(Any, v);
+        else *reinterpret_cast<uint4*>(d) = v;
       } else if (held) {
 #pragma unroll 1
         for (int f = 0; f < CE; ++f) one(held_one(held, f), Vt ? m + f : m, Vt ? n : n + f);
@@ -198,6 +207,10 @@ struct Block {
       }
     } else {
       float y[4][4];
+      Stream was[4];
+      if (p.wide)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) fetch(was[g], m0 + lr, n0 + 8 * g + 4 * h);
       values(y, acc, c, sa);
       if (EPI != kEpiQkv && !p.wide) {
 #pragma unroll
@@ -209,16 +222,16 @@ struct Block {
         for (int e = 0; e < 2; ++e) {
           const uint4 v = join(pack(y[e]), pack(y[e + 2]));
           const int x = 16 * h + 8 * e;
-          if constexpr (Vt) sink(v, nullptr, m0 + x, n0 + lr);
-          else sink(v, nullptr, m0 + lr, n0 + x);
+          if constexpr (Vt) sink(v, nullptr, m0 + x, n0 + lr, Stream{});
+          else sink(v, nullptr, m0 + lr, n0 + x, Stream{});
         }
       } else {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const uint4 v = __builtin_bit_cast(uint4, f32x4{y[g][0], y[g][1], y[g][2], y[g][3]});
           const int x = 8 * g + 4 * h;
-          if constexpr (Vt) sink(v, nullptr, m0 + x, n0 + lr);
-          else sink(v, nullptr, m0 + lr, n0 + x);
+          if constexpr (Vt) sink(v, nullptr, m0 + x, n0 + lr, was[g]);
+          else sink(v, nullptr, m0 + lr, n0 + x, was[g]);
         }
       }
     }
@@ -276,6 +289,11 @@ __device__ __forceinline__ void staged(const GemmI8Params& p, const i32x16 (&acc
       int at = lane;
       asm volatile("" : "+v"(at));
       const int nb = i0 + SB <= I ? SB : 1, ch8 = sizeof(T) == 2 ? 4 * nb : 8;    // (a last block of its own: half lines)
+      typename B::Stream was[2][2];
+      if (EPI == kEpiResidual && p.wide) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) blk.fetch(was[x >> 1][x & 1], m + 32 * o + 8 * x + at / 8, along + CE * (at % 8));
+      }
       uint4 v[4];     // chunk 4 k + 2 h + e of block k in bf16, 2 g + h in fp32
 #pragma unroll
       for (int k = 0; k < nb; ++k) {
@@ -305,8 +323,8 @@ __device__ __forceinline__ void staged(const GemmI8Params& p, const i32x16 (&acc
             const int row = q * 8 + at / ch8, ch = at % ch8;
             const char* held = area + row * kLine + ch * 16;
             const uint4 w = *reinterpret_cast<const uint4*>(held);
-            if constexpr (Vt) blk.sink(w, held, along + CE * ch, across + row);
-            else blk.sink(w, held, across + row, along + CE * ch);
+            if constexpr (Vt) blk.sink(w, held, along + CE * ch, across + row, was[pass][q]);
+            else blk.sink(w, held, across + row, along + CE * ch, was[pass][q]);
           }
         } else {        // (rows of out that 16 bytes do not fit: an element a lane)
           const int per = ch8 * CE;
@@ -883,8 +901,12 @@ enum Form { k256x256, k192x256, k128x128, k128x128Alone, k64x64, k32x64, k32x32,
 template <typename T, int EPI>
 static void launch_form(int f, const GemmI8Params& p, hipStream_t s) {
   switch (f) {
-    case k256x256: launch_big<256, T, EPI>(p, s); break;
-    case k192x256: launch_big<192, T, EPI>(p, s); break;
+    case k256x256:
+      if constexpr (EPI != kEpiResidual) launch_big<256, T, EPI>(p, s);
+      break;
+    case k192x256:
+      if constexpr (EPI != kEpiResidual) launch_big<192, T, EPI>(p, s);
+      break;
     case k128x128: launch_ring<128, 128, 2, 2, 2, 2, T, EPI>(p, s); break;
     case k128x128Alone: launch_ring<128, 128, 4, 2, 4, 2, T, EPI>(p, s); break;
     case k64x64: launch_ring<64, 64, 2, 2, 4, 2, T, EPI>(p, s); break;
@@ -905,9 +927,9 @@ static void launch_form(int f, const GemmI8Params& p, hipStream_t s) {
 // one's outputs are written beside another's products.
 struct Plan { int form, splits; };
 
-static Plan pick(int M, int N, int K, size_t ws_elems) {
+static Plan pick(int M, int N, int K, int epi, size_t ws_elems) {
   const int f = forced(), kt = ceil_div(K, 128);
-  if (f >= 0 && f < kForms) return {f, 1};
+  if (f >= 0 && f < kForms && (f > k192x256 || epi != kEpiResidual)) return {f, 1};
   float best = 0.0f;
   int form = -1;
   auto tiles = [&](int bm, int bn) { return (float)ceil_div(M, bm) * ceil_div(N, bn); };
@@ -916,8 +938,12 @@ static Plan pick(int M, int N, int K, size_t ws_elems) {
     if (form < 0 || us < best) form = c, best = us;
   };
   const float k = (float)kt, t128 = tiles(128, 128), t64 = tiles(64, 64), t3264 = tiles(32, 64), t32 = tiles(32, 32);
-  take(k256x256, 2.5f + rounds(tiles(256, 256)) * (8.0f + 1.4f * k));
-  take(k192x256, 2.5f + rounds(tiles(192, 256)) * (6.5f + 1.1f * k));
+  // (not for the gated residual, whose stream a lone workgroup waits for: 32205 x 2176 -> 1280 157 us,
+  // 154 in 128 x 128 tiles; 12288 x 1152 -> 1152 44 and 39.5)
+  if (epi != kEpiResidual) {
+    take(k256x256, 2.5f + rounds(tiles(256, 256)) * (8.0f + 1.4f * k));
+    take(k192x256, 2.5f + rounds(tiles(192, 256)) * (6.5f + 1.1f * k));
+  }
   take(k128x128, t128 <= 256 ? 5.5f + 0.65f * k : 3.0f + t128 / 512 * (4.0f + k));
   take(k128x128Alone, 4.0f + rounds(t128) * (2.5f + 0.3f * k) + t128 / 256 * (2.5f + 0.22f * k));
   take(k64x64, t64 <= 256 ? 3.5f + 0.2f * k : 3.0f + t64 / 512 * (1.0f + 0.45f * k));
@@ -946,7 +972,7 @@ static hipError_t launch_t(const GemmI8Params& p0, hipStream_t s) {
     p.rpb_shift = 31 + l;
     p.rpb_inverse = (unsigned)(((1ull << p.rpb_shift) + p.rows_per_batch - 1) / p.rows_per_batch);
   }
-  const Plan pl = pick(p.M, p.N, p.K, p.ws ? p.ws_elems : 0);
+  const Plan pl = pick(p.M, p.N, p.K, EPI, p.ws ? p.ws_elems : 0);
   p.splits = pl.splits;
   if (pl.splits > 1) {
     launch_small<32, 32, 4, 3, T, kEpiPartial>(p, s);
@@ -972,7 +998,7 @@ static hipError_t launch_epi(const GemmI8Params& p, int epi, hipStream_t s) {
 }  // namespace i8
 
 size_t gemm_int8_workspace_bytes(int M, int N, int K) {
-  const i8::Plan pl = i8::pick(M, N, K, (size_t)-1);
+  const i8::Plan pl = i8::pick(M, N, K, kEpiStore, (size_t)-1);
   return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0;
 }
 
