@@ -541,14 +541,20 @@ _NO_NORM.devices, _NO_NORM.channels, _NO_NORM.packed = (), None, bytes(_NO_NORM)
 _BLOCK_NORMS = struct.Struct("=24s24sf3i13Q")   # orch_block_norms' layout
 
 
+_HERE = None            # torch's runtime functions, at the first use
+
+
 def _stream_here(stream, device, *others):
     """_stream_on for tensors of one device: a current GPU that is theirs needs no second look."""
+    global _HERE
     if device < 0 or stream is not None or others.count(device) != len(others):
         return _stream_on(stream, device, *others)
-    from torch import _C
-    if _C._cuda_getDevice() != device:
+    if _HERE is None:
+        from torch import _C
+        _HERE = _C._cuda_getDevice, _C._cuda_getCurrentRawStream
+    if _HERE[0]() != device:
         return _stream_on(stream, device)
-    return _C._cuda_getCurrentRawStream(device)
+    return _HERE[1](device)
 
 
 def block_norms(h, y=None, h_out=None, out=None, *, post=None, pre=None, gate=None, shift=None, scale=None,
