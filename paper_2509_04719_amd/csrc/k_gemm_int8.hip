@@ -262,6 +262,17 @@ __device__ __forceinline__ void direct(const GemmI8Params& p, const i32x16 (&acc
 // wave's own; rows 144 bytes apart spread over the banks.
 constexpr int kLine = 144, kArea = 16 * kLine;
 
+// What the lanes of the wave wrote to LDS before is what they read behind it.  (LDS takes a
+// wave's accesses in order, so this is no instruction; but it keeps the compiler from sending
+// lanes that write and lanes that do not through copies of the code one after the other.)
+__device__ __forceinline__ void wave_sync() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#endif
+}
+
 template <typename T, int EPI, bool Vt, int FM, int FN>
 __device__ __forceinline__ void staged(const GemmI8Params& p, const i32x16 (&acc)[FM][FN], char* area, const float* sa,
                                        const float* sw, const float* bias, int lane, int m, int n) {
@@ -310,12 +321,14 @@ __device__ __forceinline__ void staged(const GemmI8Params& p, const i32x16 (&acc
       }
 #pragma unroll
       for (int pass = 0; pass < 2; ++pass) {
+        wave_sync();
         if ((lr >> 4) == pass) {
 #pragma unroll
           for (int x = 0; x < ch8 / 2; ++x)
             *reinterpret_cast<uint4*>(area + (lr & 15) * kLine +
                                       (sizeof(T) == 2 ? 4 * (x >> 1) + 2 * h + (x & 1) : 2 * x + h) * 16) = v[x];
         }
+        wave_sync();
         const int across = (Vt ? n : m) + 32 * o + 16 * pass;
         if (EPI == kEpiQkv || p.wide) {
 #pragma unroll
@@ -334,7 +347,6 @@ __device__ __forceinline__ void staged(const GemmI8Params& p, const i32x16 (&acc
             blk.element(B::held_one(area + row * kLine, c), across + row, along + c);
           }
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
@@ -355,14 +367,14 @@ __device__ __forceinline__ i32x16 mfma(const i32x4& a, const i32x4& w, const i32
 #endif
 }
 
-// Which tile workgroup `pid` takes: XCD-major, then groups of 8 tile rows, column-major
+// Which tile workgroup `pid` takes: XCD-major, then groups of GROUP tile rows, column-major
 // inside.
+template <int GROUP>
 struct TileAt {
   int m, n;
   __device__ __forceinline__ TileAt(int tiles_m, int tiles_n, int pid) {
     const int per = tiles_m * tiles_n / 8;
     if (pid < per * 8) pid = (pid & 7) * per + (pid >> 3);
-    constexpr int GROUP = 8;
     const int gid = pid / (GROUP * tiles_n);
     const int first_m = gid * GROUP;
     const int gsz = min(tiles_m - first_m, GROUP);
@@ -419,7 +431,7 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
-  const TileAt at(tiles_m, tiles_n, blockIdx.x);
+  const TileAt<8> at(tiles_m, tiles_n, blockIdx.x);
   const int m0 = at.m * BM, n0 = at.n * BN;
   auto& side = *reinterpret_cast<Side<BM, BN>*>(smem + G::RING);
   typename Side<BM, BN>::Regs sr;
@@ -545,6 +557,9 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
 template <int BM>
 struct BigGeo {
   static constexpr int BN = 256, BK = 128, KK = 4, STAGE = (BM + BN) * BK;
+  // (groups of 4, 8 and 16 tile rows: 192 x 256 tiles, 3328 x 1152 -> 3456 20.4, 21.8, 22.1 us; 256 x 256, 12288 x 1152
+  // -> 3456 70.1, 71.5, 72.8)
+  static constexpr int GROUP = 4;
   static constexpr int FM = BM / 64, IA = BM / 64, LPT = IA + 4;    // blocks of a wave, loads of A's rows, of all
   static constexpr int SIDES = 2 * STAGE, AREAS = SIDES + 2 * (int)sizeof(Side<BM, BN>), LDS = AREAS + 8 * kArea;
   static_assert(BM % 64 == 0 && LDS <= 160 * 1024, "LDS");
@@ -574,7 +589,7 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
       rW = buffer_rsrc(p.W, 0);
       return;
     }
-    const TileAt ta(tiles_m, tiles_n, lt);
+    const TileAt<G::GROUP> ta(tiles_m, tiles_n, lt);
     const int m0 = ta.m * BM, n0 = ta.n * BN;
 #pragma unroll
     for (int j = 0; j < LPT; ++j)
@@ -658,7 +673,7 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
   static_for<0, LPT>([&](auto jc) __attribute__((always_inline)) { load(jc, 0); });
   int st = 0, side = 0;
   for (int ct = blockIdx.x; ct < tiles; ct += gridDim.x) {
-    const TileAt ta(tiles_m, tiles_n, ct);
+    const TileAt<G::GROUP> ta(tiles_m, tiles_n, ct);
     const int m0 = ta.m * BM + wm * (BM / 2), n0 = ta.n * BN + wn * 64;
     auto tile = [&](auto vt) __attribute__((always_inline)) {
       auto step = [&](auto first, auto last) __attribute__((always_inline)) {
@@ -945,7 +960,7 @@ static Plan pick(int M, int N, int K, int epi, size_t ws_elems) {
     take(k192x256, 2.5f + rounds(tiles(192, 256)) * (6.5f + 1.1f * k));
   }
   take(k128x128, t128 <= 256 ? 5.5f + 0.65f * k : 3.0f + t128 / 512 * (4.0f + k));
-  take(k128x128Alone, 4.0f + rounds(t128) * (2.5f + 0.3f * k) + t128 / 256 * (2.5f + 0.22f * k));
+  take(k128x128Alone, 2.0f + rounds(t128) * (2.5f + 0.3f * k) + t128 / 256 * (2.5f + 0.22f * k));
   take(k64x64, t64 <= 256 ? 3.5f + 0.2f * k : 3.0f + t64 / 512 * (1.0f + 0.45f * k));
   take(k32x64, t3264 <= 256 ? 3.2f + 0.22f * k : 3.0f + t3264 / 512 * (1.3f + 0.45f * k));
   take(k32x32, 2.9f + 0.105f * k + (rounds(t32) - 1) * (1.6f + 0.155f * k));
