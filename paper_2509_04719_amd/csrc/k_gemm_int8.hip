@@ -10,6 +10,15 @@
 // Any M, N and K: rows past M and N re-read the last one and are not stored; the
 // bytes past K of the last k-tile are cleared in A's fragments (what W's hold
 // there does not matter then: integers have no NaN).
+//
+// Measured (codes of normal deviates; a large library product of int8 runs at 2164
+// TOP/s, a large copy at 5.07 TB/s): 8192 x 8192 x 8192 (uniform codes) 2420 TOP/s;
+// 32768 x 1152 -> 4608 with GELU 230-240 us (1450-1510), 12288 x 1152 -> 3456 into Q, K and V^T 71
+// (1370), 3328 x 1152 -> 3456 19-21 (1250), 3328 x 4608 -> 1152 into the residual stream 26 (1340),
+// 768 x 1152 -> 4608 11 (740), 1 x 1152 -> 4608 5.2.  With K = 1152 a tile's products take 18400
+// cycles of the matrix cores and its outputs (scales, GELU, rounding) 19600 of the vector
+// units, one after the other in the large tiles; smaller tiles, of which a CU holds two,
+// overlap the two but pull more bytes from L2 than it gives (54 B per ns and CU).
 #include <cmath>
 #include <cstdlib>
 
