@@ -557,17 +557,17 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
 }
 
 // ---------------------------------------------------------------------------
-// BM x 256 tiles, BM 256 or 192, eight waves (2 x 4, BM / 2 x 64 outputs each), k-tiles of 128 bytes in two
-// LDS stages, one workgroup a CU that takes tiles until none is left.  The k-tiles of its
-// tiles are one sequence: one barrier a k-tile, the next one's loads between the MFMAs, and
-// behind a tile's last come the next one's first, whose loads are in flight while the
-// outputs are written.  Behind the last tile the buffers of the loads are empty, so that they
-// fetch nothing.
+// BM x 256 tiles, BM 256 or 192, eight waves (2 x 4, BM / 2 x 64 outputs each), k-tiles of 128
+// bytes in two LDS stages, one workgroup a CU that takes tiles until none is left.  The
+// k-tiles of its tiles are one sequence: one barrier a k-tile, the next one's loads between the
+// MFMAs, and behind a tile's last come the next one's first, whose loads are in flight while
+// the outputs are written.  Behind the last tile the buffers of the loads are empty, so that
+// they fetch nothing.
 template <int BM>
 struct BigGeo {
   static constexpr int BN = 256, BK = 128, KK = 4, STAGE = (BM + BN) * BK;
-  // (groups of 4, 8 and 16 tile rows: 192 x 256 tiles, 3328 x 1152 -> 3456 20.4, 21.8, 22.1 us; 256 x 256, 12288 x 1152
-  // -> 3456 70.1, 71.5, 72.8)
+  // (groups of 4, 8 and 16 tile rows: 192 x 256 tiles, 3328 x 1152 -> 3456 20.4, 21.8, 22.1
+  // us; 256 x 256, 12288 x 1152 -> 3456 70.1, 71.5, 72.8)
   static constexpr int GROUP = 4;
   static constexpr int FM = BM / 64, IA = BM / 64, LPT = IA + 4;    // blocks of a wave, loads of A's rows, of all
   static constexpr int SIDES = 2 * STAGE, AREAS = SIDES + 2 * (int)sizeof(Side<BM, BN>), LDS = AREAS + 8 * kArea;
@@ -643,8 +643,9 @@ __global__ __launch_bounds__(512, 2) void big_kernel(GemmI8Params p, int tiles_m
   for (int kk = 0; kk < KK; ++kk) koff[kk] = ((2 * kk + h) ^ ((lr >> 1) & 7)) * 16;
   const int arow = (wm * (BM / 2) + lr) * BK, brow = BM * BK + (wn * 64 + lr) * BK;
   const int left = p.K - (KT - 1) * BK;     // bytes of k in a tile's last k-tile
-  // the MFMAs of stage st (first: a tile's first k-tile, on sums of 0; last: what lies past K cleared): MFMA e of k-step kk, then its share of the next k-step's fragments
-  // and, in the first k-step, of the loads into the other stage
+  // the MFMAs of stage st: MFMA e of k-step kk, then its share of the next k-step's fragments
+  // and, in the first k-step, of the loads into the other stage.  first: on sums of 0; last: what lies
+  // past K cleared
   auto compute = [&](auto vt, auto first_c, auto last_c, int st) __attribute__((always_inline)) {
     const i32x16 zero = {};
     const char* base = smem + st * STAGE;

@@ -66,13 +66,15 @@ def test_block(orch_lib):
     torch.cuda.synchronize()
     m = to_host(b.mod)
     none, ln, rms = ("none", 0.0), ("layer", 1e-6), ("rms", 1e-6)
-    # norms into codes: half a code off at most, beside what 32 bits lose
+    # norms into codes: half a code off at most, beside what 32 bits lose: 48 roundings (2^-24) of a row's
+    # largest value, which is five deviations, and six of the row itself: below 2e-5 of the largest output
     for codes, h, y, post, i in ((b.u, b.h, None, none, 0), (b.v, b.h, b.y1, rms, 3)):
         h1, u = oi.block_norms(to_host(h), None if y is None else to_host(y), post, ln, m[:, 2], m[:, i], m[:, i + 1], N)
         q, s = _held(codes)
         assert (np.abs(q * s[:, None].astype(np.float64) - u) <= s[:, None] * 0.5 + 2e-5 * np.abs(u).max(1, keepdims=True)).all()
     assert rel_l2(to_host(b.h1), h1) < 1e-6
-    # products of the codes as they are: the output's rounding (2^-8 at most, each)
+    # products of the codes as they are: the output's rounding (2^-8 at most, each), and three of 32 bits
+    # of sums that stay below 40: below 1e-5
     mm = lambda A, name: oi.product(*_held(A), *_held(b.w[name]), to_host(b.bias[name]))
     wq, wkv = oi.qkv(mm(b.u, "qkv"), B, HEADS, kv0, TOKENS, OFF)
     for got, want in ((b.q, wq), (b.kv, wkv), (b.y1, mm(b.a8, "o")), (b.f, oi.gelu_tanh(mm(b.v, "fc1"))), (b.y2, mm(b.f8, "fc2"))):

@@ -250,3 +250,32 @@ def test_split_k(orch_lib, dtype, M, K, N):
             lib.qkv_projection_quantized(A, W, bd, q, kv, M // B + 3, 2, workspace=w)
             qk.append((q, kv))
         assert torch.equal(qk[0][0], qk[1][0]) and torch.equal(qk[0][1], qk[1][1])
+
+
+def test_far_rows(orch_lib, form):
+    """Rows as far apart as they may be: the last of a tile 2^31 bytes behind its first."""
+    lib = orch_lib
+    rng = np.random.default_rng(11)
+    M, K, N, far = 257, 200, 256, (1 << 23) - 16
+    a, w = (rng.integers(-128, 128, (n, K), dtype=np.int8) for n in (M, N))
+    buf = torch.empty((2 * M, far), dtype=torch.int8, device=DEV)       # A's rows, then W's
+    ad, wd = buf[:M, :K], buf[M:M + N, 64:64 + K]
+    ad.copy_(torch.from_numpy(a))
+    wd.copy_(torch.from_numpy(w))
+    one = torch.ones(M, device=DEV)
+    out = torch.empty((M, N), device=DEV)
+    lib.linear_quantized(lib.int8_rows(ad, one), lib.int8_rows(wd, one[:N]), None, lib.EPI_STORE, out)
+    np.testing.assert_array_equal(to_host(out), oi.product(a, np.ones(M), w, np.ones(N)))
+
+
+def test_wide_gates(orch_lib, form):
+    """A gate for every token, as slices of a wider buffer."""
+    lib = orch_lib
+    rng = np.random.default_rng(12)
+    M, K, N = 131, 64, 136
+    A, W, bias, s, *_ = _operands(lib, rng, M, K, N)
+    wide, h = rng.standard_normal((M, 6 * N)).astype(np.float32), rng.standard_normal((M, N)).astype(np.float32)
+    gd, out = to_dev(wide), to_dev(h)
+    lib.linear_quantized(A, W, to_dev(bias), lib.EPI_RESIDUAL, out, gate=gd[:, 2 * N:3 * N], rows_per_batch=1)
+    g, y = wide[:, 2 * N:3 * N].astype(np.float64), s + bias
+    _check(to_host(out), h + g * y, np.abs(g) * (3 * U * np.abs(s) + U * np.abs(y)), "f32")
