@@ -513,6 +513,7 @@ def int8_rows(values, scales) -> Int8Rows:
         raise OrchError(ORCH_EINVAL, f"scales [{rows}] are needed, next to each other")
     if cols > 1 and values.stride(1) != 1:
         raise OrchError(ORCH_EINVAL, "a row's values must be next to each other")
+    _check_ints(rows, cols)     # (the sizes of every call that takes them)
     r = Int8Rows(values.data_ptr(), scales.data_ptr(), values.stride(0))
     r.tensors, r.devices, r.shape = (values, scales), (values.get_device(), scales.get_device()), (rows, cols)
     r.ref, r.address = C.byref(r), C.addressof(r)
@@ -697,7 +698,7 @@ def qkv_projection_quantized(A: Int8Rows, W: Int8Rows, bias, q_out, kv_out, kv_t
         raise OrchError(ORCH_EINVAL, f"q_out must be [B, heads, n_tok, d], contiguous, of {M} tokens and {N} / 3 channels")
     if kv_out.dim() != 2 or kv_out.shape[0] != B or kv_out.dtype is not q_out.dtype:
         raise OrchError(ORCH_EINVAL, f"kv_out must be [{B}, elements] of q_out's type")
-    _check_ints(kv_tokens, tok_offset)
+    _check_ints(B, n_tok, kv_tokens, tok_offset)
     kv_bs, c = kv_out.stride()
     if kv_out.shape[1] < 2 * kv_tokens * heads * d or c != 1:
         raise OrchError(ORCH_EINVAL, f"kv_out must hold {2 * kv_tokens * heads * d} elements a branch, next to each other")
