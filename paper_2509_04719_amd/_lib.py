@@ -672,6 +672,8 @@ def linear_quantized(A: Int8Rows, W: Int8Rows, bias, epilogue, out, gate=None, r
         raise OrchError(ORCH_EINVAL, f"out must be [{M}, {N}], contiguous")
     devices += (out.get_device(),)
     gate_stride = 0
+    if not EPI_STORE <= epilogue <= EPI_RESIDUAL:
+        _check_ints(epilogue, 0)
     if epilogue == EPI_RESIDUAL:
         _check_ints(rows_per_batch, 0)
         if code != ORCH_F32:

@@ -39,3 +39,8 @@ def test_products_past_an_int(lib, M, K, N):
 def test_qkv_past_an_int(lib, B, n, K, N):
     q, kv = torch.empty((B, 1, n, N // 3), device="meta"), torch.empty((B, 2 * 8 * N // 3), device="meta")
     _raises(lib, lambda: lib.qkv_projection_quantized(_rows(lib, B * n, K), _rows(lib, N, K), None, q, kv, 8, 0))
+
+
+@pytest.mark.parametrize("epilogue", [BIG, -BIG, BIG + 1])
+def test_epilogue_past_an_int(lib, epilogue):
+    _raises(lib, lambda: lib.linear_quantized(_rows(lib, 0, 64), _rows(lib, 96, 64), None, epilogue, torch.empty((0, 96), device="meta")))
