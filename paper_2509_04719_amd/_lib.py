@@ -614,10 +614,14 @@ def block_norms(h, y=None, h_out=None, out=None, *, post=None, pre=None, gate=No
         mods.append(t.data_ptr())
     if post.channels not in (None, hidden) or pre.channels not in (None, hidden):
         raise OrchError(ORCH_EINVAL, f"a norm's weight and bias must hold {hidden} channels")
-    if not -0x80000000 <= rows_per_batch <= 0x7fffffff:
-        _check_ints(rows_per_batch, 0)
-    p = _BLOCK_NORMS.pack(post.packed, pre.packed, residual_scale, rows, hidden, rows_per_batch, h.data_ptr(), ptr_y, *mods,
-                          ptr_ho, ptr_o, out8, st_h, st_y, mod_stride or 0, st_ho, st_o)
+    try:
+        p = _BLOCK_NORMS.pack(post.packed, pre.packed, residual_scale, rows, hidden, rows_per_batch, h.data_ptr(), ptr_y, *mods,
+                              ptr_ho, ptr_o, out8, st_h, st_y, mod_stride or 0, st_ho, st_o)
+    except struct.error:
+        _check_ints(rows, hidden, rows_per_batch)
+        raise
+    except OverflowError:
+        raise OrchError(ORCH_EINVAL, f"residual_scale {residual_scale}: past fp32's range") from None
     rc = lib.orch_op_block_norms(p, code, _stream_here(stream, h.get_device(), *others))
     if rc:
         check(rc)

@@ -44,3 +44,17 @@ def test_qkv_past_an_int(lib, B, n, K, N):
 @pytest.mark.parametrize("epilogue", [BIG, -BIG, BIG + 1])
 def test_epilogue_past_an_int(lib, epilogue):
     _raises(lib, lambda: lib.linear_quantized(_rows(lib, 0, 64), _rows(lib, 96, 64), None, epilogue, torch.empty((0, 96), device="meta")))
+
+
+@pytest.mark.parametrize("rows,hidden", [(1 << 31, 1), (BIG, 64), (0, 1 << 31), (0, BIG + 64)])
+def test_norms_past_an_int(lib, rows, hidden):
+    h = torch.empty((rows, hidden), device="meta")
+    _raises(lib, lambda: lib.block_norms(h, None, h))
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e39, float("inf"), float("nan")])
+def test_residual_scale_past_fp32(lib, scale):
+    h = torch.empty((4, 32), device="meta")
+    with pytest.raises(lib.OrchError) as e:
+        lib.block_norms(h, None, h, residual_scale=scale)
+    assert e.value.code == lib.ORCH_EINVAL and "residual_scale" in str(e.value), str(e.value)
