@@ -562,9 +562,15 @@ def block_norms(h, y=None, h_out=None, out=None, *, post=None, pre=None, gate=No
                 rows_per_batch=0, residual_scale=1.0, stream=None):
     """The pass between two blocks, see orch_block_norms: h, h_out fp32 and y, out T [rows, hidden] with
     channels next to each other (out an Int8Rows: as codes), gate, shift and scale fp32 [branches, hidden]
-    with one row stride, norms from norm()."""
+    with one row stride, norms from norm().  What no block that ends (y) or follows (out) uses is ignored."""
     shape = h.shape
     rows, hidden = shape
+    if y is None:
+        post = gate = None
+    if out is None:
+        pre = shift = scale = None
+        if h_out is None and rows:
+            raise OrchError(ORCH_EINVAL, "nothing to write: h_out and out are None")
     post, pre = post or _NO_NORM, pre or _NO_NORM
     others = post.devices + pre.devices
     f32, one = _f32(), hidden == 1
