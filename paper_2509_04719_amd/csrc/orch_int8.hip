@@ -36,7 +36,7 @@ int launched(hipError_t e, const char* what) {
 
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
-// No stride is as long as this (elements); below it no offset of 2^24 rows wraps.
+// No stride is as long as this (elements); how far rows reach is checked beside it (Rows::far).
 constexpr size_t kFar = (size_t)1 << 40;
 constexpr int kMaxRows = 1 << 24, kMaxHidden = 32768, kMaxCols = 131071;
 constexpr size_t kMaxInt8Stride = (size_t)1 << 23;
@@ -46,6 +46,11 @@ struct Rows {
   const void* p;
   size_t rows, bytes, stride;
   size_t span() const { return rows ? (rows - 1) * stride + bytes : 0; }
+  // Past 2^62 bytes, where no memory is: below it neither span() nor an offset wraps.
+  bool far() const {
+    size_t s;
+    return p && rows > 1 && (__builtin_mul_overflow(rows - 1, stride, &s) || s >= (size_t)1 << 62);
+  }
 };
 
 // Could a byte be of both?  Rows of one stride may lie between each other (two slices of a
@@ -169,6 +174,8 @@ int orch_op_block_norms(const orch_block_norms* a, int dtype, void* hip_stream) 
   const Rows outs[] = {h_out, out, codes, code_scales};
   const orch_norm none{};
   const orch_norm &post = a->y ? a->post : none, &pre = u ? a->pre : none;
+  for (const Rows& r : {h, y, h_out, out, Rows{gate ? gate : shift ? shift : scale, (size_t)branches, h4, ms}})
+    if (r.far()) return fail("strides: rows reach past 64-bit addresses");
   const Rows in[] = {h, y, {gate, (size_t)branches, h4, ms}, {shift, (size_t)branches, h4, ms}, {scale, (size_t)branches, h4, ms},
                      {post.weight, 1, h4, 0}, {post.bias, 1, h4, 0}, {pre.weight, 1, h4, 0}, {pre.bias, 1, h4, 0}};
   for (int i = 0; i < 4; ++i) {
@@ -205,6 +212,7 @@ int orch_op_quantize_rows(const void* x, size_t x_stride, int rows, int cols, co
   Rows values, scales;
   if (int rc = check_int8(out, "out", rows, cols, &values, &scales, &p.codes_stride)) return rc;
   const Rows in = {x, (size_t)rows, cols * es, x_stride * es};
+  if (in.far()) return fail("x_stride: rows reach past 64-bit addresses");
   if (overlap(in, values) || overlap(in, scales) || overlap(values, scales)) return fail("x and out overlap");
   p.x = x; p.x_stride = rows > 1 ? x_stride : 0; p.rows = rows; p.cols = cols;
   p.codes = (signed char*)out->values; p.scales = out->scales;
@@ -235,6 +243,7 @@ int orch_op_linear_quantized(const orch_int8_rows* A, int M, int K, const orch_i
     if (!aligned(gate, 4)) return fail("gate must be aligned to its elements");
     p.gate = gate; p.gate_stride = branches > 1 ? gate_stride : 0; p.rows_per_batch = rpb;
     in[5] = {gate, branches, (size_t)N * 4, gate_stride * 4};
+    if (in[5].far()) return fail("gate_stride: rows reach past 64-bit addresses");
   }
   const Rows o = {out, 1, (size_t)M * N * es, 0};
   if (int rc = check_outputs(&o, 1, in, ws)) return rc;
@@ -261,6 +270,7 @@ int orch_op_qkv_projection_quantized(const orch_int8_rows* A, int B, int n_tok, 
   if (B > 1 && (kv_bs < branch || kv_bs >= kFar)) return fail("branch stride too small or past 2^40");
   if (!aligned(q_out, 16) || !aligned(kv_out, 16) || (B > 1 && kv_bs * es % 16)) return fail("q_out, kv_out and its branches must be 16-byte aligned");
   const Rows outs[] = {{q_out, 1, (size_t)B * n_tok * hidden * es, 0}, {kv_out, (size_t)B, branch * es, kv_bs * es}};
+  if (outs[1].far()) return fail("branch stride: branches reach past 64-bit addresses");
   if (int rc = check_outputs(outs, 2, in, ws)) return rc;
   p.q = q_out; p.kv = kv_out; p.kv_bs = B > 1 ? kv_bs : 0; p.kv_tokens = kv_tokens; p.tok_offset = tok_offset;
   p.heads = heads; p.hidden = hidden; p.head_dim = head_dim; p.rows_per_batch = n_tok;
