@@ -23,6 +23,8 @@ namespace orch {
 namespace norms {
 
 constexpr int kThreads = 256;
+// Workgroups of 1024 threads along x: a grid's threads are counted in 32 bits, so the rows past these go along y.
+constexpr int kWideRows = 1 << 21;
 
 // v of the lane that DPP control word C names
 template <int C>
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(LPR > kThreads ? LPR : kThreads) void block_norms_k
   constexpr int RPB = LPR > kThreads ? 1 : kThreads / LPR;    // rows of a workgroup
   using S = Share<V, NV, LPR, Ragged>;
   __shared__ unsigned red[LPR > 64 ? 2 * LPR / 64 : 1];
-  const int row = blockIdx.x * RPB + threadIdx.x / LPR;
+  const int row = (LPR > kThreads ? blockIdx.y * kWideRows + blockIdx.x : blockIdx.x * RPB) + threadIdx.x / LPR;
   if (row >= p.rows) return;    // (the whole group of lanes; a group of several waves is a whole workgroup)
   const S sh{(int)(threadIdx.x % LPR), p.hidden};
   Group<LPR> g{red};
@@ -323,7 +325,9 @@ static bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 template <typename T, int V, int LPR, int NV, bool Ragged>
 static void launch_norms(const BlockNormsParams& p, hipStream_t s) {
   constexpr int threads = LPR > kThreads ? LPR : kThreads;
-  hipLaunchKernelGGL((block_norms_kernel<T, V, LPR, NV, Ragged>), dim3(ceil_div(p.rows, threads / LPR)), dim3(threads), 0, s, p);
+  const int groups = ceil_div(p.rows, threads / LPR);
+  const dim3 grid = LPR > kThreads && groups > kWideRows ? dim3(kWideRows, ceil_div(groups, kWideRows)) : dim3(groups);
+  hipLaunchKernelGGL((block_norms_kernel<T, V, LPR, NV, Ragged>), grid, dim3(threads), 0, s, p);
 }
 
 // As few lanes a row as keep to 20 channels each: more cost registers, and with them rows in
