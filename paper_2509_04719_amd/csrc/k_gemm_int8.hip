@@ -886,57 +886,60 @@ static int forced() {
 }
 
 template <typename K>
-static void allow_lds(K kern, int lds) {
-  (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+static hipError_t allow_lds(K kern, int lds) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
 }
 
 template <int BM, int BN, int WM, int WN, int S, int WPE, typename T, int EPI>
-static void launch_ring(const GemmI8Params& p, hipStream_t s) {
+static hipError_t launch_ring(const GemmI8Params& p, hipStream_t s) {
   using G = Geo<BM, BN, WM, WN, S>;
   auto kern = ring_kernel<BM, BN, WM, WN, S, WPE, T, EPI>;
-  static const bool once = (allow_lds(kern, G::LDS), true);
-  (void)once;
+  static const hipError_t attr = allow_lds(kern, G::LDS);
+  if (attr != hipSuccess) return attr;
   const int tm = ceil_div(p.M, BM), tn = ceil_div(p.N, BN);
   hipLaunchKernelGGL(kern, dim3((unsigned)(tm * tn)), dim3(64 * WM * WN), G::LDS, s, p, tm, tn);
+  return hipGetLastError();
 }
 
 template <int BM, int BN, int KG, int S, typename T, int EPI>
-static void launch_small(const GemmI8Params& p, hipStream_t s) {
+static hipError_t launch_small(const GemmI8Params& p, hipStream_t s) {
   using G = SmallGeo<BM, BN, KG, S>;
   auto kern = small_kernel<BM, BN, KG, S, T, EPI>;
-  static const bool once = (allow_lds(kern, G::LDS), true);
-  (void)once;
+  static const hipError_t attr = allow_lds(kern, G::LDS);
+  if (attr != hipSuccess) return attr;
   const int tn = ceil_div(p.N, BN);
   hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(p.M, BM) * tn * p.splits)), dim3(256), G::LDS, s, p, tn);
+  return hipGetLastError();
 }
 
 // Tiles go round 256 workgroups, one a CU.
 template <int BM, typename T, int EPI>
-static void launch_big(const GemmI8Params& p, hipStream_t s) {
+static hipError_t launch_big(const GemmI8Params& p, hipStream_t s) {
   using G = BigGeo<BM>;
   auto kern = big_kernel<BM, T, EPI>;
-  static const bool once = (allow_lds(kern, G::LDS), true);
-  (void)once;
+  static const hipError_t attr = allow_lds(kern, G::LDS);
+  if (attr != hipSuccess) return attr;
   const int tm = ceil_div(p.M, BM), tn = ceil_div(p.N, G::BN);
   hipLaunchKernelGGL(kern, dim3((unsigned)cmin(tm * tn, 256)), dim3(512), G::LDS, s, p, tm, tn);
+  return hipGetLastError();
 }
 
 enum Form { k256x256, k192x256, k128x128, k128x128Alone, k64x64, k32x64, k32x32, kForms };
 
 template <typename T, int EPI>
-static void launch_form(int f, const GemmI8Params& p, hipStream_t s) {
+static hipError_t launch_form(int f, const GemmI8Params& p, hipStream_t s) {
   switch (f) {
     case k256x256:
-      if constexpr (EPI != kEpiResidual) launch_big<256, T, EPI>(p, s);
-      break;
+      if constexpr (EPI != kEpiResidual) return launch_big<256, T, EPI>(p, s);
+      else return hipErrorInvalidValue;     // (pick() does not take it)
     case k192x256:
-      if constexpr (EPI != kEpiResidual) launch_big<192, T, EPI>(p, s);
-      break;
-    case k128x128: launch_ring<128, 128, 2, 2, 2, 2, T, EPI>(p, s); break;
-    case k128x128Alone: launch_ring<128, 128, 4, 2, 4, 2, T, EPI>(p, s); break;
-    case k64x64: launch_ring<64, 64, 2, 2, 4, 2, T, EPI>(p, s); break;
-    case k32x64: launch_small<32, 64, 2, 3, T, EPI>(p, s); break;
-    default: launch_small<32, 32, 4, 3, T, EPI>(p, s); break;
+      if constexpr (EPI != kEpiResidual) return launch_big<192, T, EPI>(p, s);
+      else return hipErrorInvalidValue;     // (pick() does not take it)
+    case k128x128: return launch_ring<128, 128, 2, 2, 2, 2, T, EPI>(p, s);
+    case k128x128Alone: return launch_ring<128, 128, 4, 2, 4, 2, T, EPI>(p, s);
+    case k64x64: return launch_ring<64, 64, 2, 2, 4, 2, T, EPI>(p, s);
+    case k32x64: return launch_small<32, 64, 2, 3, T, EPI>(p, s);
+    default: return launch_small<32, 32, 4, 3, T, EPI>(p, s);
   }
 }
 
@@ -1000,13 +1003,12 @@ static hipError_t launch_t(const GemmI8Params& p0, hipStream_t s) {
   const Plan pl = pick(p.M, p.N, p.K, EPI, p.ws ? p.ws_elems : 0);
   p.splits = pl.splits;
   if (pl.splits > 1) {
-    launch_small<32, 32, 4, 3, T, kEpiPartial>(p, s);
+    if (const hipError_t e = launch_small<32, 32, 4, 3, T, kEpiPartial>(p, s); e != hipSuccess) return e;
     const int bn = ceil_div(p.N, 32), blocks = ceil_div(p.M, 32) * bn;
     hipLaunchKernelGGL((split_sum_kernel<T, EPI>), dim3(blocks), dim3(256), 0, s, p, bn);
-  } else {
-    launch_form<T, EPI>(pl.form, p, s);
+    return hipGetLastError();
   }
-  return hipGetLastError();
+  return launch_form<T, EPI>(pl.form, p, s);
 }
 
 template <typename T>
