@@ -536,13 +536,16 @@ typedef struct {
 } orch_block_norms;
 
 /* One pass over memory, everything in fp32 (statistics of two passes over the row in
- * registers; squares of 1e19 and more are past its range, and such rows come out as 0 or NaN), one
- * rounding to T.  out8: as orch_op_quantize_rows of u, which is not
+ * registers), one rounding to T.  A norm needs a row whose sum of squares fp32 holds (RMS;
+ * LAYER: of squares about its mean, and its sum of magnitudes), below 2^128: a root mean
+ * square, or standard deviation, below 2^64 / sqrt(hidden), 5.4e17 for 1152 channels.  Rows
+ * past that come out as 0 or NaN.  out8: as orch_op_quantize_rows of u, which is not
  * rounded to T before.  h_out may be h and out may be y, with the same strides.  Any
  * element-aligned address and stride is taken; four channels an access where all
  * rows are aligned to it.  No rows are no error.  Errors: ORCH_EINVAL (kinds, eps, hidden
- * outside 1 .. 32768, 2^24 rows or more, strides, alignment, neither h_out nor out nor out8, both
- * out and out8, an output that overlaps another buffer otherwise), ORCH_EHIP. */
+ * outside 1 .. 32768, 2^24 rows or more, strides, rows that reach past 64-bit addresses,
+ * alignment, neither h_out nor out nor out8, both out and out8, an output that overlaps
+ * another buffer otherwise), ORCH_EHIP. */
 int orch_op_block_norms(const orch_block_norms* p, int dtype, void* hip_stream);
 
 /* Rows of x (T, x_stride elements apart) to int8 with a scale each: q = x * (127 / m) to
