@@ -11,14 +11,26 @@
 // bytes past K of the last k-tile are cleared in A's fragments (what W's hold
 // there does not matter then: integers have no NaN).
 //
-// Measured (codes of normal deviates; a large library product of int8 runs at 2164
-// TOP/s, a large copy at 5.07 TB/s): 8192 x 8192 x 8192 (uniform codes) 2420 TOP/s;
-// 32768 x 1152 -> 4608 with GELU 230-240 us (1450-1510), 12288 x 1152 -> 3456 into Q, K and V^T 71
-// (1370), 3328 x 1152 -> 3456 19-21 (1250), 3328 x 4608 -> 1152 into the residual stream 26 (1340),
-// 768 x 1152 -> 4608 11 (740), 1 x 1152 -> 4608 5.2.  With K = 1152 a tile's products take 18400
-// cycles of the matrix cores and its outputs (scales, GELU, rounding) 19600 of the vector
-// units, one after the other in the large tiles; smaller tiles, of which a CU holds two,
-// overlap the two but pull more bytes from L2 than it gives (54 B per ns and CU).
+// Measured (kernel times, median of 60 over three sets of inputs in turn, codes of normal deviates of
+// uneven channels; the large ones move by 10% with the clock, which falls under their load; a large library
+// product of int8 runs at 2110-2160 TOP/s, a large copy at 5.1 TB/s), us (TOP/s):
+//   8192 x 8192 -> 8192    plain, bf16, uniform codes   475-520  (2120-2310)
+//   32768 x 1152 -> 4608   plain, bf16   206-229  (1520-1690)     plain, fp32   263  (1320)
+//                          GELU, bf16    230-257  (1350-1510)     GELU, fp32    305  (1140)
+//   32768 x 4608 -> 1152   residual      241  (1440)
+//   32205 x 2176 -> 1280   residual      157  (1140)
+//   12288 x 1152 -> 3456   QKV, bf16     71  (1380)               QKV, fp32     105  (930)
+//   12288 x 1152 -> 1152   residual      35-39  (840-930)
+//   3328 x 1152 -> 3456    plain, bf16   19.9  (1330)    QKV, bf16   22.2  (1190)    QKV, fp32   29  (910)
+//   3328 x 1152 -> 4608    GELU, bf16    28.0  (1260)
+//   3328 x 4608 -> 1152    residual      25.8  (1370)
+//   3328 x 1152 -> 1152    residual      14  (630)
+//   768 x 1152 -> 4608     GELU, bf16    10.3  (790)
+//   768 x 4608 -> 1152     residual      11.4  (710)
+//   1 x 1152 -> 4608, GELU 5.0; 1 x 4608 -> 1152, residual 8.1; 96 x 384 -> 1152, QKV 4.6
+// With K = 1152 a tile's products take 18400 cycles of the matrix cores and its outputs (scales, GELU,
+// rounding) 19600 of the vector units, one after the other in the large tiles; smaller tiles, of which a
+// CU holds two, overlap the two but pull more bytes from L2 than it gives (54 B per ns and CU).
 #include <cmath>
 #include <cstdlib>
 
@@ -266,8 +278,10 @@ __device__ __forceinline__ void direct(const GemmI8Params& p, const i32x16 (&acc
 }
 
 // The same by way of LDS, so that a store instruction writes whole 128-byte lines (eight
-// rows of 64 bf16 or 32 fp32; stores straight from the registers write 32 bytes of 32 rows:
-// 32768 x 1152 -> 4608 took 231 us, by way of LDS 213).  16 rows at a time in an area of the
+// rows of 64 bf16 or 32 fp32) and addresses are formed for one line at a time.  Stores straight from
+// the registers write 32 bytes of 32 rows: 256 x 256 tiles spill (6 to 600 registers), 192 x 256 ones take,
+// plain, bf16, 250 us for 235-244 at 32768 x 1152 -> 4608, 91.5 for 90 at 12288 rows, 19.1 for 19.9 where there is
+// one round of tiles (3328 x 1152 -> 3456).  16 rows at a time in an area of the
 // wave's own; rows 144 bytes apart spread over the banks.
 constexpr int kLine = 144, kArea = 16 * kLine;
 
@@ -566,8 +580,8 @@ __global__ __launch_bounds__(64 * WM * WN, WPE) void ring_kernel(GemmI8Params p,
 template <int BM>
 struct BigGeo {
   static constexpr int BN = 256, BK = 128, KK = 4, STAGE = (BM + BN) * BK;
-  // (groups of 4, 8 and 16 tile rows: 192 x 256 tiles, 3328 x 1152 -> 3456 20.4, 21.8, 22.1
-  // us; 256 x 256, 12288 x 1152 -> 3456 70.1, 71.5, 72.8)
+  // (groups of 4, 8 and 16 tile rows: 192 x 256 tiles, 3328 x 1152 -> 3456 20.0, 20.1, 20.2
+  // us; 256 x 256, 12288 x 1152 -> 3456, QKV 71-78, 71-76, 75-76, 32768 x 1152 -> 4608, plain 213, 209-215, 218-221)
   static constexpr int GROUP = 4;
   static constexpr int FM = BM / 64, IA = BM / 64, LPT = IA + 4;    // blocks of a wave, loads of A's rows, of all
   static constexpr int SIDES = 2 * STAGE, AREAS = SIDES + 2 * (int)sizeof(Side<BM, BN>), LDS = AREAS + 8 * kArea;
@@ -946,11 +960,11 @@ static hipError_t launch_form(int f, const GemmI8Params& p, hipStream_t s) {
 // The form with the least estimated time in us, T its tiles and KT the k-tiles of 128: fitted to M
 // from 1 to 32768 at the DiT projections of hidden 384 and 1152 and K up to 4608 (one run each,
 // stores of bf16).  Measured, us, 256 x 256 / 192 x 256 / 128 x 128 / alone / 64 x 64 / 32 x 64 / 32 x 32:
-//   32768 x 1152 -> 4608      198 / 210 / 229 / 324 / 383 / 800 / 1900
-//   3328 x 1152 -> 3456        23 /  20 /  22 /  26 /  31 /  58 /  131
-//   3328 x 4608 -> 1152        59 /  50 /  35 /  25 /  36 /  54 /  107
-//   768 x 4608 -> 1152         46 /  38 /  26 /  18 /  11 /  15 /   27
-//   96 x 4608 -> 1152           - /   - /   - /   - / 9.4 / 11.4 / 7.1
+//   32768 x 1152 -> 4608  206-229 / 219 / 234 / 273 / 344 / 813 / 1710
+//   3328 x 1152 -> 3456       22 /  20 /  24 /  26 /  28 /  58 /  132
+//   3328 x 4608 -> 1152       47 /  40 /  29 /  23 /  30 /  50 /   95
+//   768 x 4608 -> 1152        46 /  39 /  26 /  17 /  10 /  15 /   27
+//   96 x 4608 -> 1152          - /   - /   - /   - / 9.0 / 11.6 / 7.5
 // A CU holds one workgroup of the large tiles, of `alone` and of 32 x 32, two of the others, where
 // one's outputs are written beside another's products.
 struct Plan { int form, splits; };
@@ -966,8 +980,8 @@ static Plan pick(int M, int N, int K, int epi, size_t ws_elems) {
     if (form < 0 || us < best) form = c, best = us;
   };
   const float k = (float)kt, t128 = tiles(128, 128), t64 = tiles(64, 64), t3264 = tiles(32, 64), t32 = tiles(32, 32);
-  // (not for the gated residual, whose stream a lone workgroup waits for: 32205 x 2176 -> 1280 157 us,
-  // 154 in 128 x 128 tiles; 12288 x 1152 -> 1152 44 and 39.5)
+  // (not for the gated residual, whose stream a lone workgroup waits for: 32205 x 2176 -> 1280 172 us in 256 x 256
+  // tiles, 161 in 192 x 256, 157 in 128 x 128; 12288 x 1152 -> 1152 36, 44 and 35-39)
   if (epi != kEpiResidual) {
     take(k256x256, 2.5f + rounds(tiles(256, 256)) * (8.0f + 1.4f * k));
     take(k192x256, 2.5f + rounds(tiles(192, 256)) * (6.5f + 1.1f * k));
@@ -978,7 +992,7 @@ static Plan pick(int M, int N, int K, int epi, size_t ws_elems) {
   take(k32x64, t3264 <= 256 ? 3.2f + 0.22f * k : 3.0f + t3264 / 512 * (1.3f + 0.45f * k));
   take(k32x32, 2.9f + 0.105f * k + (rounds(t32) - 1) * (1.6f + 0.155f * k));
   // Few blocks of a long K: its k-tiles over more workgroups, 16 at least each, and a second launch
-  // that adds their sums (32 x 18432 -> 128: 18.3 -> 12.9 us; 131056 111 -> 22)
+  // that adds their sums (32 x 18432 -> 128, plain: 18.2 us, in two launches 5.3 and 7.7; 131056: 113, 11.0 and 10.4)
   if (form == k32x32 && kt >= 96) {
     const int wgs = ceil_div(M, 32) * ceil_div(N, 32), sp = cmin(cmin(256 / cmin(wgs, 256), kMaxSplits), kt / 16);
     if (sp > 1 && (size_t)sp * M * N <= ws_elems) return {form, sp};

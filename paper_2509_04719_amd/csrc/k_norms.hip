@@ -9,13 +9,16 @@
 // workgroup), so the statistics are two-pass (mean, then squares about it) at no
 // cost in memory.
 //
-// Measured (bf16 y and u, a large copy at 5.07 TB/s): 32768 x 1152 (453 MB) 91 us, 5.0
-// TB/s; 3328 x 1152 (46 MB) 10.5 us, 4.4 TB/s; 768 x 1152 5 us, 32 x 128 3.3 us, of them most
-// the launch, one round trip to memory and the reductions' chain.  With a load for each
-// channel group behind a branch of its own (the compiler waits at each) 123, 17.5 and 20.5
-// us.  513 x 1021, rows at any address: 5.6 us, 15.6 with one channel an access.
-// The quantiser: 3328 x 4608 bf16 (46 MB) 10.9 us, 19452 x 3881 fp32 at odd addresses
-// (378 MB) 67 us.
+// Measured (kernel times, three sets of inputs in turn, of which the last-level cache keeps a part; a
+// large copy runs at 5.1 TB/s), RMS norm, gate, LayerNorm and modulation, no weights, bf16 y and u: 32768 x
+// 1152 (453 MB) 85 us, 5.3 TB/s; 3328 x 1152 (46 MB) 11.2 us, 4.1 TB/s; 768 x 1152 5.3 us; into codes 78,
+// 11.8 and 5.8; all fp32 32768 x 1152 (604 MB) 106, 3328 x 1152 12.5, 32 x 128 3.1.  With learned weights
+// 32768 x 1152 92-95.  The smallest are a launch, one round trip to memory and the reductions' chain.
+// Dropped: a load for each channel group behind a branch of its own, at which the compiler waits
+// (1.5 times as long at 32768 rows, 1.6 at 3328, 4 at 768); one channel an access where rows lie at any
+// address (513 x 1021: 2.8 times as long as the 5.4 us now).
+// The quantiser: 3328 x 4608 bf16 (46 MB) 11.2 us, 19452 x 3881 fp32 at odd addresses (378 MB) 66,
+// 333 x 1000 fp32 2.9.
 #include "common.h"
 #include "kernels.h"
 
@@ -330,9 +333,10 @@ static void launch_norms(const BlockNormsParams& p, hipStream_t s) {
   hipLaunchKernelGGL((block_norms_kernel<T, V, LPR, NV, Ragged>), grid, dim3(threads), 0, s, p);
 }
 
-// As few lanes a row as keep to 20 channels each: more cost registers, and with them rows in
-// flight (1152 channels, 64 lanes against 32 of 36 channels: 3328 rows 11.0 and 11.1 us,
-// 32768 rows 83 and 89, 768 rows 4.9 and 6.0; 256 lanes: 11.5, 94 and 5.1).
+// As few lanes a row as keep to 20 channels each: more channels cost registers, and with them rows in
+// flight, and lengthen the chain of a lone row; more lanes share out less (1152 channels in 64 lanes, in 32
+// of 36 channels and in 256, no weights, bf16: 768 rows 5.4, 6.5 and 5.7 us, 3328 rows 11.4, 11.0 and
+// 11.9, 32768 rows 85, 86 and 95).
 template <typename T, bool Ragged>
 static void launch_norms_width(const BlockNormsParams& p, hipStream_t s) {
   const int H = p.hidden;
